@@ -3,6 +3,8 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -10,7 +12,11 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsom.so")
 SOURCES = [os.path.join(CSRC, "som_sweep.hip"), os.path.join(CSRC, "som_rows.hip"),
            os.path.join(CSRC, "som_kernels.hip"), os.path.join(CSRC, "som_update.hip"),
-           os.path.join(CSRC, "som_api.cpp"), os.path.join(CSRC, "som_noalloc.hip")]
+           os.path.join(CSRC, "som_api.cpp"), os.path.join(CSRC, "som_noalloc.hip"),
+           os.path.join(CSRC, "som_mm_nn.hip"), os.path.join(CSRC, "som_mm_nt.hip"),
+           os.path.join(CSRC, "som_mm_tn.hip"), os.path.join(CSRC, "som_route.hip"),
+           os.path.join(CSRC, "som_experts.hip"), os.path.join(CSRC, "som_clip.hip"),
+           os.path.join(CSRC, "som_dense_api.cpp")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -31,13 +37,22 @@ PROBE_LIB = os.path.join(HERE, "libsomprobe.so")
 PROBE_SOURCES = [os.path.join(CSRC, "probe.hip")]
 
 
-def _compile(sources, out, verbose):
-    tmp = out + ".tmp"
-    cmd = [HIPCC, *FLAGS, *sources, "-o", tmp]
+def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
-    os.replace(tmp, out)
+
+
+def _compile(sources, out, verbose):
+    """Each source to an object of its own, as many at once as there are CPUs (up to eight), then one library."""
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in sources]
+        flags = [f for f in FLAGS if f != "-shared"]
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda so: _run([HIPCC, *flags, "-c", so[0], "-o", so[1]], verbose), zip(sources, objects)))
+        linked = out + ".tmp"
+        _run([HIPCC, *FLAGS, *objects, "-o", linked], verbose)
+    os.replace(linked, out)
 
 
 def build(verbose: bool = False) -> str:

@@ -1,0 +1,147 @@
+// som_dense.h -- shared between the host layer of the dense entry points (include/som_dense.h)
+// and their kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/som.h"
+#include "../../include/som_dense.h"
+
+namespace som {
+
+som_status set_error(som_status st, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+
+// ---------------------------------------------------------------- matrix products
+
+// One tile row of a grouped product: the rows [row, end) of the ordered pairs belong to
+// expert e; the tile starts at `row` and takes as many of them as it is high.
+struct TileRow {
+    int32_t e, row, end, pad;
+};
+
+// C = A B with an epilogue. `A` has the M rows of the result (the reduction runs along its
+// columns) except in products over rows (TN), where the reduction runs over the rows of both
+// operands and the result is K_cols(A) x K_cols(B).
+struct Product {
+    const void *A, *B;
+    int64_t lda, ldb;       // elements
+    const int32_t *amap;    // non-null: row r of A is row amap[r] of the array
+    const int32_t *bmap;    // TN only: the same for B
+    int64_t M, N, K;        // result rows and columns, reduction length (grouped: see below)
+    // Grouped products. NN, NT: the tile rows; M is the number of pairs, B and the bias advance
+    // by strideB and strideBias from expert to expert. TN: expert e reduces over the rows
+    // [off[e], off[e + 1]) and the result advances by strideC.
+    const TileRow *tiles;
+    const int32_t *n_tiles;
+    int32_t split;          // workgroup tiles in the height of a tile row
+    const int32_t *off;
+    int32_t groups;         // 0: not grouped
+    int64_t strideB, strideBias, strideC;
+    // Epilogue.
+    const void *bias;
+    int32_t bias_f32, act;
+    const void *res;        // residual, rows' type
+    int64_t ldr;
+    void *out;
+    int64_t ldo;
+    int32_t out_f32;
+    void *pre;              // value before the activation, rows' type: written by NN, read by kSlope
+    int64_t ldp;
+    const float *w;         // a weight for each row (kInner, kPairs, kSlope; TN: of the reduction's rows)
+    float *parts;           // kSlope: per row and column part, the sum of act(pre) * product
+    int64_t n_parts;
+    void *db;               // TN: the column sums of B (each row times w), as bias_f32 says
+    int64_t strideDb;
+};
+
+enum Epilogue {
+    kLinear,  // out = res + act(acc + bias), pre = acc + bias
+    kInner,   // out = w * act(acc + bias), pre = acc + bias
+    kPairs,   // out (fp32) = acc + w * bias
+    kSlope,   // out = w * acc * act'(pre), parts = sum over columns of act(pre) * acc
+    kGrad     // TN: out = acc, db = column sums of B
+};
+
+// Rows of a tile of the product the host picks, so that the plan can lay the tile rows out.
+enum TileSize { kTileSmall, kTileMid, kTileLarge };
+constexpr int tile_rows(TileSize t) { return t == kTileSmall ? 32 : t == kTileMid ? 128 : 256; }
+constexpr int tile_cols(TileSize t) { return t == kTileLarge ? 256 : 128; }
+
+// Tile rows of a plan over P pairs of E experts, at most.
+inline int64_t max_tile_rows(int64_t P, int64_t E, int rows) { return P / rows + (E < P ? E : P); }
+
+hipError_t launch_nn(bool bf16, Epilogue e, TileSize t, const Product &p, hipStream_t st);
+hipError_t launch_nt(bool bf16, Epilogue e, TileSize t, const Product &p, hipStream_t st);
+hipError_t launch_tn(bool bf16, const Product &p, hipStream_t st);
+
+// Columns of a kSlope tile that share a partial sum.
+constexpr int slope_part_cols(TileSize t) { return t == kTileSmall ? 32 : 64; }
+
+// ---------------------------------------------------------------- routing
+
+struct RouteArgs {
+    const void *logits;
+    int64_t ldl;
+    const float *bias;
+    int64_t N;
+    int32_t E, k, score, renorm, groups, group_top;
+    int32_t *idx;            // written by the choice, read by the gradient
+    void *weights;           // the gradient's dweights
+    int32_t weight_type;
+    int32_t *counts;
+    void *dlogits;
+    int64_t lddl;
+};
+
+hipError_t launch_route(int logit_type, const RouteArgs &a, hipStream_t st);
+hipError_t launch_route_bwd(int logit_type, const RouteArgs &a, hipStream_t st);
+
+// ---------------------------------------------------------------- experts
+
+// The pairs (row, place) ordered by expert, in the pairs' order within one.
+struct PairPlan {
+    int32_t *off;       // [E + 1] where each expert's pairs start
+    int32_t *n_tiles;   // [1]
+    TileRow *tiles;     // tile rows of `rows` pairs
+    int32_t *row;       // [P] ordered pair -> row
+    float *w;           // [P] ordered pair -> weight
+    int32_t *pos;       // [P] pair -> its place in the order, -1 for a pair without an expert
+};
+
+hipError_t launch_pairs(bool bf16, const int32_t *idx, const void *w, int64_t P, int32_t k, int32_t E, int rows,
+                        const PairPlan &plan, hipStream_t st);
+
+// out[n] = res[n] + the rows y[pos[n, j]] (fp32, D wide) in the order of j.
+hipError_t launch_combine(bool bf16, const float *y, const int32_t *pos, int64_t N, int32_t k, int64_t D,
+                          const void *res, int64_t ldr, void *out, int64_t ldo, hipStream_t st);
+
+// dw[n, j] = the sum of parts[pos] plus <b2[idx], dout[n]>; 0 for a pair without an expert.
+hipError_t launch_weight_grad(bool bf16, const float *parts, int64_t n_parts, const int32_t *pos, const int32_t *idx,
+                              const void *b2, const void *dout, int64_t lddo, int64_t N, int32_t k, int64_t D,
+                              void *dw, hipStream_t st);
+
+// dz = dy act'(pre), rows of M elements; dz is dense.
+hipError_t launch_slope(bool bf16, const void *dy, int64_t lddy, const void *pre, int64_t ldp, int act, int64_t N,
+                        int64_t M, void *dz, hipStream_t st);
+
+// ---------------------------------------------------------------- clipping
+
+constexpr int kClipTensors = 48;      // tensors of one launch
+constexpr int64_t kClipChunk = 65536; // elements of a workgroup
+
+struct ClipTable {
+    const void *in[kClipTensors];
+    void *out[kClipTensors];
+    int64_t size[kClipTensors];
+    int32_t first[kClipTensors + 1];  // chunks before each tensor
+    int32_t type[kClipTensors];
+    int32_t count;
+};
+
+hipError_t launch_squares(const ClipTable &t, double *partial, hipStream_t st);
+hipError_t launch_norm(const double *partial, int64_t n, float max_norm, float *norm, float *scale, hipStream_t st);
+hipError_t launch_scale(const ClipTable &t, const float *scale, hipStream_t st);
+
+}  // namespace som

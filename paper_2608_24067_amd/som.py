@@ -31,6 +31,8 @@ EXPORTS = (
     "som_bmu_sf_sweep_f16", "som_bmu_sf_finalize", "som_update_workspace_bytes", "som_update", "som_update_f16",
     "som_sigma", "som_radius", "som_bmu_input_flags",
     "som_validate_csr_host", "som_last_error",
+    "som_linear", "som_linear_bwd_workspace_bytes", "som_linear_bwd", "som_route", "som_route_bwd",
+    "som_experts_workspace_bytes", "som_experts", "som_experts_bwd", "som_clip_workspace_bytes", "som_clip",
 )
 
 
@@ -106,6 +108,26 @@ def load():
                  "som_bmu_finalize",
                  "som_bmu2_search", "som_bmu2_sweep", "som_bmu2_finalize", "som_bmu_input_flags",
                  "som_validate_csr_host"):
+        getattr(lib, name).restype = ctypes.c_int
+    # dense rows (dense.py)
+    f32 = ctypes.c_float
+    lib.som_linear.argtypes = [i32, vp, i64, vp, i64, vp, i32, i32, vp, i64, vp, i64, i32, vp, i64, i64, i64, i64, vp]
+    lib.som_linear_bwd_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.som_linear_bwd.argtypes = [i32, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp, i64, vp, i32, i64, i64,
+                                   i64, vp, sz, vp]
+    lib.som_route.argtypes = [i32, vp, i64, vp, i64, i64, i32, vp, vp, i32, vp, vp, vp]
+    lib.som_route_bwd.argtypes = [i32, vp, i64, vp, vp, i32, vp, i64, i64, i32, vp, vp, i64, vp]
+    lib.som_experts_workspace_bytes.argtypes = [i64, i32, i64, i64, i64, i32]
+    lib.som_experts.argtypes = [i32, vp, i64, vp, vp, vp, vp, vp, vp, i32, vp, i64, vp, i64, i64, i32, i64, i64, i64,
+                                i32, vp, sz, vp]
+    lib.som_experts_bwd.argtypes = [i32, vp, i64, vp, vp, vp, vp, vp, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64,
+                                    i32, i64, i64, i64, vp, sz, vp]
+    lib.som_clip_workspace_bytes.argtypes = [vp, i64]
+    lib.som_clip.argtypes = [vp, vp, vp, vp, i64, f32, vp, vp, sz, vp]
+    for name in ("som_linear_bwd_workspace_bytes", "som_experts_workspace_bytes", "som_clip_workspace_bytes"):
+        getattr(lib, name).restype = sz
+    for name in ("som_linear", "som_linear_bwd", "som_route", "som_route_bwd", "som_experts", "som_experts_bwd",
+                 "som_clip"):
         getattr(lib, name).restype = ctypes.c_int
     lib.som_last_error.argtypes = []
     lib.som_last_error.restype = ctypes.c_char_p

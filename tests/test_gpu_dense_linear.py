@@ -1,0 +1,178 @@
+"""som_linear and its gradients against 64-bit products, on the GPU."""
+import pytest
+import torch
+
+import paper_2608_24067_amd.dense as dense
+import paper_2608_24067_amd.som as som
+from dense_ref import LIP, U, act, check, curve, slope, sums, wide
+
+pytestmark = pytest.mark.gpu
+
+HALVES = [torch.float16, torch.bfloat16]
+
+
+def strided(shape, pad, dtype, dev, g, scale=1.0, offset=0):
+    """A matrix whose rows are `pad` elements longer, filled with NaN around it, `offset` elements into its buffer."""
+    buf = torch.full((shape[0] * (shape[1] + pad) + offset,), float("nan"), dtype=dtype, device=dev)
+    t = buf[offset:].view(shape[0], shape[1] + pad)[:, :shape[1]]
+    t.copy_((torch.randn(shape, generator=g) * scale).to(dtype))
+    return t
+
+
+def case(seed, N, K, M, dtype, dev, pad=0, offset=0):
+    g = torch.Generator().manual_seed(seed)
+    x = strided((N, K), pad, dtype, dev, g, offset=offset)
+    W = strided((K, M), pad, dtype, dev, g, K ** -0.5, offset=offset)
+    b = (torch.randn(M, generator=g) * 0.3).to(dev)
+    r = strided((N, M), pad, dtype, dev, g, offset=offset)
+    return x, W, b, r, g
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("N,K,M,pad,offset,a,f32", [
+    (1, 64, 64, 0, 0, "none", True),
+    (1, 1, 1, 0, 0, "gelu", False),          # a single product
+    (1, 1024, 4096, 0, 0, "none", True),     # one row on a 64 x 64 map
+    (2, 24, 8, 0, 0, "relu", False),         # less than a reduction step
+    (3, 31, 33, 0, 0, "silu", False),        # odd everywhere
+    (17, 96, 130, 6, 0, "gelu", False),      # widths that are no chunks, strided rows
+    (16, 40, 72, 8, 8, "none", False),       # chunks in strided rows
+    (33, 257, 129, 0, 1, "none", True),      # rows at any element
+    (64, 128, 128, 0, 0, "silu", False),
+    (100, 1003, 625, 0, 0, "none", True),    # a 25 x 25 map of odd width
+    (128, 64, 4096, 0, 0, "relu", False),
+    (300, 200, 1000, 0, 0, "gelu", False),   # ragged tiles of 128
+    (257, 136, 40000, 0, 0, "none", False),  # ragged tiles of 256
+    (5000, 72, 2600, 24, 0, "gelu", False),  # tiles of 256, a short reduction, strided rows
+])
+def test_linear(dev, dtype, N, K, M, pad, offset, a, f32):
+    x, W, b, r, _ = case(11, N, K, M, dtype, dev, pad, offset)
+    out = torch.full((N, M), float("nan"), dtype=torch.float32 if f32 else dtype, device=dev)
+    pre = torch.empty(N, M, dtype=dtype, device=dev)
+    dense.linear(x, W, b, residual=r, act=a, out=out, pre=pre)
+    z = wide(x) @ wide(W) + wide(b)
+    err = sums(K + 1, wide(x).abs() @ wide(W).abs() + wide(b).abs())
+    check(pre, z, err, "pre")
+    y = act(a, z) + wide(r)
+    check(out, y, LIP * err + 2.0 ** -20 * (z.abs().clamp_min(1) if a != "none" else 0) + 2.0 ** -23 * (z.abs() + wide(r).abs()),
+          "y")
+
+
+def test_plain_product_bias_of_the_rows_type_and_residual_in_place(dev):
+    x, W, b, r, _ = case(12, 70, 64, 96, torch.bfloat16, dev)
+    err = sums(64, wide(x).abs() @ wide(W).abs())
+    check(dense.linear(x, W), wide(x) @ wide(W), err, "product")
+    b = b.to(torch.bfloat16)
+    y = wide(x) @ wide(W) + wide(b) + wide(r)
+    dense.linear(x, W, b, residual=r, out=r)
+    check(r, y, err + 2.0 ** -22 * (y.abs() + wide(b).abs() + 10), "in place")
+
+
+def test_infinities_and_nan_stay_in_their_rows(dev):
+    # also where tiles reach past the last row and the last reduction step
+    for N, K, M in ((40, 70, 30), (260, 72, 1000), (5, 8, 8)):
+        x, W, b, r, _ = case(13, N, K, M, torch.float16, dev)
+        clean = dense.linear(x, W, b)
+        x = x.clone()
+        x[N // 2, K - 1] = float("inf")
+        x[N - 1, 0] = float("nan")
+        got = dense.linear(x, W, b)
+        rows = torch.ones(N, dtype=torch.bool, device=dev)
+        rows[N // 2] = rows[N - 1] = False
+        assert torch.equal(got[rows], clean[rows])
+        assert not torch.isfinite(got[N // 2]).any() and torch.isnan(got[N - 1]).all()
+
+
+def test_scores_rank_units_as_the_search_does(dev):
+    # rows of a few ones, as dense rows: the highest score is the search's unit
+    V, M, N = 96, 225, 64
+    g = torch.Generator().manual_seed(14)
+    W = (torch.randint(0, 256, (V, M), generator=g).float() / 256).half().to(dev)
+    x = (torch.rand(N, V, generator=g) < 0.1)
+    x[0] = False
+    rp = torch.cat([torch.zeros(1, dtype=torch.int64), x.sum(1).cumsum(0)]).int().to(dev)
+    ci = x.nonzero()[:, 1].int().to(dev)
+    norms = som.codebook_norms(W, V, M)
+    bmu, _ = som.bmu_search(W, norms, rp, ci, V, M)
+    scores = dense.linear(x.half().to(dev), W, (-0.5 * norms).float(), out_dtype=torch.float32)
+    idx, _ = dense.route(scores, 1)
+    d = norms - 2 * (x.double().to(dev) @ W.double())
+    picked = d.gather(1, idx.long())[:, 0]
+    best = d.gather(1, bmu.long()[:, None])[:, 0]
+    assert bool(((picked - best).abs() <= 2.0 ** -16 * (1 + norms.max())).all())
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("N,K,M,pad,a,f32", [
+    (1, 1, 1, 0, "silu", False),
+    (1, 64, 128, 0, "gelu", False),
+    (7, 31, 65, 0, "none", True),
+    (33, 64, 40, 8, "relu", False),
+    (100, 130, 257, 3, "gelu", True),
+    (500, 264, 136, 0, "silu", False),
+    (1000, 64, 72, 0, "none", False),
+    (130, 4200, 4104, 0, "none", False),   # tiles of 256 in the weights' gradient
+    (5001, 520, 2056, 0, "gelu", False),
+])
+def test_linear_gradients(dev, dtype, N, K, M, pad, a, f32):
+    x, W, b, _, g = case(15, N, K, M, dtype, dev, pad)
+    dy = strided((N, M), pad, dtype, dev, g)
+    pre = torch.empty(N, M, dtype=dtype, device=dev)
+    dense.linear(x, W, b, act=a, pre=pre)
+    dx, dW, db = dense.linear_bwd(x, W, dy, pre=pre, act=a, bias_dtype=torch.float32 if f32 else None)
+    # the formula on the pre that was kept; dz is rounded once
+    dz = wide(dy) * slope(a, wide(pre))
+    off = (U[dtype] * dz.abs() + 2.0 ** -20 * wide(dy).abs() * wide(pre).abs().clamp_min(1)) if a != "none" else 0 * dz
+    mag = dz.abs() + off
+    check(dx, dz @ wide(W).T, off @ wide(W).abs().T + sums(M, mag @ wide(W).abs().T), "dx")
+    check(dW, wide(x).T @ dz, wide(x).abs().T @ off + sums(N, wide(x).abs().T @ mag), "dW")
+    check(db, dz.sum(0), off.sum(0) + sums(N, mag.sum(0)), "db")
+    assert db.dtype == (torch.float32 if f32 else dtype)
+
+
+@pytest.mark.parametrize("a", ["none", "gelu", "silu", "relu"])
+def test_linear_gradients_against_differences(dev, a):
+    # <dy, y(x + h v) - y(x - h v)> / 2h in 64 bits against <dx, v>, and the same for W and b
+    x, W, b, _, g = case(16, 12, 40, 24, torch.float16, dev)
+    dy = torch.randn(12, 24, generator=g).half().to(dev)
+    pre = torch.empty(12, 24, dtype=torch.float16, device=dev)
+    dense.linear(x, W, b, act=a, pre=pre)
+    grads = dense.linear_bwd(x, W, dy, pre=pre, act=a, bias_dtype=torch.float32)
+    args = [wide(x), wide(W), wide(b)]
+    h = 1e-6
+    for i, grad in enumerate(grads):
+        v = torch.randn(args[i].shape, generator=g, dtype=torch.float64)
+        v /= v.norm()
+        up, down = list(args), list(args)
+        up[i], down[i] = args[i] + h * v, args[i] - h * v
+        f = lambda t: (wide(dy) * act(a, t[0] @ t[1] + t[2])).sum()  # noqa: E731
+        diff = float(f(up) - f(down)) / (2 * h)
+        # each gradient value is off by at most 2^-9 of its terms' magnitude (dz, pre and the result rounded)
+        dz = wide(dy).abs() * LIP
+        terms = [dz @ args[1].abs().T, args[0].abs().T @ dz, dz.sum(0)][i]
+        assert abs(diff - float((wide(grad) * v).sum())) <= 2.0 ** -9 * float((terms * v.abs()).sum()) + 1e-5
+
+
+def test_parts_of_the_gradient_and_no_rows(dev):
+    x, W, b, _, g = case(17, 40, 48, 56, torch.bfloat16, dev)
+    dy = torch.randn(40, 56, generator=g).bfloat16().to(dev)
+    whole = dense.linear_bwd(x, W, dy)
+    for i in range(3):
+        out = [None, None, None]
+        out[i] = torch.full_like(whole[i], float("nan"))
+        assert torch.equal(dense.linear_bwd(x, W, dy, out=out)[i], whole[i])
+    dx, dW, db = dense.linear_bwd(x[:0], W, dy[:0])
+    assert dx.shape == (0, 48) and not dW.any() and not db.any()
+    assert dense.linear(x[:0], W, b).shape == (0, 56)
+
+
+def test_another_stream_and_repeats_give_the_same_bits(dev):
+    x, W, b, r, g = case(18, 777, 520, 264, torch.bfloat16, dev)
+    dy = torch.randn(777, 264, generator=g).bfloat16().to(dev)
+    first = (dense.linear(x, W, b, residual=r),) + dense.linear_bwd(x, W, dy)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = (dense.linear(x, W, b, residual=r),) + dense.linear_bwd(x, W, dy)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(first, again))

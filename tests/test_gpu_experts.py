@@ -1,0 +1,227 @@
+"""som_experts and its gradients against an expert-by-expert form in 64 bits, on the GPU."""
+import pytest
+import torch
+
+import paper_2608_24067_amd.dense as dense
+from dense_ref import LIP, U, act, check, curve, slope, sums, wide
+
+pytestmark = pytest.mark.gpu
+
+
+def case(seed, N, k, E, D, F, dtype, dev, empty=0.1, lonely=False, ones=False):
+    g = torch.Generator().manual_seed(seed)
+
+    def normal(*shape, scale=1.0):
+        return (torch.randn(shape, generator=g) * scale).to(dtype).to(dev)
+
+    s = dict(x=normal(N, D), W1=normal(E, D, F, scale=D ** -0.5), b1=normal(E, F, scale=0.2),
+             W2=normal(E, F, D, scale=F ** -0.5), b2=normal(E, D, scale=0.2))
+    idx = torch.randint(0, E, (N, k), generator=g, dtype=torch.int32)  # an expert may stand twice in a row
+    if lonely:
+        idx[:] = E - 1  # one expert takes all
+    idx[torch.rand(N, k, generator=g) < empty] = -1
+    if N > 2:
+        idx[N // 2] = -1  # a row that no expert takes
+        idx[0, 0] = E + 3  # an index that is none
+    s["idx"] = idx.to(dev)
+    s["w"] = (torch.rand(N, k, generator=g) + 0.1).to(dtype).to(dev)
+    s["w"][N - 1] = 0
+    return s, g
+
+
+def forms(s, a, res):
+    """out and the bound of what is rounded or summed before it."""
+    x, w, idx = wide(s["x"]), wide(s["w"]), s["idx"].cpu()
+    E, u = s["W1"].shape[0], U[s["x"].dtype]
+    D, F = s["W1"].shape[1:]
+    out = wide(res).clone() if res is not None else torch.zeros_like(x)
+    bound = 2.0 ** -20 * (out.abs() + 1)
+    for e in range(E):
+        n, j = (idx == e).nonzero(as_tuple=True)
+        if not n.numel():
+            continue
+        W1, W2 = wide(s["W1"][e]), wide(s["W2"][e])
+        b1 = wide(s["b1"][e]) if s["b1"] is not None else torch.zeros(F, dtype=torch.float64)
+        b2 = wide(s["b2"][e]) if s["b2"] is not None else torch.zeros(D, dtype=torch.float64)
+        z = x[n] @ W1 + b1
+        dz = sums(D + 1, x[n].abs() @ W1.abs() + b1.abs())
+        we = w[n, j][:, None]
+        h = we * act(a, z)
+        dh = u * h.abs() + we * (LIP * dz + 2.0 ** -20 * z.abs().clamp_min(1))
+        out.index_add_(0, n, h @ W2 + we * b2)
+        bound.index_add_(0, n, dh @ W2.abs() + sums(F + 2, (h.abs() + dh) @ W2.abs() + we * b2.abs()))
+    return out, bound
+
+
+SHAPES = [
+    (1, 1, 1, 8, 8), (1, 2, 4, 64, 128), (1, 2, 64, 256, 512), (3, 2, 5, 31, 33), (4, 4, 3, 24, 40),
+    (17, 3, 7, 65, 130), (33, 4, 32, 128, 96), (100, 2, 8, 72, 200), (700, 2, 3, 136, 264), (2000, 1, 4, 100, 50),
+    (600, 32, 2, 64, 72), (40, 2, 1024, 16, 24),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("N,k,E,D,F", SHAPES)
+def test_experts(dev, dtype, N, k, E, D, F):
+    for a, lonely in (("gelu", False), ("none", True)):
+        s, g = case(31, N, k, E, D, F, dtype, dev, lonely=lonely)
+        out = dense.experts(**s, act=a, residual=s["x"])
+        ref, bound = forms(s, a, s["x"])
+        check(out, ref, bound, f"out, {a}")
+
+
+def test_tiles_of_every_size(dev):
+    # enough rows and columns for tiles of 128 and 256, aligned or not
+    for N, k, E, D, F, off in ((1500, 2, 5, 1024, 1160, 0), (5000, 2, 4, 2048, 2056, 0), (5000, 2, 4, 2048, 2056, 1)):
+        s, g = case(32, N, k, E, D, F, torch.bfloat16, dev, empty=0.3)
+        if off:  # the rows start at any element
+            buf = torch.empty(N * (D + off), dtype=torch.bfloat16, device=dev).view(N, D + off)[:, off:]
+            buf.copy_(s["x"])
+            s["x"] = buf
+        out = dense.experts(**s, act="silu")
+        ref, bound = forms(s, "silu", None)
+        check(out, ref, bound, f"out {N}")
+
+
+def test_without_biases_in_place_and_strided(dev):
+    s, g = case(33, 50, 2, 6, 64, 80, torch.float16, dev)
+    s["b1"] = s["b2"] = None
+    buf = torch.full((50, 96), float("nan"), dtype=torch.float16, device=dev)
+    res = buf[:, 8:72]
+    res.copy_(torch.randn(50, 64, generator=g).half())
+    ref, bound = forms(s, "relu", res)
+    dense.experts(**s, act="relu", residual=res, out=res)
+    check(res, ref, bound, "in place")
+    assert torch.isnan(buf[:, :8]).all() and torch.isnan(buf[:, 72:]).all()
+
+
+def gradients(s, a, dout, pre):
+    """By the formulas, with the slopes at the z that is held in the rows' type; and their bounds."""
+    x, w, idx, g = wide(s["x"]), wide(s["w"]), s["idx"].cpu(), wide(dout)
+    E, u = s["W1"].shape[0], U[s["x"].dtype]
+    D, F = s["W1"].shape[1:]
+    ref = {n: torch.zeros(s[n].shape, dtype=torch.float64) for n in ("x", "w", "W1", "b1", "W2", "b2")}
+    off = {n: torch.zeros_like(t) for n, t in ref.items()}
+    for e in range(E):
+        n, j = (idx == e).nonzero(as_tuple=True)
+        if not n.numel():
+            continue
+        W1, W2, b1, b2 = (wide(s[q][e]) for q in ("W1", "W2", "b1", "b2"))
+        we, ge, xe = w[n, j][:, None], g[n], x[n]
+        z = xe @ W1 + b1
+        ez = u * z.abs() + sums(D + 1, xe.abs() @ W1.abs() + b1.abs())  # z as held
+        h, sl = act(a, z), slope(a, z)
+        eh = LIP * ez + 2.0 ** -20 * z.abs().clamp_min(1)
+        es = curve(a) * ez + 2.0 ** -20 * z.abs().clamp_min(1)
+        if a == "relu":
+            es = es + (z.abs() <= ez).double()  # the kink may lie between z and its rounding
+        q = ge @ W2.T
+        eq = sums(D, ge.abs() @ W2.abs().T)
+        dz = we * q * sl
+        edz = we * (eq * (sl.abs() + es) + q.abs() * es)
+        edz = edz + u * (dz.abs() + edz)
+        nj = (n, j)
+        ref["w"][nj] = (h * q).sum(1) + ge @ b2
+        t = (h.abs() + eh) * (q.abs() + eq)
+        off["w"][nj] = (eh * q.abs() + h.abs() * eq + eh * eq).sum(1) + sums(D + F, t.sum(1) + ge.abs() @ b2.abs())
+        ref["x"].index_add_(0, n, dz @ W1.T)
+        off["x"].index_add_(0, n, edz @ W1.abs().T + sums(F + 34, (dz.abs() + edz) @ W1.abs().T))
+        ref["W1"][e], ref["b1"][e] = xe.T @ dz, dz.sum(0)
+        c = len(n)
+        off["W1"][e] = xe.abs().T @ edz + sums(c, xe.abs().T @ (dz.abs() + edz))
+        off["b1"][e] = edz.sum(0) + sums(c, (dz.abs() + edz).sum(0))
+        hw = we * h
+        ehw = we * (eh + u * h.abs())
+        ref["W2"][e], ref["b2"][e] = hw.T @ ge, (we * ge).sum(0)
+        off["W2"][e] = ehw.T @ ge.abs() + sums(c, (hw.abs() + ehw).T @ ge.abs())
+        off["b2"][e] = sums(c, (we * ge.abs()).sum(0))
+    return ref, off
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("N,k,E,D,F", SHAPES + [(3000, 2, 2, 1032, 520), (5000, 2, 4, 2048, 1160)])
+def test_experts_gradients(dev, dtype, N, k, E, D, F):
+    a = ["gelu", "silu", "relu", "none"][(N + E) % 4]
+    s, g = case(34, N, k, E, D, F, dtype, dev)
+    dout = torch.randn(N, D, generator=g).to(dtype).to(dev)
+    ws = torch.empty(dense.experts_workspace_bytes(N, k, E, D, F, keep=True), dtype=torch.uint8, device=dev)
+    dense.experts(**s, act=a, keep=True, workspace=ws)
+    got = dense.experts_bwd(s["x"], s["idx"], s["w"], s["W1"], s["W2"], s["b2"], dout, act=a, workspace=ws)
+    ref, off = gradients(s, a, dout, None)
+    for name, t in zip(("x", "w", "W1", "b1", "W2", "b2"), got):
+        check(t, ref[name], off[name], f"d{name}, {a}")
+    # the workspace serves again, for a part of the gradients, with the same bits
+    for i in range(6):
+        out = [None] * 6
+        out[i] = torch.full_like(got[i], float("nan"))
+        part = dense.experts_bwd(s["x"], s["idx"], s["w"], s["W1"], s["W2"], s["b2"], dout, act=a, out=out, workspace=ws)
+        assert torch.equal(part[i], got[i])
+
+
+@pytest.mark.parametrize("a", ["gelu", "silu", "none"])
+def test_experts_gradients_against_differences(dev, a):
+    s, g = case(35, 9, 2, 3, 16, 24, torch.float16, dev, empty=0.0)
+    dout = torch.randn(9, 16, generator=g).half().to(dev)
+    ws = torch.empty(dense.experts_workspace_bytes(9, 2, 3, 16, 24, keep=True), dtype=torch.uint8, device=dev)
+    dense.experts(**s, act=a, keep=True, workspace=ws)
+    got = dense.experts_bwd(s["x"], s["idx"], s["w"], s["W1"], s["W2"], s["b2"], dout, act=a, workspace=ws)
+    names = ("x", "w", "W1", "b1", "W2", "b2")
+    args = {n: wide(s[n]) for n in names}
+    idx = s["idx"].cpu().long()
+
+    def f(t):
+        total = 0.0
+        for n in range(9):
+            for j in range(2):
+                e = int(idx[n, j])
+                if 0 <= e < 3:
+                    y = act(a, t["x"][n] @ t["W1"][e] + t["b1"][e]) @ t["W2"][e] + t["b2"][e]
+                    total = total + t["w"][n, j] * (y * wide(dout)[n]).sum()
+        return float(total)
+
+    h = 1e-6
+    _, off = gradients(s, a, dout, None)
+    for name, grad in zip(names, got):
+        v = torch.randn(args[name].shape, generator=g, dtype=torch.float64)
+        diff = (f({**args, name: args[name] + h * v}) - f({**args, name: args[name] - h * v})) / (2 * h)
+        room = ((off[name] + U[torch.float16] * (wide(grad).abs() + off[name])) * v.abs()).sum()
+        assert abs(diff - float((wide(grad) * v).sum())) <= float(room) + 1e-6
+
+
+def test_bad_values_stay_in_their_rows(dev):
+    s, g = case(36, 300, 2, 4, 64, 96, torch.bfloat16, dev)
+    clean = dense.experts(**s)
+    s["x"][150 - 1] = float("nan")
+    s["x"][7] = float("inf")
+    got = dense.experts(**s)
+    keep = torch.ones(300, dtype=torch.bool, device=dev)
+    keep[149] = keep[7] = False
+    assert torch.equal(got[keep], clean[keep])
+
+
+def test_no_rows_and_no_expert(dev):
+    s, g = case(37, 4, 2, 3, 32, 40, torch.float16, dev)
+    s["idx"].fill_(-1)
+    assert torch.equal(dense.experts(**s, residual=s["x"]), s["x"])
+    ws = torch.empty(dense.experts_workspace_bytes(4, 2, 3, 32, 40, keep=True), dtype=torch.uint8, device=dev)
+    dense.experts(**s, keep=True, workspace=ws)
+    grads = dense.experts_bwd(s["x"], s["idx"], s["w"], s["W1"], s["W2"], s["b2"], s["x"], workspace=ws)
+    assert not any(bool(t.any()) for t in grads)
+    none = {n: (t[:0] if n in ("x", "idx", "w") else t) for n, t in s.items()}
+    assert dense.experts(**none).shape == (0, 32)
+    ws = torch.empty(dense.experts_workspace_bytes(0, 2, 3, 32, 40, keep=True), dtype=torch.uint8, device=dev)
+    out = [torch.full_like(s[n], float("nan")) for n in ("W1", "b1", "W2", "b2")]
+    dense.experts_bwd(none["x"], none["idx"], none["w"], s["W1"], s["W2"], s["b2"], none["x"], workspace=ws,
+                      out=[None, None] + out)
+    assert not any(bool(t.any()) for t in out)
+
+
+def test_same_bits_on_another_stream(dev):
+    s, g = case(38, 900, 2, 8, 128, 256, torch.bfloat16, dev)
+    first = dense.experts(**s)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = dense.experts(**s)
+    torch.cuda.synchronize()
+    assert torch.equal(first, again)
