@@ -108,7 +108,18 @@ struct PairPlan {
     int32_t *row;       // [P] ordered pair -> row
     float *w;           // [P] ordered pair -> weight
     int32_t *pos;       // [P] pair -> its place in the order, -1 for a pair without an expert
+    int32_t *counts;    // [pair_stretches(P)][E] scratch
 };
+
+// Up to this many pairs are ordered by one workgroup (2,048 pairs: one launch of about 8 us
+// against three of 4); more in stretches of 512 pairs, at most 256 of them.
+constexpr int64_t kPairsOfOne = 2048;
+inline int pair_stretches(int64_t P)
+{
+    if (P <= kPairsOfOne) return 0;
+    const int64_t n = (P + 511) / 512;
+    return (int)(n < 256 ? n : 256);
+}
 
 hipError_t launch_pairs(bool bf16, const int32_t *idx, const void *w, int64_t P, int32_t k, int32_t E, int rows,
                         const PairPlan &plan, hipStream_t st);

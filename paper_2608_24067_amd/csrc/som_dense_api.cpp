@@ -58,7 +58,7 @@ som::TileSize pick_tile(int64_t rows, int64_t groups, int64_t cols, bool whole)
 // ---------------------------------------------------------------- experts
 
 struct ExpertsLayout {
-    size_t off, n_tiles, tiles, row, w, pos, inner, y, pre, dz, parts, total;
+    size_t off, n_tiles, tiles, row, w, pos, counts, inner, y, pre, dz, parts, total;
     som::TileSize tile;
     int64_t n_parts;
 };
@@ -84,9 +84,10 @@ ExpertsLayout experts_layout(int64_t N, int32_t k, int64_t E, int64_t D, int64_t
     L.off = take((E + 1) * 4);
     L.n_tiles = take(4);
     L.tiles = take(som::max_tile_rows(P, E, tile_rows(L.tile)) * (int64_t)sizeof(som::TileRow));
-    L.row = take(P * 4);
+    L.row = take((P + 1) * 4);  // a product over no rows reads one entry past the last
     L.w = take(P * 4);
     L.pos = take(P * 4);
+    L.counts = take(som::pair_stretches(P) * E * 4);
     L.inner = take(P * F * 2);
     L.y = take(P * D * 4);
     L.pre = take(keep ? P * F * 2 : 0);
@@ -112,6 +113,7 @@ Experts carve(void *ws, const ExpertsLayout &L)
     x.plan.row = reinterpret_cast<int32_t *>(b + L.row);
     x.plan.w = reinterpret_cast<float *>(b + L.w);
     x.plan.pos = reinterpret_cast<int32_t *>(b + L.pos);
+    x.plan.counts = reinterpret_cast<int32_t *>(b + L.counts);
     x.inner = b + L.inner;
     x.y = reinterpret_cast<float *>(b + L.y);
     x.pre = b + L.pre;

@@ -9,52 +9,47 @@ namespace {
 using mm::load4;
 using mm::store4;
 
-// One workgroup orders all pairs: each wave counts its stretch of them by expert, a scan over
-// waves and experts gives every wave its first place in every expert, and each wave places its
-// pairs 64 at a time, a pair after those of the same expert in lower lanes. The order is the
-// pairs' own within an expert, so sums over it are the same on every run.
-template <typename T>
-__global__ __launch_bounds__(1024) void k_pairs(const int32_t *__restrict__ idx, const T *__restrict__ w, int P,
-                                                 int k, int E, int rows, const PairPlan plan)
+// The pairs are ordered by counting: stretches of them, a wave each, are counted by expert; a
+// scan over stretches and experts gives every stretch its first place in every expert; and each
+// wave places its pairs 64 at a time, a pair after those of the same expert in lower lanes. The
+// order is the pairs' own within an expert, so sums over it are the same on every run. Few pairs
+// take one workgroup for all three (16 stretches at most); more take a kernel each.
+
+// A stretch's pairs to count[e]; its indexes are loaded eight chunks at a time.
+template <typename F> __device__ inline void chunks_of(const int32_t *idx, int64_t first, int64_t last, int E, F f)
 {
-    extern __shared__ int lds[];
-    const int waves = blockDim.x / 64, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-    int *count = lds;                // [waves][E]
-    int *start = lds + waves * E;    // [E]
-    int *scan = start + E;           // [2][blockDim.x]
-    for (int i = threadIdx.x; i < waves * E; i += blockDim.x) count[i] = 0;
-    __syncthreads();
-    const int stretch = ((P + waves - 1) / waves + 63) / 64 * 64;
-    const int64_t first = (int64_t)wave * stretch, last = min((int64_t)P, first + stretch);
-    for (int64_t i = first + lane; i < last; i += 64) {
-        const int e = idx[i];
-        if (e >= 0 && e < E) atomicAdd(&count[wave * E + e], 1);
-    }
-    __syncthreads();
-    // E <= blockDim.x: a thread an expert
-    const int e = threadIdx.x;
-    int own = 0;
-    if (e < E)
-        for (int v = 0; v < waves; ++v) {
-            const int c = count[v * E + e];
-            count[v * E + e] = own;
-            own += c;
+    const int lane = threadIdx.x % 64;
+    for (int64_t i0 = first; i0 < last; i0 += 512) {
+        int x[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const int64_t i = i0 + c * 64 + lane;
+            x[c] = i < last ? idx[i] : -1;
         }
-    const int tiles = (own + rows - 1) / rows;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+            if (i0 + c * 64 < last) f(i0 + c * 64 + lane, (unsigned)x[c] < (unsigned)E ? x[c] : -1);
+    }
+}
+
+// own: the expert's pairs (0 beyond E), a thread an expert. Writes the experts' starts and tile
+// rows; scan: 2 * blockDim.x words of LDS. Returns the expert's start.
+__device__ inline int lay_out(int own, int E, int rows, int *scan, const PairPlan &plan)
+{
+    const int e = threadIdx.x, tiles = (own + rows - 1) / rows;
     int *a = scan, *b = scan + blockDim.x;
     a[e] = own;
     b[e] = tiles;
     __syncthreads();
-    for (int d = 1; d < (int)blockDim.x; d *= 2) {
+    for (int d = 1; d < (int)blockDim.x && d < E; d *= 2) {
         const int x = e >= d ? a[e - d] : 0, y = e >= d ? b[e - d] : 0;
         __syncthreads();
         a[e] += x;
         b[e] += y;
         __syncthreads();
     }
+    const int at = a[e] - own;
     if (e < E) {
-        const int at = a[e] - own;
-        start[e] = at;
         plan.off[e] = at;
         if (e == E - 1) {
             plan.off[E] = a[e];
@@ -62,31 +57,112 @@ __global__ __launch_bounds__(1024) void k_pairs(const int32_t *__restrict__ idx,
         }
         for (int t = 0; t < tiles; ++t) plan.tiles[b[e] - tiles + t] = TileRow{e, at + t * rows, at + own, 0};
     }
-    __syncthreads();
-    volatile int *mine = count + wave * E;  // read and then written by one wave, in order
-    for (int64_t i0 = first; i0 < last; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const int x = i < last ? idx[i] : -1;
-        const bool ok = x >= 0 && x < E;
+    return at;
+}
+
+// next[e]: the stretch's next place of expert e, in LDS, the wave's own.
+template <typename T>
+__device__ inline void place(const int32_t *idx, const T *w, int64_t first, int64_t last, int k, int E,
+                             volatile int *next, const PairPlan &plan)
+{
+    const int lane = threadIdx.x % 64;
+    chunks_of(idx, first, last, E, [&](int64_t i, int x) {
+        const bool ok = x >= 0;
         unsigned long long same = __ballot(ok);
-        for (int bit = 0; bit < 10; ++bit) {
+        for (int bit = 0; 1 << bit < E; ++bit) {
             const unsigned long long v = __ballot(x >> bit & 1);
             same &= (x >> bit & 1) ? v : ~v;
         }
         const int before = __popcll(same & ((1ull << lane) - 1));
-        const int base = ok ? mine[x] : 0;
+        const int base = ok ? next[x] : 0;
         __builtin_amdgcn_wave_barrier();
-        if (ok && before == 0) mine[x] = base + __popcll(same);
+        if (ok && before == 0) next[x] = base + __popcll(same);  // reads before writes: one wave, in order
         __builtin_amdgcn_wave_barrier();
         if (i < last) {
-            const int p = ok ? start[x] + base + before : -1;
+            const int p = ok ? base + before : -1;
             plan.pos[i] = p;
             if (ok) {
                 plan.row[p] = (int)(i / k);
                 plan.w[p] = (float)w[i];
             }
         }
+    });
+}
+
+__device__ inline int64_t stretch_of(int64_t P, int waves) { return ((P + waves - 1) / waves + 63) / 64 * 64; }
+
+template <typename T>
+__global__ __launch_bounds__(1024) void k_pairs(const int32_t *__restrict__ idx, const T *__restrict__ w, int64_t P,
+                                                int k, int E, int rows, const PairPlan plan)
+{
+    extern __shared__ int lds[];
+    const int waves = blockDim.x / 64, wave = threadIdx.x / 64;
+    int *count = lds, *scan = lds + waves * E;  // [waves][E], [2][blockDim.x]
+    for (int i = threadIdx.x; i < waves * E; i += blockDim.x) count[i] = 0;
+    __syncthreads();
+    const int64_t first = wave * stretch_of(P, waves), last = min(P, first + stretch_of(P, waves));
+    chunks_of(idx, first, last, E, [&](int64_t, int x) {
+        if (x >= 0) atomicAdd(&count[wave * E + x], 1);
+    });
+    __syncthreads();
+    int own = 0;
+    if ((int)threadIdx.x < E)
+        for (int v = 0; v < waves; ++v) own += count[v * E + threadIdx.x];
+    int at = lay_out(own, E, rows, scan, plan);
+    if ((int)threadIdx.x < E)
+        for (int v = 0; v < waves; ++v) {
+            const int c = count[v * E + threadIdx.x];
+            count[v * E + threadIdx.x] = at;
+            at += c;
+        }
+    __syncthreads();
+    place(idx, w, first, last, k, E, count + wave * E, plan);
+}
+
+// counts: [gridDim.x][E], one wave a workgroup.
+__global__ __launch_bounds__(64) void k_pairs_count(const int32_t *__restrict__ idx, int64_t P, int E, int32_t *counts)
+{
+    extern __shared__ int lds[];
+    for (int i = threadIdx.x; i < E; i += 64) lds[i] = 0;
+    __syncthreads();
+    const int64_t len = stretch_of(P, gridDim.x), first = blockIdx.x * len, last = min(P, first + len);
+    chunks_of(idx, first, last, E, [&](int64_t, int x) {
+        if (x >= 0) atomicAdd(&lds[x], 1);
+    });
+    __syncthreads();
+    for (int i = threadIdx.x; i < E; i += 64) counts[(int64_t)blockIdx.x * E + i] = lds[i];
+}
+
+// The counts become each stretch's first places.
+__global__ __launch_bounds__(1024) void k_pairs_scan(int32_t *counts, int stretches, int E, int rows, const PairPlan plan)
+{
+    __shared__ int scan[2 * 1024];
+    const int e = threadIdx.x;
+    int own = 0;
+    if (e < E) {
+#pragma unroll 8
+        for (int v = 0; v < stretches; ++v) own += counts[v * E + e];
     }
+    int at = lay_out(own, E, rows, scan, plan);
+    if (e < E) {
+#pragma unroll 8
+        for (int v = 0; v < stretches; ++v) {
+            const int c = counts[v * E + e];
+            counts[v * E + e] = at;
+            at += c;
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(64) void k_pairs_place(const int32_t *__restrict__ idx, const T *__restrict__ w, int64_t P,
+                                                    int k, int E, const int32_t *__restrict__ counts, const PairPlan plan)
+{
+    extern __shared__ int lds[];
+    for (int i = threadIdx.x; i < E; i += 64) lds[i] = counts[(int64_t)blockIdx.x * E + i];
+    __syncthreads();
+    const int64_t len = stretch_of(P, gridDim.x), first = blockIdx.x * len, last = min(P, first + len);
+    place(idx, w, first, last, k, E, lds, plan);
 }
 
 template <typename T>
@@ -172,22 +248,29 @@ unsigned spread(int64_t items) { return (unsigned)(items < 1 ? 1 : items > 65536
 hipError_t launch_pairs(bool bf16, const int32_t *idx, const void *w, int64_t P, int32_t k, int32_t E, int rows,
                         const PairPlan &plan, hipStream_t st)
 {
-    int waves = P <= 512 && E <= 256 ? 4 : E <= 512 ? 8 : 16;  // a thread an expert at least
-    if (P > 4096 && E <= 512) waves = 16;
-    const size_t lds = ((size_t)waves * E + E + 2 * 64 * waves) * sizeof(int);  // at most 77 KB
-    if (lds > 64 << 10) {
-        const hipError_t e = hipFuncSetAttribute(
-            bf16 ? reinterpret_cast<const void *>(&k_pairs<__bf16>) : reinterpret_cast<const void *>(&k_pairs<_Float16>),
-            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    auto with = [&](auto one, auto many, auto *weights) {
+        if (P <= kPairsOfOne) {
+            const int waves = E <= 256 ? (P <= 512 ? 4 : 16) : E <= 512 ? 8 : 16;  // a thread an expert at least
+            const size_t lds = ((size_t)waves * E + 2 * 64 * waves) * sizeof(int);  // at most 72 KB
+            if (lds > 64 << 10) {
+                const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(one),
+                                                         hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+                if (e != hipSuccess) return e;
+            }
+            hipLaunchKernelGGL(one, dim3(1), dim3(64 * waves), lds, st, idx, weights, P, k, E, rows, plan);
+            return hipGetLastError();
+        }
+        const int n = pair_stretches(P);
+        hipLaunchKernelGGL(k_pairs_count, dim3(n), dim3(64), E * sizeof(int), st, idx, P, E, plan.counts);
+        hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-    }
-    if (bf16)
-        hipLaunchKernelGGL(k_pairs<__bf16>, dim3(1), dim3(64 * waves), lds, st, idx, static_cast<const __bf16 *>(w),
-                           (int)P, k, E, rows, plan);
-    else
-        hipLaunchKernelGGL(k_pairs<_Float16>, dim3(1), dim3(64 * waves), lds, st, idx,
-                           static_cast<const _Float16 *>(w), (int)P, k, E, rows, plan);
-    return hipGetLastError();
+        hipLaunchKernelGGL(k_pairs_scan, dim3(1), dim3(E <= 256 ? 256 : 1024), 0, st, plan.counts, n, E, rows, plan);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        hipLaunchKernelGGL(many, dim3(n), dim3(64), E * sizeof(int), st, idx, weights, P, k, E, plan.counts, plan);
+        return hipGetLastError();
+    };
+    return bf16 ? with(&k_pairs<__bf16>, &k_pairs_place<__bf16>, static_cast<const __bf16 *>(w))
+                : with(&k_pairs<_Float16>, &k_pairs_place<_Float16>, static_cast<const _Float16 *>(w));
 }
 
 hipError_t launch_combine(bool bf16, const float *y, const int32_t *pos, int64_t N, int32_t k, int64_t D,

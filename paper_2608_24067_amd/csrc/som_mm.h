@@ -47,32 +47,57 @@ template <typename T> struct Vec8;
 template <> struct Vec8<_Float16> { typedef f16x8 type; };
 template <> struct Vec8<__bf16> { typedef bf16x8 type; };
 
-// Activations and their derivatives at z, in fp32.
-__device__ inline float act_value(int act, float z)
+// exp(x): 2^t on the hardware with what t = x log2(e) lost in rounding put back, within 3 units in
+// the last place; 0 below about -87, also at minus infinity.
+__device__ inline float exp_f32(float x)
 {
-    if (act == SOM_ACT_RELU) return z <= 0.0f ? 0.0f : z;  // NaN stays NaN
-    if (act == SOM_ACT_SILU) return z / (1.0f + expf(-z));
-    if (act == SOM_ACT_GELU) return z * (0.5f + 0.5f * erff(z * 0.70710678f));
-    return z;
+    x = fmaxf(x, -200.0f);
+    const float t = x * 1.44269504f;
+    const float lost = fmaf(x, 1.44269504f, -t) + x * 1.925963e-8f;
+    return __builtin_amdgcn_exp2f(t) * fmaf(lost, 0.693147181f, 1.0f);
 }
 
+// The normal distribution Phi(z) and exp(-z^2 / 2), by formula 7.1.26 of Abramowitz and Stegun's
+// Handbook of Mathematical Functions for the error function: within 1.5e-7, which 16-bit results
+// do not see, for a third of erff's instructions.
+__device__ inline float normal_f32(float z, float &bell)
+{
+    const float x = fabsf(z) * 0.707106781f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    bell = exp_f32(-0.5f * z * z);
+    float q = fmaf(1.061405429f, t, -1.453152027f);
+    q = fmaf(q, t, 1.421413741f);
+    q = fmaf(q, t, -0.284496736f);
+    q = fmaf(q, t, 0.254829592f);
+    const float tail = 0.5f * q * t * bell;  // of Phi beyond |z|
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+
+// Activations and their derivatives at z, in fp32.
 __device__ inline void act_both(int act, float z, float &value, float &slope)
 {
-    if (act == SOM_ACT_RELU) {
-        value = act_value(act, z);
+    value = z;
+    slope = 1.0f;
+    if (act == SOM_ACT_RELU) {  // NaN stays NaN
+        value = z <= 0.0f ? 0.0f : z;
         slope = z <= 0.0f ? 0.0f : z > 0.0f ? 1.0f : z;
     } else if (act == SOM_ACT_SILU) {
-        const float q = 1.0f / (1.0f + expf(-z));
+        const float q = __builtin_amdgcn_rcpf(1.0f + exp_f32(fminf(-z, 88.0f)));
         value = z * q;
-        slope = q * (1.0f + z * (1.0f - q));
+        slope = q * fmaf(z, 1.0f - q, 1.0f);
     } else if (act == SOM_ACT_GELU) {
-        const float q = 0.5f + 0.5f * erff(z * 0.70710678f);
+        float bell;
+        const float q = normal_f32(z, bell);
         value = z * q;
-        slope = q + z * (0.39894228f * expf(-0.5f * z * z));
-    } else {
-        value = z;
-        slope = 1.0f;
+        slope = fmaf(0.39894228f * z, bell, q);
     }
+}
+
+__device__ inline float act_value(int act, float z)
+{
+    float value, slope;
+    act_both(act, z, value, slope);
+    return value;
 }
 
 // n (1 to 4) consecutive values at p, whose alignment is that of one element.
@@ -116,7 +141,7 @@ template <int BR> __device__ inline int unit_xor(int k)
 // One operand's tile of kBK steps by BR rows (along) or columns (across), loaded by NT threads,
 // tile after tile. A chunk past the last row (column) is read from inside the operand instead:
 // it only reaches results that are not written. A chunk past the last step must be zero.
-template <typename T, int BR, bool ACROSS, int NT> struct Loader {
+template <typename T, int BR, bool ACROSS, bool MAPPED, int NT> struct Loader {
     static constexpr int kChunks = BR * kBK / 8;
     static constexpr int kPer = (kChunks + NT - 1) / NT;
     static constexpr int kRowChunks = ACROSS ? BR / 8 : kBK / 8;
@@ -127,8 +152,8 @@ template <typename T, int BR, bool ACROSS, int NT> struct Loader {
     const T *ptr[kPer];  // the chunk in the next tile (across with a map: its column in row 0)
     int k[kPer];         // its step in the tile
     int cnt[kPer];       // elements inside the operand, of loads through registers
-    Scalar map;          // across: the rows' map, from the first row of the reduction
-    int next[kPer][ACROSS ? kWaveRows : 1];  // and what it says for the wave's rows of the next tile
+    Scalar map;          // MAPPED (across): the rows' map, from the first row of the reduction
+    int next[kPer][MAPPED ? kWaveRows : 1];  // and what it says for the wave's rows of the next tile
     int64_t ld;
     int K, t;            // reduction length; the next tile's first step
 
@@ -139,7 +164,7 @@ template <typename T, int BR, bool ACROSS, int NT> struct Loader {
         ld = ld_;
         K = K_;
         t = 0;
-        map = ACROSS && rows ? (Scalar)(rows + k0) : nullptr;
+        if (MAPPED) map = (Scalar)(rows + k0);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int c = i * NT + (int)threadIdx.x;
@@ -149,7 +174,7 @@ template <typename T, int BR, bool ACROSS, int NT> struct Loader {
                 k[i] = row;
                 cnt[i] = min(8, r1 - col);
                 if (CHUNKS) col = min(col, r1 - 8);
-                ptr[i] = p + col + (map ? 0 : (k0 + row) * ld);
+                ptr[i] = p + col + (MAPPED ? 0 : (k0 + row) * ld);
             } else {
                 const int src = s ^ ((row >> 2) & 3);
                 const int r = min(r0 + row, r1 - 1);
@@ -165,13 +190,13 @@ template <typename T, int BR, bool ACROSS, int NT> struct Loader {
     // vector loads in flight.
     __device__ void look_up()
     {
-        if (!ACROSS || !map) return;
+        if (!MAPPED) return;
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
 #pragma unroll
             for (int q = 0; q < kWaveRows; ++q)
-                next[i][q] = t < K ? map[min(t + (i * NT + wave * 64) / kRowChunks + q, K - 1)] : 0;
+                next[i][q] = map[max(min(t + (i * NT + wave * 64) / kRowChunks + q, K - 1), 0)];
     }
 
     __device__ static bool mine(int i) { return kChunks % NT == 0 || i * NT + (int)threadIdx.x < kChunks; }
@@ -179,41 +204,38 @@ template <typename T, int BR, bool ACROSS, int NT> struct Loader {
     // The chunk's address in the next tile.
     __device__ const T *source(int i) const
     {
-        if (!ACROSS || !map) return ptr[i];
-        int row = next[i][0];
+        if (!MAPPED) return ptr[i];
+        int row = 0;
 #pragma unroll
-        for (int q = 1; q < kWaveRows; ++q)
-            row = ((int)threadIdx.x & 63) / kRowChunks == q ? next[i][q] : row;
+        for (int q = 0; q < kWaveRows; ++q)
+            row |= next[i][q] & -(int)(((int)threadIdx.x & 63) / kRowChunks == q);
         return ptr[i] + (int64_t)row * ld;
     }
 
     __device__ void advance()
     {
         t += kBK;
-        if (!ACROSS || !map) {
+        if (!MAPPED) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) ptr[i] += ACROSS ? kBK * ld : (int64_t)kBK;
         }
         look_up();
     }
 
-    // The next tile, straight to LDS. The instruction is written out because the compiler waits
-    // for every such load of its own before any read of LDS; the kernel's loop waits as it needs.
-    // A wave's 64 chunks go to consecutive 16-byte places from m0 on.
-    __device__ void async(uint32_t lds)
+    // Chunk i of the next tile, straight to LDS; INSIDE: the tile ends within the operand. The
+    // instruction is written out because the compiler waits for every such load of its own before
+    // any read of LDS; the kernel's loop waits as it needs. A wave's 64 chunks go to consecutive
+    // 16-byte places from m0 on.
+    template <bool INSIDE> __device__ void async(int i, uint32_t lds) const
     {
+        if (!mine(i)) return;
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if (!mine(i)) continue;
-            const void *from = source(i);
-            if (t + kBK > K && t + k[i] >= K) from = g_zero;
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                         :
-                         : "s"(lds + (uint32_t)(i * NT + wave * 64) * 16), "v"(from)
-                         : "memory");
-        }
-        advance();
+        const void *from = source(i);
+        if (!INSIDE) from = t + k[i] < K ? from : g_zero;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                     :
+                     : "s"(lds + (uint32_t)(i * NT + wave * 64) * 16), "v"(from)
+                     : "memory");
     }
 
     // The next tile, into registers.
@@ -245,38 +267,34 @@ template <typename T, int BR, bool ACROSS, int NT> struct Loader {
     }
 };
 
-// A lane's fragment of 16 rows (columns) from `at`, a multiple of 16, of a tile in LDS.
+// A lane's fragments of 16 rows (columns) each, from row (column) `at` of a tile in LDS. `at` is a
+// multiple of the wave's rows, so the unit of fragment j is an exclusive or away from the first's.
 template <typename T, int BR, bool ACROSS> struct Reader {
-    int base, f;
+    uint32_t base;
 
     __device__ void init(int at)
     {
         const int lane = (int)threadIdx.x & 63, g = lane >> 4, i = lane & 15;
         if (ACROSS) {
             const int row = 8 * g + (i >> 2);
-            f = unit_xor<BR>(row);
-            base = row * (BR * 2) + (i & 3) * 8;
-            unit = at >> 4;
+            base = row * (BR * 2) + ((((uint32_t)at >> 4) ^ unit_xor<BR>(row)) << 5) + (i & 3) * 8;
         } else {
-            f = 0;
-            unit = 0;
             base = (at + i) * (kBK * 2) + ((g ^ (i >> 2)) << 4);
         }
     }
 
-    int unit;
-
-    __device__ typename Vec8<T>::type read(const char *lds, int j) const
+    // lds: the tile's address in LDS, a multiple of 1,024.
+    __device__ typename Vec8<T>::type read(uint32_t lds, int j) const
     {
         s16x8 r;
         if (ACROSS) {
-            const char *p = lds + base + (((unit + j) ^ f) << 5);
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) s16x4 *)(p + 4 * BR * 2));
+            const uint32_t p = (lds + base) ^ (uint32_t)(j << 5);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)p);
+            const s16x4 hi =
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)(p + 4 * BR * 2));
             r = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         } else {
-            r = *reinterpret_cast<const s16x8 *>(lds + base + j * (16 * kBK * 2));
+            r = *(const __attribute__((address_space(3))) s16x8 *)(uintptr_t)(lds + base + (uint32_t)j * (16 * kBK * 2));
         }
         return __builtin_bit_cast(typename Vec8<T>::type, r);
     }
@@ -287,6 +305,14 @@ template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int PER_CU_> struct S
     static constexpr int NT = 64 * WM * WN;
     static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
 };
+
+// A wave's LDS accesses before this are done before those after it (LDS serves a wave in order;
+// the wait is for the values, the clobber for the compiler). Nothing else is waited for.
+__device__ inline void wave_sync_lds()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
 
 // Workgroup b of `total` tiles: consecutive tiles go to one XCD (workgroups are dealt to the
 // eight XCDs in turn), so that its L2 serves the operands they share. The grid is a multiple
@@ -310,12 +336,19 @@ __device__ inline void tile_place(int64_t t, int nm, int nn, int &m, int &n)
 
 enum Layout { kNN, kNT, kTN };
 
-template <typename T, Layout L, Epilogue EPI, class S, bool ASYNC>
+template <bool V> struct Inside {
+    static constexpr bool value = V;
+};
+
+// Which operand of a product over rows (TN) goes through a map of its rows.
+enum Mapped { kNoMap, kMapA, kMapB };
+
+template <typename T, Layout L, Epilogue EPI, class S, bool ASYNC, Mapped MAP>
 __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(const Product p)
 {
     constexpr bool A_ACROSS = L == kTN, B_ACROSS = L != kNT;
-    typedef Loader<T, S::BM, A_ACROSS, S::NT> LoadA;
-    typedef Loader<T, S::BN, B_ACROSS, S::NT> LoadB;
+    typedef Loader<T, S::BM, A_ACROSS, MAP == kMapA, S::NT> LoadA;
+    typedef Loader<T, S::BN, B_ACROSS, MAP == kMapB, S::NT> LoadB;
     constexpr int kStage = LoadA::kBytes + LoadB::kBytes;
     constexpr int kStages = ASYNC ? S::STAGES : 2;
     extern __shared__ __align__(1024) char lds[];
@@ -374,155 +407,273 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
 #pragma unroll
         for (int j = 0; j < S::NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
-    // The column sums of B: one more block of rows for the waves of the first tile row, each
-    // row the weights (or ones).
-    const bool sums = L == kTN && p.db && mt == 0 && wm == 0;
-    f32x4 col[S::NI];
+    // The column sums of B: one more block of rows for the tiles of the first tile row, each row
+    // the weights (or ones); the WM waves that read the same columns share them out.
+    const bool sums = L == kTN && p.db && mt == 0;
+    constexpr int kSums = S::NI / S::WM;
+    f32x4 col[kSums];
 #pragma unroll
-    for (int j = 0; j < S::NI; ++j) col[j] = f32x4{0, 0, 0, 0};
+    for (int j = 0; j < kSums; ++j) col[j] = f32x4{0, 0, 0, 0};
 
     const int steps = (K + kBK - 1) / kBK;
-    auto compute = [&](int t) {
-        const char *at = lds + (t % kStages) * kStage;
-        typename Vec8<T>::type b[S::NI];
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    typedef typename Vec8<T>::type Frag;
+    struct FragsB {
+        Frag f[S::NI];
+    };
+    auto multiply_row = [&](int i, const Frag &a, const FragsB &b) {
 #pragma unroll
-        for (int j = 0; j < S::NI; ++j) b[j] = rb.read(at + LoadA::kBytes, j);
+        for (int j = 0; j < S::NI; ++j) acc[i][j] = mma(b.f[j], a, acc[i][j]);
+    };
+    auto add_sums = [&](int t, const FragsB &b) {
+        Frag ones;
+        const int k = t * kBK + 8 * (((int)threadIdx.x & 63) >> 4);
 #pragma unroll
-        for (int i = 0; i < S::MI; ++i) {
-            const typename Vec8<T>::type a = ra.read(at, i);
+        for (int q = 0; q < 8; ++q) ones[q] = (T)(k + q < K ? (p.w ? p.w[k0 + k + q] : 1.0f) : 0.0f);
 #pragma unroll
-            for (int j = 0; j < S::NI; ++j) acc[i][j] = mma(b[j], a, acc[i][j]);
-        }
-        if (L == kTN && sums) {
-            typename Vec8<T>::type ones;
-            const int k = t * kBK + 8 * (((int)threadIdx.x & 63) >> 4);
+        for (int w = 0; w < S::WM; ++w) {
+            if (w != wm) continue;
 #pragma unroll
-            for (int q = 0; q < 8; ++q) ones[q] = (T)(k + q < K ? (p.w ? p.w[k0 + k + q] : 1.0f) : 0.0f);
-#pragma unroll
-            for (int j = 0; j < S::NI; ++j) col[j] = mma(b[j], ones, col[j]);
+            for (int j = 0; j < kSums; ++j) col[j] = mma(b.f[w * kSums + j], ones, col[j]);
         }
     };
 
     if (ASYNC) {
-        // kStages - 1 tiles in flight. A wave waits for its own loads of the tile it needs,
-        // the barrier makes that every wave's; it also says that the tile computed before is
-        // no longer read, whose place the next loads take. Past the last tile the loads bring
-        // zeros, so that the number in flight is the same in every step.
-        // (a wave that has fewer chunks than others counts on its own: kLoads is the least).
+        // Step t multiplies tile t, MI rows of NI blocks. Its fragments of B and its first kWindow of
+        // A are in registers when it starts; the others of A are read kWindow rows ahead, from the
+        // last rows on those of tile t + 1, whose fragments of B are read as well; the loads of
+        // tiles up to t + kStages - 1 are in flight. A wave waits for its own loads of tile t + 1 and
+        // for its own reads of tile t - 1, the barrier makes that every wave's: tile t + 1 may be
+        // read, and the place of tile t - 1 be loaded anew. Past the last tile the loads bring
+        // zeros, so that the number in flight is the same in every step (a wave that has fewer
+        // chunks than others counts on its own: kLoads is the least).
         constexpr int kLoads = LoadA::kChunks / S::NT + LoadB::kChunks / S::NT;
         static_assert(LoadA::kChunks % 64 == 0 && LoadB::kChunks % 64 == 0, "whole waves load");
-        const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 #pragma unroll
-        for (int s = 0; s < kStages - 1; ++s) {
-            la.async(base + s * kStage);
-            lb.async(base + s * kStage + LoadA::kBytes);
+        for (int t = 0; t < kStages - 1; ++t) {
+#pragma unroll
+            for (int i = 0; i < LoadA::kPer; ++i) la.template async<false>(i, base + t * kStage);
+#pragma unroll
+            for (int i = 0; i < LoadB::kPer; ++i) lb.template async<false>(i, base + t * kStage + LoadA::kBytes);
+            la.advance();
+            lb.advance();
         }
-        for (int t = 0; t < steps; ++t) {
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
-            const uint32_t next = base + (uint32_t)((t + kStages - 1) % kStages) * kStage;
-            la.async(next);
-            lb.async(next + LoadA::kBytes);
-            compute(t);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
+        constexpr int kWindow = S::MI < 4 ? S::MI : 4;
+        FragsB even, odd;
+        Frag a[kWindow];
+#pragma unroll
+        for (int j = 0; j < S::NI; ++j) even.f[j] = rb.read(base + LoadA::kBytes, j);
+#pragma unroll
+        for (int i = 0; i < kWindow; ++i) a[i] = ra.read(base, i);
+        auto step = [&](int t, const FragsB &now, FragsB &then, auto inside) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 3) * kLoads) : "memory");
+            const uint32_t here = base + (uint32_t)(t % kStages) * kStage;
+            const uint32_t next = base + (uint32_t)((t + 1) % kStages) * kStage;
+            const uint32_t to = base + (uint32_t)((t + kStages - 1) % kStages) * kStage;
+            constexpr int kB = (2 * S::NI + S::MI - 1) / S::MI;  // fragments of B a row: done in the first half
+            constexpr int kAll = LoadA::kPer + LoadB::kPer, kOf = (kAll + S::MI - 1) / S::MI;
+#pragma unroll
+            for (int i = 0; i < S::MI; ++i) {
+                multiply_row(i, a[i % kWindow], now);
+                a[i % kWindow] = i + kWindow < S::MI ? ra.read(here, i + kWindow) : ra.read(next, i + kWindow - S::MI);
+#pragma unroll
+                for (int j = i * kB; j < (i + 1) * kB && j < S::NI; ++j)
+                    then.f[j] = rb.read(next + LoadA::kBytes, j);
+#pragma unroll
+                for (int c = i * kOf; c < (i + 1) * kOf; ++c) {
+                    if (c < LoadA::kPer) la.template async<decltype(inside)::value>(c, to);
+                    else if (c < kAll) lb.template async<decltype(inside)::value>(c - LoadA::kPer, to + LoadA::kBytes);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            la.advance();
+            lb.advance();
+            if (L == kTN && sums) add_sums(t, now);
+        };
+        int t = 0;
+        for (; (t + kStages + 1) * kBK <= K; t += 2) {
+            step(t, even, odd, Inside<true>());
+            step(t + 1, odd, even, Inside<true>());
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing lands in LDS after the workgroup has left it
+        for (; t < steps; t += 2) {
+            step(t, even, odd, Inside<false>());
+            if (t + 1 < steps) step(t + 1, odd, even, Inside<false>());
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // nothing lands in LDS after the workgroup left it
     } else {
-        s16x8 va[LoadA::kPer], vb[LoadB::kPer];
-        if (steps > 0) {
-            la.fetch(va);
-            lb.fetch(vb);
-            LoadA::put(lds, va);
-            LoadB::put(lds + LoadA::kBytes, vb);
-            __syncthreads();
+        // Tiles go through registers, kAhead of them in flight, into two places of LDS.
+        constexpr int kAhead = 3;
+        s16x8 va[kAhead][LoadA::kPer], vb[kAhead][LoadB::kPer];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            la.fetch(va[i]);
+            lb.fetch(vb[i]);
         }
-        for (int t = 0; t < steps; ++t) {
-            if (t + 1 < steps) {
-                la.fetch(va);
-                lb.fetch(vb);
+        for (int t0 = 0; t0 < steps; t0 += kAhead) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int t = t0 + i;
+                if (t >= steps) break;
+                char *at = lds + (t % 2) * kStage;
+                LoadA::put(at, va[i]);
+                LoadB::put(at + LoadA::kBytes, vb[i]);
+                __syncthreads();
+                la.fetch(va[i]);
+                lb.fetch(vb[i]);
+                FragsB b;
+                const uint32_t from = base + (uint32_t)(t % 2) * kStage;
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) b.f[j] = rb.read(from + LoadA::kBytes, j);
+#pragma unroll
+                for (int m = 0; m < S::MI; ++m) multiply_row(m, ra.read(from, m), b);
+                if (L == kTN && sums) add_sums(t, b);
             }
-            compute(t);
-            if (t + 1 < steps) {
-                char *next = lds + ((t + 1) % 2) * kStage;
-                LoadA::put(next, va);
-                LoadB::put(next + LoadA::kBytes, vb);
-            }
-            __syncthreads();
         }
     }
 
-    // Epilogue: lane (g, i) of the wave has the row i and the columns 4g ... 4g + 3 of each block.
+    // Epilogue. Lane (g, i) of a wave has row i and columns 4g ... 4g + 3 of each 16 x 16 block; 16
+    // rows at a time go through LDS, so that a row's columns are read and written side by side.
+    // (Rows there are 16 bytes longer than the columns: the 64 writes of 16 bytes meet every
+    // bank equally often.)
+    constexpr int kCols = S::NI * 16, kRow = kCols + 4, kLanes = kCols / 4, kAtOnce = 64 / kLanes;
     const int lane = (int)threadIdx.x & 63, g = lane >> 4, li = lane & 15;
-    const int row0 = m0 + wm * S::MI * 16 + li, col0 = n0 + wn * S::NI * 16 + 4 * g;
+    const int row0 = m0 + wm * S::MI * 16, col0 = n0 + wn * kCols;
     const int64_t ob = L == kTN ? (int64_t)e * p.strideC : 0;
+    const int sub = lane / kLanes, n = col0 + lane % kLanes * 4, cnt = min(4, (int)p.N - n);
+    float *own = reinterpret_cast<float *>(lds) + wave * (16 * kRow);
+    float bias[4] = {0, 0, 0, 0};
+    if ((EPI == kLinear || EPI == kInner || EPI == kPairs) && p.bias && cnt > 0) {
+        if (p.bias_f32) load4(static_cast<const float *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
+        else load4(static_cast<const T *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
+    }
+    __syncthreads();  // the tiles are no longer read
+    constexpr int kTurns = 16 / kAtOnce;
+    // 16 rows: a lane's four columns of every kAtOnce-th row. Each stage runs over all of them, so
+    // that its loads are in flight together and its branches are taken once.
+    auto rows16 = [&](int i, auto whole) {
+        constexpr bool W = decltype(whole)::value;
+        const int c4 = W ? 4 : cnt;
+        float v[kTurns][4], wr[kTurns];
+        int m[kTurns];
+        bool in[kTurns];
 #pragma unroll
-    for (int i = 0; i < S::MI; ++i) {
-        const int m = row0 + 16 * i;
-        const bool row_in = m < m1 && (L != kTN || p.out);
-        float wr = 1.0f, part = 0.0f;
-        if (L != kTN && p.w && row_in) wr = p.w[m];
+        for (int r = 0; r < kTurns; ++r) {
+            const f32x4 c = *reinterpret_cast<const f32x4 *>(own + (r * kAtOnce + sub) * kRow + lane % kLanes * 4);
+            m[r] = row0 + 16 * i + r * kAtOnce + sub;
+            in[r] = W || (m[r] < m1 && cnt > 0);
+            wr[r] = (EPI == kInner || EPI == kPairs || EPI == kSlope) && p.w && in[r] ? p.w[m[r]] : 1.0f;
 #pragma unroll
-        for (int j = 0; j < S::NI; ++j) {
-            const int n = col0 + 16 * j, cnt = min(4, (int)p.N - n);
-            if (!row_in || cnt <= 0) continue;
-            float v[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = acc[i][j][q];
-            if (EPI == kLinear || EPI == kInner || EPI == kPairs) {
-                if (p.bias) {
-                    float b[4];
-                    if (p.bias_f32) load4(static_cast<const float *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, b);
-                    else load4(static_cast<const T *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, b);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) v[q] += EPI == kPairs ? wr * b[q] : b[q];
-                }
+            for (int q = 0; q < 4; ++q) {
+                v[r][q] = c[q];
+                if (EPI == kLinear || EPI == kInner) v[r][q] += bias[q];
+                if (EPI == kPairs) v[r][q] = fmaf(wr[r], bias[q], v[r][q]);
             }
-            if (EPI == kLinear || EPI == kInner) {
-                if (p.pre) store4(static_cast<T *>(p.pre) + (int64_t)m * p.ldp + n, cnt, v);
+        }
+        if (EPI == kLinear || EPI == kInner) {
+            if (p.pre) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] = act_value(p.act, v[q]);
+                for (int r = 0; r < kTurns; ++r)
+                    if (in[r]) store4(static_cast<T *>(p.pre) + (int64_t)m[r] * p.ldp + n, c4, v[r]);
             }
-            if (EPI == kInner) {
+            if (p.act == SOM_ACT_GELU) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] *= wr;
-            }
-            if (EPI == kLinear && p.res) {
-                float r[4];
-                load4(static_cast<const T *>(p.res) + (int64_t)m * p.ldr + n, cnt, r);
+                for (int r = 0; r < kTurns; ++r)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] += r[q];
-            }
-            if (EPI == kSlope) {
-                float z[4];
-                load4(static_cast<const T *>(p.pre) + (int64_t)m * p.ldp + n, cnt, z);
+                    for (int q = 0; q < 4; ++q) v[r][q] = act_value(SOM_ACT_GELU, v[r][q]);
+            } else if (p.act == SOM_ACT_SILU) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float value, slope;
-                    act_both(p.act, z[q], value, slope);
-                    part += q < cnt ? value * v[q] : 0.0f;
-                    v[q] *= wr * slope;
-                }
+                for (int r = 0; r < kTurns; ++r)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[r][q] = act_value(SOM_ACT_SILU, v[r][q]);
+            } else if (p.act == SOM_ACT_RELU) {
+#pragma unroll
+                for (int r = 0; r < kTurns; ++r)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[r][q] = act_value(SOM_ACT_RELU, v[r][q]);
             }
-            if (EPI == kPairs || (EPI == kLinear && p.out_f32))
-                store4(static_cast<float *>(p.out) + ob + (int64_t)m * p.ldo + n, cnt, v);
-            else
-                store4(static_cast<T *>(p.out) + ob + (int64_t)m * p.ldo + n, cnt, v);
+        }
+        if (EPI == kInner) {
+#pragma unroll
+            for (int r = 0; r < kTurns; ++r)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[r][q] *= wr[r];
+        }
+        if (EPI == kLinear && p.res) {
+            float t[kTurns][4];
+#pragma unroll
+            for (int r = 0; r < kTurns; ++r)
+                if (in[r]) load4(static_cast<const T *>(p.res) + (int64_t)m[r] * p.ldr + n, c4, t[r]);
+#pragma unroll
+            for (int r = 0; r < kTurns; ++r)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[r][q] += t[r][q];
         }
         if (EPI == kSlope) {
-            part += __shfl_xor(part, 16);
-            part += __shfl_xor(part, 32);
-            if (row_in && g == 0 && col0 < p.N)
-                p.parts[(int64_t)m * p.n_parts + (n0 / (16 * S::NI) + wn)] = part;
+            float z[kTurns][4];
+#pragma unroll
+            for (int r = 0; r < kTurns; ++r)
+                if (in[r]) load4(static_cast<const T *>(p.pre) + (int64_t)m[r] * p.ldp + n, c4, z[r]);
+            float part[kTurns];
+            auto slopes = [&](int act) {
+#pragma unroll
+                for (int r = 0; r < kTurns; ++r) {
+                    part[r] = 0.0f;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float value, slope;
+                        act_both(act, z[r][q], value, slope);
+                        part[r] += in[r] && q < c4 ? value * v[r][q] : 0.0f;
+                        v[r][q] *= wr[r] * slope;
+                    }
+                }
+            };
+            if (p.act == SOM_ACT_GELU) slopes(SOM_ACT_GELU);
+            else if (p.act == SOM_ACT_SILU) slopes(SOM_ACT_SILU);
+            else if (p.act == SOM_ACT_RELU) slopes(SOM_ACT_RELU);
+            else slopes(SOM_ACT_NONE);
+#pragma unroll
+            for (int d = 1; d < kLanes; d *= 2)
+#pragma unroll
+                for (int r = 0; r < kTurns; ++r) part[r] += __shfl_xor(part[r], d);
+#pragma unroll
+            for (int r = 0; r < kTurns; ++r)
+                if (in[r] && lane % kLanes == 0) p.parts[(int64_t)m[r] * p.n_parts + col0 / kCols] = part[r];
         }
+        if (EPI == kPairs || (EPI == kLinear && p.out_f32)) {
+#pragma unroll
+            for (int r = 0; r < kTurns; ++r)
+                if (in[r]) store4(static_cast<float *>(p.out) + ob + (int64_t)m[r] * p.ldo + n, c4, v[r]);
+        } else {
+#pragma unroll
+            for (int r = 0; r < kTurns; ++r)
+                if (in[r]) store4(static_cast<T *>(p.out) + ob + (int64_t)m[r] * p.ldo + n, c4, v[r]);
+        }
+    };
+#pragma unroll 1
+    for (int i = 0; i < S::MI; ++i) {  // rolled: the code of sixteen rows stands here once
+        if (L == kTN && !p.out) break;
+#pragma unroll
+        for (int at = 0; at < S::MI; ++at) {
+            if (at != i) continue;
+#pragma unroll
+            for (int j = 0; j < S::NI; ++j) *reinterpret_cast<f32x4 *>(own + li * kRow + j * 16 + 4 * g) = acc[at][j];
+        }
+        wave_sync_lds();
+        if (row0 + 16 * i + 16 <= m1 && col0 + kCols <= (int)p.N) rows16(i, Inside<true>());
+        else rows16(i, Inside<false>());
+        wave_sync_lds();
     }
     if (L == kTN && sums && li == 0) {
 #pragma unroll
-        for (int j = 0; j < S::NI; ++j) {
-            const int n = col0 + 16 * j, cnt = min(4, (int)p.N - n);
-            if (cnt <= 0) continue;
+        for (int j = 0; j < kSums; ++j) {
+            const int c = col0 + 16 * (wm * kSums + j) + 4 * g, left = min(4, (int)p.N - c);
+            if (left <= 0) continue;
             float v[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] = col[j][q];
-            if (p.bias_f32) store4(static_cast<float *>(p.db) + (int64_t)e * p.strideDb + n, cnt, v);
-            else store4(static_cast<T *>(p.db) + (int64_t)e * p.strideDb + n, cnt, v);
+            if (p.bias_f32) store4(static_cast<float *>(p.db) + (int64_t)e * p.strideDb + c, left, v);
+            else store4(static_cast<T *>(p.db) + (int64_t)e * p.strideDb + c, left, v);
         }
     }
 }
@@ -539,22 +690,23 @@ inline bool chunked(Layout l, const Product &p)
     return l != kTN || p.M % 8 == 0;
 }
 
-template <typename T, Layout L, Epilogue EPI, class S, bool ASYNC>
+template <typename T, Layout L, Epilogue EPI, class S, bool ASYNC, Mapped MAP = kNoMap>
 hipError_t launch(const Product &p, int64_t tile_rows_total, hipStream_t st)
 {
     constexpr int kStage = (S::BM + S::BN) * kBK * 2;
-    constexpr int bytes = kStage * (ASYNC ? S::STAGES : 2);
+    constexpr int tiles = kStage * (ASYNC ? S::STAGES : 2), rows = S::WM * S::WN * 16 * (S::NI * 16 + 4) * 4;
+    constexpr int bytes = tiles > rows ? tiles : rows;
     const int64_t nn = (p.N + S::BN - 1) / S::BN;
     const int64_t total = tile_rows_total * nn;
     if (total <= 0) return hipSuccess;
     const int64_t grid = (total + 7) / 8 * 8;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
     if (bytes > 64 << 10) {
-        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_product<T, L, EPI, S, ASYNC>),
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_product<T, L, EPI, S, ASYNC, MAP>),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (err != hipSuccess) return err;
     }
-    hipLaunchKernelGGL((k_product<T, L, EPI, S, ASYNC>), dim3((unsigned)grid), dim3(S::NT), bytes, st, p);
+    hipLaunchKernelGGL((k_product<T, L, EPI, S, ASYNC, MAP>), dim3((unsigned)grid), dim3(S::NT), bytes, st, p);
     return hipGetLastError();
 }
 

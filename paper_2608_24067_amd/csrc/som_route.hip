@@ -2,14 +2,16 @@
 //
 // A row is held in the registers of 16 or 64 lanes (LPR), VPL logits a lane, four neighbours at
 // a time. The choice is k rounds of a maximum over order-preserving 32-bit images of
-// logit + bias, the lowest index among equals; softmax statistics are fp32, shifted by the
-// row's maximum.
+// logit + bias, the lowest index among equals; each lane offers its best unit and knows its
+// second, and looks at its units again only when both are taken (one pass of VPL units instead
+// of one a round). Softmax statistics are fp32, shifted by the row's maximum.
 
 #include "som_mm.h"
 
 namespace som {
 namespace {
 
+using mm::exp_f32;
 using mm::load4;
 using mm::store4;
 
@@ -72,7 +74,7 @@ __device__ inline void open_unit(float logit, float bias, float &l, uint32_t &ke
     key = open ? image(s) : 0;
 }
 
-__device__ inline float score_sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
+__device__ inline float score_sigmoid(float l) { return 1.0f / (1.0f + exp_f32(fminf(-l, 88.0f))); }
 
 __device__ inline void store_weight(int type, void *p, int64_t at, float v)
 {
@@ -97,7 +99,7 @@ template <int LPR> __device__ inline float share(bool softmax, float l)
     if (!softmax) top = fminf(top, 0.0f);
     float s = 0;
     if (l > -__builtin_inff())
-        s = softmax ? expf(l - top) : top < 0.0f ? expf(l - top) / (1.0f + expf(l)) : score_sigmoid(l);
+        s = softmax ? exp_f32(l - top) : top < 0.0f ? exp_f32(l - top) / (1.0f + exp_f32(l)) : score_sigmoid(l);
     const float total = sum_f32<LPR>(s);
     return total > 0.0f ? s / total : 0.0f;
 }
@@ -133,12 +135,34 @@ template <int LPR, int VPL> struct Row {
         for (int i = 0; i < VPL; ++i) m = fmaxf(m, l[i]);
         return max_f32<LPR>(m);
     }
-    __device__ float total(float m) const
+    __device__ float total(float m)  // l becomes exp(l - m), 0 where closed
     {
+        const float shift = m > -__builtin_inff() ? m : 0.0f;
         float z = 0;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) z += l[i] > -__builtin_inff() ? expf(l[i] - m) : 0.0f;
+        for (int i = 0; i < VPL; ++i) {
+            l[i] = exp_f32(l[i] - shift);
+            z += l[i];
+        }
         return sum_f32<LPR>(z);
+    }
+
+    // The lane's two best units that rank after (key, e); 0 where there is none.
+    uint32_t v1, v2;
+    int i1, i2;
+    __device__ void two_best(uint32_t after, int e, int sub)
+    {
+        v1 = v2 = 0;
+        i1 = i2 = 0;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            const uint32_t x = key[i] < after || (key[i] == after && unit(i, sub) > e) ? key[i] : 0;
+            const bool first = x > v1, second = x > v2;
+            i2 = first ? i1 : second ? i : i2;
+            v2 = first ? v1 : second ? x : v2;
+            i1 = first ? i : i1;
+            v1 = first ? x : v1;
+        }
     }
 };
 
@@ -191,30 +215,68 @@ template <typename T, int LPR, int VPL> __global__ __launch_bounds__(kThreads) v
 
     // Place j is held by lane j of the row.
     int unit = -1;
+    r.two_best(~0u, 0, sub);
+    int left = 2;  // units the lane offers before it must look again
+    uint32_t last = ~0u;
+    int last_e = 0;
     for (int j = 0; j < a.k; ++j) {
-        uint32_t v = 0;
-        int at = 0;
-#pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (r.key[i] > v) v = r.key[i], at = i;
-        const uint32_t w = max_u32<LPR>(v);
-        const uint32_t e = min_u32<LPR>(v == w ? (uint32_t)Row<LPR, VPL>::unit(at, sub) : ~0u);
-        if (sub == j) unit = w ? (int)e : -1;
-#pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (Row<LPR, VPL>::unit(i, sub) == (int)e) r.key[i] = 0;
+        const int own = Row<LPR, VPL>::unit(r.i1, sub);
+        const uint32_t w = max_u32<LPR>(r.v1);
+        const int e = (int)min_u32<LPR>(r.v1 == w ? (uint32_t)own : ~0u);
+        if (sub == j) unit = w ? e : -1;
+        if (w && own == e && r.v1 == w) {
+            last = w;
+            last_e = e;
+            r.v1 = r.v2;
+            r.i1 = r.i2;
+            r.v2 = 0;
+            --left;
+        }
+        if (__any(left == 0) && j + 1 < a.k) {
+            if (left == 0) {
+                r.two_best(last, last_e, sub);
+                left = 2;
+            }
+        }
     }
 
     const bool took = unit >= 0;
     const float l = took ? fminf((float)p[unit], kMost) : -__builtin_inff();
     float s = 0;
     if (a.renorm) s = share<LPR>(softmax, l);
-    else if (took) s = softmax ? expf(l - m) / z : score_sigmoid(l);
+    else if (took) s = softmax ? exp_f32(l - m) / z : score_sigmoid(l);
     if (in && sub < a.k) {
         a.idx[row * a.k + sub] = unit;
         store_weight(a.weight_type, a.weights, row * a.k + sub, s);
-        if (a.counts && took) atomicAdd(&a.counts[unit], 1);
     }
+    // The counts: one workgroup counts its own rows; of more, the first clears them for k_counts.
+    if (a.counts && blockIdx.x == 0) {
+        for (int i = threadIdx.x; i < a.E; i += kThreads) a.counts[i] = 0;
+        if (gridDim.x == 1) {
+            __threadfence_block();
+            __syncthreads();
+            if (in && took) atomicAdd(&a.counts[unit], 1);
+        }
+    }
+}
+
+// How many rows took each unit: a workgroup counts its share of the choices in LDS and adds what
+// it found. (Adding every choice in global memory took 80 of 89 us for 16,411 rows and 8 of 256
+// units: neighbouring counts share a cache line, and a line takes about 90 additions a us.)
+__global__ __launch_bounds__(1024) void k_counts(const int32_t *__restrict__ idx, int64_t n, int E, int32_t *counts)
+{
+    __shared__ int own[SOM_ROUTE_MAX_UNITS];
+    for (int i = threadIdx.x; i < E; i += 1024) own[i] = 0;
+    __syncthreads();
+    const int64_t step = (int64_t)gridDim.x * 1024;
+#pragma unroll 4
+    for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < n; i += step) {
+        const int e = idx[i];
+        if (e >= 0) atomicAdd(&own[e], 1);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < E; i += 1024)
+        if (own[i]) atomicAdd(&counts[i], own[i]);
 }
 
 // softmax: dl = p (dw - sum dw p) over all open units (dw is 0 where a unit was not taken);
@@ -250,33 +312,42 @@ template <typename T, int LPR, int VPL> __global__ __launch_bounds__(kThreads) v
         m = r.top();
         z = r.total(m);
     }
+    const float over = z > 0.0f ? 1.0f / z : 0.0f;
     float g, sum = 0;  // g: the taken unit's gradient
     if (a.renorm) {
         const float w = share<LPR>(softmax, l);
         g = w * (dw - sum_f32<LPR>(dw * w));
         if (!softmax && took) g *= score_sigmoid(-l);
     } else if (softmax) {
-        const float s = took ? expf(l - m) / z : 0.0f;
+        const float s = took ? exp_f32(l - m) * over : 0.0f;
         sum = sum_f32<LPR>(dw * s);
         g = s * (dw - sum);
     } else {
         g = took ? dw * score_sigmoid(l) * score_sigmoid(-l) : 0.0f;
     }
 #pragma unroll
-    for (int i = 0; i < VPL; i += 4) {
-        const int e = Row<LPR, VPL>::unit(i, sub), n = max(0, min(4, a.E - e));
-        float v[4] = {0, 0, 0, 0};
-        if (shares) {
+    for (int i = 0; i < VPL; ++i) r.l[i] = shares ? -sum * over * r.l[i] : 0.0f;
+    for (int j = 0; j < a.k; ++j) {  // the taken units in their lanes
+        if (LPR == 64) {
+            const int u = __builtin_amdgcn_readlane(unit, j);
+            const float gj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), j));
+            if (u < 0) continue;
+            const int at = (u / (4 * LPR)) * 4 + u % 4;  // the same register in every lane
+            const bool mine = u / 4 % LPR == sub;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = r.l[i + q] > -__builtin_inff() ? -sum * (expf(r.l[i + q] - m) / z) : 0.0f;
-        }
-        for (int j = 0; j < a.k; ++j) {  // the taken units among these four
-            const int uj = __shfl(unit, j, LPR);
+            for (int i = 0; i < VPL; ++i)
+                if (i == at) r.l[i] = mine ? gj : r.l[i];
+        } else {
+            const int u = __shfl(unit, j, LPR);
             const float gj = __shfl(g, j, LPR);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = uj == e + q ? gj : v[q];
+            for (int i = 0; i < VPL; ++i) r.l[i] = Row<LPR, VPL>::unit(i, sub) == u ? gj : r.l[i];
         }
-        if (in && n > 0) store4(d + e, n, v);
+    }
+#pragma unroll
+    for (int i = 0; i < VPL; i += 4) {
+        const int e = Row<LPR, VPL>::unit(i, sub), n = max(0, min(4, a.E - e));
+        if (in && n > 0) store4(d + e, n, &r.l[i]);
     }
 }
 
@@ -286,6 +357,10 @@ __global__ void k_zero(int32_t *p, int n)
     if (i < n) p[i] = 0;
 }
 
+// Lanes that hold a row, and the rows of a workgroup.
+int lanes_of(const RouteArgs &a) { return a.E <= 256 && a.k <= 16 ? 16 : 64; }
+int rows_of_one(const RouteArgs &a) { return kThreads / lanes_of(a); }
+
 template <typename T, bool BWD> hipError_t pick(const RouteArgs &a, hipStream_t st)
 {
     auto go = [&](auto kernel, int lpr) {
@@ -294,14 +369,15 @@ template <typename T, bool BWD> hipError_t pick(const RouteArgs &a, hipStream_t 
         hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, st, a);
         return hipGetLastError();
     };
+    const bool few = lanes_of(a) == 16;
     if (BWD) {
-        if (a.E <= 64 && a.k <= 16) return go(k_route_bwd<T, 16, 4>, 16);
-        if (a.E <= 256 && a.k <= 16) return go(k_route_bwd<T, 16, 16>, 16);
+        if (few && a.E <= 64) return go(k_route_bwd<T, 16, 4>, 16);
+        if (few) return go(k_route_bwd<T, 16, 16>, 16);
         if (a.E <= 1024) return go(k_route_bwd<T, 64, 16>, 64);
         return go(k_route_bwd<T, 64, 64>, 64);
     }
-    if (a.E <= 64 && a.k <= 16) return go(k_route<T, 16, 4>, 16);
-    if (a.E <= 256 && a.k <= 16) return go(k_route<T, 16, 16>, 16);
+    if (few && a.E <= 64) return go(k_route<T, 16, 4>, 16);
+    if (few) return go(k_route<T, 16, 16>, 16);
     if (a.E <= 1024) return go(k_route<T, 64, 16>, 64);
     return go(k_route<T, 64, 64>, 64);
 }
@@ -317,12 +393,15 @@ template <bool BWD> hipError_t typed(int type, const RouteArgs &a, hipStream_t s
 
 hipError_t launch_route(int logit_type, const RouteArgs &a, hipStream_t st)
 {
-    if (a.counts) {
+    if (a.N == 0) {
         hipLaunchKernelGGL(k_zero, dim3((unsigned)((a.E + 255) / 256)), dim3(256), 0, st, a.counts, a.E);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess || a.N == 0) return e;
+        return hipGetLastError();
     }
-    return typed<false>(logit_type, a, st);
+    const hipError_t e = typed<false>(logit_type, a, st);
+    if (e != hipSuccess || !a.counts || a.N <= rows_of_one(a)) return e;
+    const int64_t n = a.N * a.k, blocks = (n + 8191) / 8192;
+    hipLaunchKernelGGL(k_counts, dim3((unsigned)(blocks < 32 ? blocks : 32)), dim3(1024), 0, st, a.idx, n, a.E, a.counts);
+    return hipGetLastError();
 }
 
 hipError_t launch_route_bwd(int logit_type, const RouteArgs &a, hipStream_t st)
