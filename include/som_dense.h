@@ -63,10 +63,11 @@ som_status som_linear(int32_t type, const void *X, int64_t ldx, const void *W, i
  *   dX [N, K] = dz W^T, dW [K, M] = X^T dz, dbias [M] (bias_type) = the column sums of dz, where
  *   dz = dY act'(pre); the residual's gradient is dY itself.
  * `pre` is what som_linear wrote; it is not read when act is SOM_ACT_NONE (then NULL will do). dz
- * is held in `type`. The workspace holds it: som_linear_bwd_workspace_bytes(N, M, act) bytes,
- * 256-byte aligned (0 bytes and NULL for SOM_ACT_NONE). N == 0 writes zeros to dW and dbias.
+ * is held in `type`. The workspace, som_linear_bwd_workspace_bytes(N, K, M, act) bytes, 256-byte
+ * aligned, holds dz (unless act is SOM_ACT_NONE) and, for many rows of a small dW, parts of it in
+ * fp32 (where it needs neither the size is 0 and NULL will do). N == 0 writes zeros to dW, dbias.
  */
-size_t som_linear_bwd_workspace_bytes(int64_t N, int64_t M, int32_t act);
+size_t som_linear_bwd_workspace_bytes(int64_t N, int64_t K, int64_t M, int32_t act);
 
 som_status som_linear_bwd(int32_t type, const void *X, int64_t ldx, const void *W, int64_t ldw, const void *pre,
                           int64_t ldp, int32_t act, const void *dY, int64_t lddy, void *dX, int64_t lddx, void *dW,

@@ -14,7 +14,7 @@ SOURCES = [os.path.join(CSRC, "som_sweep.hip"), os.path.join(CSRC, "som_rows.hip
            os.path.join(CSRC, "som_kernels.hip"), os.path.join(CSRC, "som_update.hip"),
            os.path.join(CSRC, "som_api.cpp"), os.path.join(CSRC, "som_noalloc.hip"),
            os.path.join(CSRC, "som_mm_nn.hip"), os.path.join(CSRC, "som_mm_nt.hip"),
-           os.path.join(CSRC, "som_mm_tn.hip"), os.path.join(CSRC, "som_route.hip"),
+           os.path.join(CSRC, "som_mm_tn.hip"), os.path.join(CSRC, "som_few.hip"), os.path.join(CSRC, "som_route.hip"),
            os.path.join(CSRC, "som_experts.hip"), os.path.join(CSRC, "som_clip.hip"),
            os.path.join(CSRC, "som_dense_api.cpp")]
 

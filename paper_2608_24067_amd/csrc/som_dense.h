@@ -32,7 +32,8 @@ struct Product {
     int64_t M, N, K;        // result rows and columns, reduction length (grouped: see below)
     // Grouped products. NN, NT: the tile rows; M is the number of pairs, B and the bias advance
     // by strideB and strideBias from expert to expert. TN: expert e reduces over the rows
-    // [off[e], off[e + 1]) and the result advances by strideC.
+    // [off[e], off[e + 1]) and the result advances by strideC; without `off` the groups are equal
+    // parts of the K rows.
     const TileRow *tiles;
     const int32_t *n_tiles;
     int32_t split;          // workgroup tiles in the height of a tile row
@@ -65,19 +66,25 @@ enum Epilogue {
 };
 
 // Rows of a tile of the product the host picks, so that the plan can lay the tile rows out.
-enum TileSize { kTileSmall, kTileMid, kTileLarge };
-constexpr int tile_rows(TileSize t) { return t == kTileSmall ? 32 : t == kTileMid ? 128 : 256; }
+enum TileSize { kTileFew, kTileSmall, kTileMid, kTileLarge };  // kTileFew: som_few.hip, else som_mm*.hip
+constexpr int tile_rows(TileSize t) { return t == kTileFew ? 16 : t == kTileSmall ? 32 : t == kTileMid ? 128 : 256; }
 constexpr int tile_cols(TileSize t) { return t == kTileLarge ? 256 : 128; }
 
 // Tile rows of a plan over P pairs of E experts, at most.
 inline int64_t max_tile_rows(int64_t P, int64_t E, int rows) { return P / rows + (E < P ? E : P); }
 
 hipError_t launch_nn(bool bf16, Epilogue e, TileSize t, const Product &p, hipStream_t st);
+// The same (kLinear, kInner, kPairs) for few rows. splits: workgroups that share out a tile's
+// reduction (kPairs only, else 1); split s of row m is written to row s * M + m of the result.
+hipError_t launch_few(bool bf16, Epilogue e, const Product &p, int splits, hipStream_t st);
 hipError_t launch_nt(bool bf16, Epilogue e, TileSize t, const Product &p, hipStream_t st);
-hipError_t launch_tn(bool bf16, const Product &p, hipStream_t st);
+hipError_t launch_tn(bool bf16, TileSize t, const Product &p, hipStream_t st);  // kTileMid or kTileLarge
 
-// Columns of a kSlope tile that share a partial sum.
-constexpr int slope_part_cols(TileSize t) { return t == kTileSmall ? 32 : 64; }
+// Partial sums of a row that a kSlope product over N columns leaves (one for each wave's columns).
+inline int64_t slope_parts(TileSize t, int64_t N)
+{
+    return (N + tile_cols(t) - 1) / tile_cols(t) * (tile_cols(t) / (t == kTileSmall ? 32 : 64));
+}
 
 // ---------------------------------------------------------------- routing
 
@@ -124,14 +131,20 @@ inline int pair_stretches(int64_t P)
 hipError_t launch_pairs(bool bf16, const int32_t *idx, const void *w, int64_t P, int32_t k, int32_t E, int rows,
                         const PairPlan &plan, hipStream_t st);
 
-// out[n] = res[n] + the rows y[pos[n, j]] (fp32, D wide) in the order of j.
-hipError_t launch_combine(bool bf16, const float *y, const int32_t *pos, int64_t N, int32_t k, int64_t D,
+// out[n] = res[n] + the rows y[pos[n, j]] (fp32, D wide) in the order of j, each the sum of
+// `splits` rows N k apart.
+hipError_t launch_combine(bool bf16, const float *y, int splits, const int32_t *pos, int64_t N, int32_t k, int64_t D,
                           const void *res, int64_t ldr, void *out, int64_t ldo, hipStream_t st);
 
 // dw[n, j] = the sum of parts[pos] plus <b2[idx], dout[n]>; 0 for a pair without an expert.
 hipError_t launch_weight_grad(bool bf16, const float *parts, int64_t n_parts, const int32_t *pos, const int32_t *idx,
                               const void *b2, const void *dout, int64_t lddo, int64_t N, int32_t k, int64_t D,
                               void *dw, hipStream_t st);
+
+// out = the sum of `parts` fp32 arrays of n values, one after the other, in their order; out is
+// fp32 or of the rows' type, in rows of M values ldo apart.
+hipError_t launch_sum_parts(bool bf16, const float *in, int parts, int64_t n, int64_t M, void *out, int64_t ldo,
+                            bool out_f32, hipStream_t st);
 
 // dz = dy act'(pre), rows of M elements; dz is dense.
 hipError_t launch_slope(bool bf16, const void *dy, int64_t lddy, const void *pre, int64_t ldp, int act, int64_t N,

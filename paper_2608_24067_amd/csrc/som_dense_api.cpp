@@ -43,6 +43,9 @@ bool dim_ok(int64_t v) { return v >= 1 && v < INT32_MAX; }
 // Whether an operand's rows can be moved in whole 16-byte chunks.
 bool chunks(const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0; }
 
+// Experts (and whole calls) of up to this many rows go to the kernel for few rows.
+constexpr int64_t kFewRows = 8;
+
 // The tile of a product of `rows` rows a group and `cols` columns. Large tiles read each
 // operand least often but need enough of them to fill the 256 CUs.
 som::TileSize pick_tile(int64_t rows, int64_t groups, int64_t cols, bool whole)
@@ -55,11 +58,31 @@ som::TileSize pick_tile(int64_t rows, int64_t groups, int64_t cols, bool whole)
     return som::kTileSmall;
 }
 
+// The tile of a product over rows (M x N a group). Large tiles pay from one a CU on (8192 rows,
+// 2048 x 4096, 128 of them: 172 us against 135 by Mid tiles; 10,007 rows to 32 experts, 1024 of
+// them: 107 against 143).
+som::TileSize pick_tile_tn(int64_t M, int64_t N, int64_t groups)
+{
+    return (M + 255) / 256 * ((N + 255) / 256) * groups >= 256 ? som::kTileLarge : som::kTileMid;
+}
+
+// Parts that a layer's weights' gradient (K x M from N rows) is computed in, where its tiles do
+// not fill the CUs: 512 rows a part at least, and at most 8 MB of fp32 parts.
+int grad_parts(int64_t N, int64_t K, int64_t M)
+{
+    const int64_t tiles = (K + 127) / 128 * ((M + 127) / 128), bytes = (K + 1) * M * 4;
+    int64_t n = 512 / tiles;
+    if (n > N / 512) n = N / 512;
+    if (n > (8 << 20) / bytes) n = (8 << 20) / bytes;
+    return n < 2 ? 1 : (int)n;
+}
+
 // ---------------------------------------------------------------- experts
 
 struct ExpertsLayout {
     size_t off, n_tiles, tiles, row, w, pos, counts, inner, y, pre, dz, parts, total;
     som::TileSize tile;
+    int splits;  // of the second product's reduction (few rows)
     int64_t n_parts;
 };
 
@@ -74,7 +97,14 @@ ExpertsLayout experts_layout(int64_t N, int32_t k, int64_t E, int64_t D, int64_t
     ExpertsLayout L;
     const int64_t P = N * k, met = P < E ? (P < 1 ? 1 : P) : E;
     L.tile = pick_tile(P / met, met, D < F ? D : F, D % 8 == 0 && F % 8 == 0);
-    L.n_parts = (F + som::slope_part_cols(som::kTileSmall) - 1) / som::slope_part_cols(som::kTileSmall);
+    L.splits = 1;
+    if (!keep && P / met <= kFewRows) {
+        // Few rows: fill the CUs by splitting the second reduction, a step of 32 a wave at least.
+        L.tile = som::kTileFew;
+        const int64_t tiles = met * ((D + 127) / 128), most = (F + 255) / 256;
+        while (L.splits < 16 && tiles * L.splits < 256 && L.splits * 2 <= most) L.splits *= 2;
+    }
+    L.n_parts = som::slope_parts(som::kTileSmall, F);  // the most of any tile
     size_t at = 0;
     auto take = [&](int64_t bytes) {
         const size_t p = at;
@@ -89,7 +119,7 @@ ExpertsLayout experts_layout(int64_t N, int32_t k, int64_t E, int64_t D, int64_t
     L.pos = take(P * 4);
     L.counts = take(som::pair_stretches(P) * E * 4);
     L.inner = take(P * F * 2);
-    L.y = take(P * D * 4);
+    L.y = take(L.splits * P * D * 4);
     L.pre = take(keep ? P * F * 2 : 0);
     L.dz = take(keep ? P * F * 2 : 0);
     L.parts = take(keep ? P * L.n_parts * 4 : 0);
@@ -168,15 +198,25 @@ som_status som_linear(int32_t type, const void *X, int64_t ldx, const void *W, i
     p.out = Y, p.ldo = ldy, p.out_f32 = y_type == SOM_F32;
     p.pre = pre, p.ldp = ldp;
     const bool whole = chunks(X, ldx) && chunks(W, ldw) && K % 8 == 0 && M % 8 == 0;
+    if (N <= 2 * kFewRows) {
+        const hipError_t e = som::launch_few(type == SOM_BF16, som::kLinear, p, 1, static_cast<hipStream_t>(stream));
+        return e == hipSuccess ? ok() : hip_fail(e, who);
+    }
     const hipError_t e = som::launch_nn(type == SOM_BF16, som::kLinear, pick_tile(N, 1, M, whole), p,
                                         static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, who);
 }
 
-size_t som_linear_bwd_workspace_bytes(int64_t N, int64_t M, int32_t act)
+static size_t slope_bytes(int64_t N, int64_t M, int32_t act)
 {
-    if (N < 0 || N >= INT32_MAX || !dim_ok(M) || !act_ok(act) || act == SOM_ACT_NONE) return 0;
-    return align256((size_t)N * (size_t)M * 2);
+    return act == SOM_ACT_NONE ? 0 : align256((size_t)N * (size_t)M * 2);
+}
+
+size_t som_linear_bwd_workspace_bytes(int64_t N, int64_t K, int64_t M, int32_t act)
+{
+    if (N < 0 || N >= INT32_MAX || !dim_ok(K) || !dim_ok(M) || !act_ok(act)) return 0;
+    const int parts = grad_parts(N, K, M);
+    return slope_bytes(N, M, act) + (parts > 1 ? align256((size_t)parts * (size_t)(K + 1) * (size_t)M * 4) : 0);
 }
 
 som_status som_linear_bwd(int32_t type, const void *X, int64_t ldx, const void *W, int64_t ldw, const void *pre,
@@ -197,7 +237,7 @@ som_status som_linear_bwd(int32_t type, const void *X, int64_t ldx, const void *
     if (odd(X, type) || odd(W, type) || (slope && odd(pre, type)) || odd(dY, type) || odd(dX, type) || odd(dW, type) ||
         (dbias && odd(dbias, bias_type)))
         return bad(who, "a pointer is not aligned to its elements");
-    const som_status st = check_workspace(who, workspace, workspace_bytes, som_linear_bwd_workspace_bytes(N, M, act));
+    const som_status st = check_workspace(who, workspace, workspace_bytes, som_linear_bwd_workspace_bytes(N, K, M, act));
     if (st != SOM_OK) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool bf16 = type == SOM_BF16;
@@ -222,9 +262,23 @@ som_status som_linear_bwd(int32_t type, const void *X, int64_t ldx, const void *
         Product p{};
         p.A = X, p.lda = ldx, p.B = dz, p.ldb = ldz;
         p.M = K, p.N = M, p.K = N, p.split = 1;
-        p.out = dW, p.ldo = lddw;
-        p.db = dbias, p.bias_f32 = bias_type == SOM_F32;
-        e = som::launch_tn(bf16, p, s);
+        const int parts = grad_parts(N, K, M);
+        if (parts == 1) {
+            p.out = dW, p.ldo = lddw;
+            p.db = dbias, p.bias_f32 = bias_type == SOM_F32;
+            e = som::launch_tn(bf16, pick_tile_tn(K, M, 1), p, s);
+            return e == hipSuccess ? ok() : hip_fail(e, who);
+        }
+        // each part's dW and column sums in fp32, then their sum
+        float *sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + slope_bytes(N, M, act));
+        float *cols = sums + (size_t)parts * (size_t)K * (size_t)M;
+        p.groups = parts;
+        p.out = dW ? sums : nullptr, p.ldo = M, p.out_f32 = 1, p.strideC = K * M;
+        p.db = dbias ? cols : nullptr, p.bias_f32 = 1, p.strideDb = M;
+        e = som::launch_tn(bf16, pick_tile_tn(K, M, parts), p, s);
+        if (e == hipSuccess && dW) e = som::launch_sum_parts(bf16, sums, parts, K * M, M, dW, lddw, false, s);
+        if (e == hipSuccess && dbias)
+            e = som::launch_sum_parts(bf16, cols, parts, M, M, dbias, M, bias_type == SOM_F32, s);
         if (e != hipSuccess) return hip_fail(e, who);
     }
     return ok();
@@ -345,7 +399,7 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
         p.w = x.plan.w;
         p.out = x.inner, p.ldo = F;
         if (keep) p.pre = x.pre, p.ldp = F;
-        e = som::launch_nn(bf16, som::kInner, t, p, s);
+        e = t == som::kTileFew ? som::launch_few(bf16, som::kInner, p, 1, s) : som::launch_nn(bf16, som::kInner, t, p, s);
         if (e != hipSuccess) return hip_fail(e, who);
     }
     {
@@ -357,10 +411,11 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
         p.bias = b2, p.strideBias = D;
         p.w = x.plan.w;
         p.out = x.y, p.ldo = D;
-        e = som::launch_nn(bf16, som::kPairs, t, p, s);
+        e = t == som::kTileFew ? som::launch_few(bf16, som::kPairs, p, L.splits, s)
+                               : som::launch_nn(bf16, som::kPairs, t, p, s);
         if (e != hipSuccess) return hip_fail(e, who);
     }
-    e = som::launch_combine(bf16, x.y, x.plan.pos, N, k, D, residual, ldr, out, ldo, s);
+    e = som::launch_combine(bf16, x.y, L.splits, x.plan.pos, N, k, D, residual, ldr, out, ldo, s);
     return e == hipSuccess ? ok() : hip_fail(e, who);
 }
 
@@ -403,7 +458,7 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
         p.pre = x.pre, p.ldp = F;
         p.out = x.dz, p.ldo = F;
         p.parts = x.parts;
-        p.n_parts = (F + som::slope_part_cols(t) - 1) / som::slope_part_cols(t);
+        p.n_parts = som::slope_parts(t, F);
         e = som::launch_nt(bf16, som::kSlope, t, p, s);
         if (e != hipSuccess) return hip_fail(e, who);
         if (dw) {
@@ -420,7 +475,7 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
         p.out = x.y, p.ldo = D;
         e = som::launch_nt(bf16, som::kPairs, t, p, s);
         if (e != hipSuccess) return hip_fail(e, who);
-        e = som::launch_combine(bf16, x.y, x.plan.pos, N, k, D, nullptr, 0, dX, lddx, s);
+        e = som::launch_combine(bf16, x.y, 1, x.plan.pos, N, k, D, nullptr, 0, dX, lddx, s);
         if (e != hipSuccess) return hip_fail(e, who);
     }
     if (dW1 || db1) {
@@ -431,7 +486,7 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
         p.off = x.plan.off, p.groups = (int32_t)E;
         p.out = dW1, p.ldo = F, p.strideC = D * F;
         p.db = db1, p.strideDb = F;
-        e = som::launch_tn(bf16, p, s);
+        e = som::launch_tn(bf16, pick_tile_tn(D, F, E), p, s);
         if (e != hipSuccess) return hip_fail(e, who);
     }
     if (dW2 || db2) {
@@ -442,7 +497,7 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
         p.off = x.plan.off, p.groups = (int32_t)E;
         p.out = dW2, p.ldo = D, p.strideC = D * F;
         p.db = db2, p.strideDb = D, p.w = x.plan.w;
-        e = som::launch_tn(bf16, p, s);
+        e = som::launch_tn(bf16, pick_tile_tn(F, D, E), p, s);
         if (e != hipSuccess) return hip_fail(e, who);
     }
     return ok();

@@ -166,7 +166,8 @@ __global__ __launch_bounds__(64) void k_pairs_place(const int32_t *__restrict__ 
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_combine(const float *__restrict__ y, const int32_t *__restrict__ pos,
+__global__ __launch_bounds__(256) void k_combine(const float *__restrict__ y, int splits,
+                                                 const int32_t *__restrict__ pos,
                                                  int64_t N, int k, int64_t D, const T *__restrict__ res, int64_t ldr,
                                                  T *out, int64_t ldo)
 {
@@ -181,6 +182,13 @@ __global__ __launch_bounds__(256) void k_combine(const float *__restrict__ y, co
             if (p < 0) continue;
             float v[4];
             load4(y + (int64_t)p * D + d, cnt, v);
+#pragma unroll 8
+            for (int r = 1; r < splits; ++r) {
+                float u[4];
+                load4(y + (r * N * k + p) * D + d, cnt, u);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] += u[q];
+            }
 #pragma unroll
             for (int q = 0; q < 4; ++q) s[q] += v[q];
         }
@@ -220,24 +228,55 @@ __global__ __launch_bounds__(256) void k_weight_grad(const float *__restrict__ p
     }
 }
 
+// in: parts arrays of n values; four values a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void k_sum_parts(const float *__restrict__ in, int parts, int64_t n, int64_t M,
+                                                   T *__restrict__ out, int64_t ldo)
+{
+    const int64_t per = (M + 3) / 4, total = n / M * per;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
+        const int64_t row = t / per, m = t % per * 4;
+        const int cnt = (int)min((int64_t)4, M - m);
+        float s[4] = {0, 0, 0, 0};
+#pragma unroll 8
+        for (int r = 0; r < parts; ++r) {
+            float v[4];
+            load4(in + r * n + row * M + m, cnt, v);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s[q] += v[q];
+        }
+        store4(out + row * ldo + m, cnt, s);
+    }
+}
+
+// Eight values of a row a thread.
 template <typename T>
 __global__ __launch_bounds__(256) void k_slope(const T *__restrict__ dy, int64_t lddy, const T *__restrict__ pre,
                                                int64_t ldp, int act, int64_t N, int64_t M, T *__restrict__ dz)
 {
-    const int64_t per = (M + 3) / 4, total = N * per;
+    typedef T vec __attribute__((ext_vector_type(8)));
+    typedef vec any __attribute__((aligned(2)));
+    const int64_t per = (M + 7) / 8, total = N * per;
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
-        const int64_t n = t / per, m = t % per * 4;
-        const int cnt = (int)min((int64_t)4, M - m);
-        float g[4], z[4];
-        load4(dy + n * lddy + m, cnt, g);
-        load4(pre + n * ldp + m, cnt, z);
+        const int64_t n = t / per, m = t % per * 8;
+        const T *g = dy + n * lddy + m, *z = pre + n * ldp + m;
+        T *out = dz + n * M + m;
+        float value, slope;
+        if (m + 8 <= M) {
+            const vec gv = *reinterpret_cast<const any *>(g), zv = *reinterpret_cast<const any *>(z);
+            vec r;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float value, slope;
-            mm::act_both(act, z[q], value, slope);
-            g[q] *= slope;
+            for (int q = 0; q < 8; ++q) {
+                mm::act_both(act, (float)zv[q], value, slope);
+                r[q] = (T)((float)gv[q] * slope);
+            }
+            *reinterpret_cast<any *>(out) = r;
+        } else {
+            for (int q = 0; m + q < M; ++q) {
+                mm::act_both(act, (float)z[q], value, slope);
+                out[q] = (T)((float)g[q] * slope);
+            }
         }
-        store4(dz + n * M + m, cnt, g);
     }
 }
 
@@ -273,15 +312,15 @@ hipError_t launch_pairs(bool bf16, const int32_t *idx, const void *w, int64_t P,
                 : with(&k_pairs<_Float16>, &k_pairs_place<_Float16>, static_cast<const _Float16 *>(w));
 }
 
-hipError_t launch_combine(bool bf16, const float *y, const int32_t *pos, int64_t N, int32_t k, int64_t D,
+hipError_t launch_combine(bool bf16, const float *y, int splits, const int32_t *pos, int64_t N, int32_t k, int64_t D,
                           const void *res, int64_t ldr, void *out, int64_t ldo, hipStream_t st)
 {
     const unsigned grid = spread((N * ((D + 3) / 4) + 255) / 256);
     if (bf16)
-        hipLaunchKernelGGL(k_combine<__bf16>, dim3(grid), dim3(256), 0, st, y, pos, N, k, D,
+        hipLaunchKernelGGL(k_combine<__bf16>, dim3(grid), dim3(256), 0, st, y, splits, pos, N, k, D,
                            static_cast<const __bf16 *>(res), ldr, static_cast<__bf16 *>(out), ldo);
     else
-        hipLaunchKernelGGL(k_combine<_Float16>, dim3(grid), dim3(256), 0, st, y, pos, N, k, D,
+        hipLaunchKernelGGL(k_combine<_Float16>, dim3(grid), dim3(256), 0, st, y, splits, pos, N, k, D,
                            static_cast<const _Float16 *>(res), ldr, static_cast<_Float16 *>(out), ldo);
     return hipGetLastError();
 }
@@ -302,10 +341,23 @@ hipError_t launch_weight_grad(bool bf16, const float *parts, int64_t n_parts, co
     return hipGetLastError();
 }
 
+hipError_t launch_sum_parts(bool bf16, const float *in, int parts, int64_t n, int64_t M, void *out, int64_t ldo,
+                            bool out_f32, hipStream_t st)
+{
+    const unsigned grid = spread((n / M * ((M + 3) / 4) + 255) / 256);
+    auto with = [&](auto kernel, auto *to) {
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, in, parts, n, M, to, ldo);
+        return hipGetLastError();
+    };
+    if (out_f32) return with(&k_sum_parts<float>, static_cast<float *>(out));
+    return bf16 ? with(&k_sum_parts<__bf16>, static_cast<__bf16 *>(out))
+                : with(&k_sum_parts<_Float16>, static_cast<_Float16 *>(out));
+}
+
 hipError_t launch_slope(bool bf16, const void *dy, int64_t lddy, const void *pre, int64_t ldp, int act, int64_t N,
                         int64_t M, void *dz, hipStream_t st)
 {
-    const unsigned grid = spread((N * ((M + 3) / 4) + 255) / 256);
+    const unsigned grid = spread((N * ((M + 7) / 8) + 255) / 256);
     if (bf16)
         hipLaunchKernelGGL(k_slope<__bf16>, dim3(grid), dim3(256), 0, st, static_cast<const __bf16 *>(dy), lddy,
                            static_cast<const __bf16 *>(pre), ldp, act, N, M, static_cast<__bf16 *>(dz));

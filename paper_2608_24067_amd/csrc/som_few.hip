@@ -1,0 +1,187 @@
+// som_few.hip -- products of few rows with feature-major matrices: bound by reading the matrix once.
+//
+// A workgroup has a tile of up to 16 rows and 128 columns; its waves share out the reduction. A
+// wave's step is 32 features: lane (c, g) reads, of features 8g ... 8g + 7, the eight columns
+// from 8c on (16 bytes each; sixteen lanes read 256 bytes of a feature), and turns these 8 x 8
+// values about in registers into eight operands of v_mfma_f32_16x16x32: operand j holds column
+// 8c + j of every lane. The matrix goes from memory to registers with no LDS and no barrier in
+// between, kDeep steps (32 KB a wave) in flight. The waves' sums meet in LDS, added in the waves'
+// order. Rows past the tile repeat its last one; features past the end count as zeros.
+//
+// Where the tiles are fewer than the CUs the reduction is also split over workgroups, whose
+// results (kPairs only) are added by the kernel that combines a row's pairs.
+
+#include "som_mm.h"
+
+namespace som {
+namespace {
+
+using namespace mm;
+
+constexpr int kWaves = 8, kThreads = 64 * kWaves, kDeep = 4, kCols = 128, kRows = tile_rows(kTileFew);
+
+// An 8 x 8 block of 16-bit values turned about: out[j] element k = in[k] element j.
+__device__ inline void turn(const s16x8 *in, s16x8 *out)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    u32x4 a[8], b[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) a[k] = __builtin_bit_cast(u32x4, in[k]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)  // values j of rows 2k and 2k + 1
+            b[j][k] = __builtin_amdgcn_perm(a[2 * k + 1][j / 2], a[2 * k][j / 2], j % 2 ? 0x07060302 : 0x05040100);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) out[j] = __builtin_bit_cast(s16x8, b[j]);
+}
+
+// n of 8 values at p, aligned to one; zeros for the others.
+__device__ inline s16x8 load8(const short *p, int n)
+{
+    typedef s16x8 any __attribute__((aligned(2)));
+    if (n >= 8) return *reinterpret_cast<const any *>(p);
+    s16x8 r = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < n) r[j] = p[j];
+    return r;
+}
+
+template <typename T, Epilogue EPI> __global__ __launch_bounds__(kThreads, 2) void k_few(const Product p, int splits)
+{
+    typedef typename Vec8<T>::type Frag;
+    __shared__ __align__(16) float lds[kWaves][kRows][kCols + 4];
+    const int nn = (int)((p.N + kCols - 1) / kCols);
+    const int nm = p.groups ? *p.n_tiles : (int)((p.M + kRows - 1) / kRows);
+    const int64_t t = blockIdx.x;
+    if (t >= (int64_t)nm * nn * splits) return;
+    const int split = (int)(t % splits), nt = (int)(t / splits % nn), mt = (int)(t / splits / nn);
+    int e = 0, m0 = mt * kRows, m1 = min((int)p.M, m0 + kRows);
+    if (p.groups) {
+        const TileRow r = p.tiles[mt];
+        e = r.e;
+        m0 = r.row;
+        m1 = min(r.end, m0 + kRows);
+    }
+    const int K = (int)p.K, N = (int)p.N;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int c = lane & 15, g = lane >> 4;
+    // This wave's steps: an even share of the whole reduction's.
+    const int parts = splits * kWaves, own = split * kWaves + wave, steps = (K + 31) / 32;
+    const int s0 = (int)((int64_t)steps * own / parts), s1 = (int)((int64_t)steps * (own + 1) / parts);
+
+    const int row = min(m0 + c, m1 - 1);
+    const short *a = static_cast<const short *>(p.A) + (p.amap ? (int64_t)p.amap[row] : (int64_t)row) * p.lda + 8 * g;
+    const int col = nt * kCols + 8 * c, cols = min(8, N - col);
+    const short *b = static_cast<const short *>(p.B) + (int64_t)e * p.strideB + 8 * (int64_t)g * p.ldb + (cols > 0 ? col : 0);
+
+    f32x4 acc[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = f32x4{0, 0, 0, 0};
+    auto multiply = [&](const s16x8 &va, const s16x8 *vb) {
+        s16x8 f[8];
+        turn(vb, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            acc[j] = mma(__builtin_bit_cast(Frag, f[j]), __builtin_bit_cast(Frag, va), acc[j]);
+    };
+    int s = s0;
+    if (nt * kCols + kCols <= N) {
+        typedef s16x8 any __attribute__((aligned(2)));
+        const int whole = min(s1, K / 32);  // steps with all their features
+        for (; s + kDeep <= whole; s += kDeep) {
+            s16x8 va[kDeep], vb[kDeep][8];
+#pragma unroll
+            for (int d = 0; d < kDeep; ++d) {
+                const int64_t k = (int64_t)(s + d) * 32;
+                va[d] = *reinterpret_cast<const any *>(a + k);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) vb[d][q] = *reinterpret_cast<const any *>(b + (k + q) * p.ldb);
+            }
+#pragma unroll
+            for (int d = 0; d < kDeep; ++d) multiply(va[d], vb[d]);
+        }
+        for (; s < whole; ++s) {
+            const int64_t k = (int64_t)s * 32;
+            s16x8 vb[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) vb[q] = *reinterpret_cast<const any *>(b + (k + q) * p.ldb);
+            const s16x8 va = *reinterpret_cast<const any *>(a + k);
+            multiply(va, vb);
+        }
+    }
+    for (; s < s1; ++s) {
+        const int64_t k = (int64_t)s * 32;
+        const int left = K - s * 32 - 8 * g;  // features of the lane's eight
+        s16x8 vb[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) vb[q] = load8(b + (k + q) * p.ldb, q < left ? cols : 0);
+        multiply(load8(a + k, left), vb);
+    }
+
+    // Lane (m, g) has columns (4g + i) 8 + j of row m in acc[j][i].
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            *reinterpret_cast<f32x4 *>(&lds[wave][c][(4 * g + i) * 8 + 4 * h]) =
+                f32x4{acc[4 * h][i], acc[4 * h + 1][i], acc[4 * h + 2][i], acc[4 * h + 3][i]};
+    __syncthreads();
+    const int r = threadIdx.x / (kCols / 4), q4 = threadIdx.x % (kCols / 4) * 4;
+    const int m = m0 + r, n = nt * kCols + q4, cnt = min(4, N - n);
+    if (m >= m1 || cnt <= 0) return;
+    f32x4 sum = *reinterpret_cast<const f32x4 *>(&lds[0][r][q4]);
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) sum += *reinterpret_cast<const f32x4 *>(&lds[w][r][q4]);
+    float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+    const float wr = EPI != kLinear && p.w ? p.w[m] : 1.0f;
+    if (p.bias && split == 0) {
+        float bias[4];
+        if (p.bias_f32) load4(static_cast<const float *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
+        else load4(static_cast<const T *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += EPI == kPairs ? wr * bias[q] : bias[q];
+    }
+    if (EPI == kPairs) {
+        store4(static_cast<float *>(p.out) + ((int64_t)split * p.M + m) * p.ldo + n, cnt, v);
+        return;
+    }
+    if (p.pre) store4(static_cast<T *>(p.pre) + (int64_t)m * p.ldp + n, cnt, v);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = act_value(p.act, v[q]);
+    if (EPI == kInner) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] *= wr;
+    }
+    if (EPI == kLinear && p.res) {
+        float t4[4];
+        load4(static_cast<const T *>(p.res) + (int64_t)m * p.ldr + n, cnt, t4);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += t4[q];
+    }
+    if (EPI == kLinear && p.out_f32) store4(static_cast<float *>(p.out) + (int64_t)m * p.ldo + n, cnt, v);
+    else store4(static_cast<T *>(p.out) + (int64_t)m * p.ldo + n, cnt, v);
+}
+
+template <typename T> hipError_t go(Epilogue e, const Product &p, int splits, hipStream_t st)
+{
+    const int64_t rows = p.groups ? max_tile_rows(p.M, p.groups, kRows) : (p.M + kRows - 1) / kRows;
+    const int64_t grid = rows * ((p.N + kCols - 1) / kCols) * splits;
+    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    auto with = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, st, p, splits);
+        return hipGetLastError();
+    };
+    return e == kLinear ? with(k_few<T, kLinear>) : e == kInner ? with(k_few<T, kInner>) : with(k_few<T, kPairs>);
+}
+
+}  // namespace
+
+hipError_t launch_few(bool bf16, Epilogue e, const Product &p, int splits, hipStream_t st)
+{
+    if (p.M <= 0 || p.N <= 0) return hipSuccess;
+    return bf16 ? go<__bf16>(e, p, splits, st) : go<_Float16>(e, p, splits, st);
+}
+
+}  // namespace som

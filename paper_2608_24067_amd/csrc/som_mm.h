@@ -22,6 +22,8 @@
 // and no stray infinity meets a zero.
 #pragma once
 
+#include <atomic>
+
 #include "som_dense.h"
 
 namespace som {
@@ -115,11 +117,12 @@ template <typename T> __device__ inline void load4(const T *p, int n, float *v)
     }
 }
 
-template <typename T> __device__ inline void store4(T *p, int n, const float *v)
+// v[from ... n - 1] to p + from ...
+template <typename T> __device__ inline void store4(T *p, int from, int n, const float *v)
 {
     typedef T vec __attribute__((ext_vector_type(4)));
     typedef vec any __attribute__((aligned(sizeof(T))));
-    if (n == 4) {
+    if (from <= 0 && n == 4) {
         vec t;
 #pragma unroll
         for (int i = 0; i < 4; ++i) t[i] = (T)v[i];
@@ -127,9 +130,11 @@ template <typename T> __device__ inline void store4(T *p, int n, const float *v)
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (i < n) p[i] = (T)v[i];
+            if (i >= from && i < n) p[i] = (T)v[i];
     }
 }
+
+template <typename T> __device__ inline void store4(T *p, int n, const float *v) { store4(p, 0, n, v); }
 
 // The place of 32-byte units in an "across" row.
 template <int BR> __device__ inline int unit_xor(int k)
@@ -222,6 +227,9 @@ template <typename T, int BR, bool ACROSS, bool MAPPED, int NT> struct Loader {
         look_up();
     }
 
+    // Whether all chunks' rows (columns) are inside; the same for every thread of the workgroup.
+    __device__ static bool covers(int r0, int r1) { return kChunks % NT == 0 && (!ACROSS || r0 + BR <= r1); }
+
     // Chunk i of the next tile, straight to LDS; INSIDE: the tile ends within the operand. The
     // instruction is written out because the compiler waits for every such load of its own before
     // any read of LDS; the kernel's loop waits as it needs. A wave's 64 chunks go to consecutive
@@ -238,12 +246,17 @@ template <typename T, int BR, bool ACROSS, bool MAPPED, int NT> struct Loader {
                      : "memory");
     }
 
-    // The next tile, into registers.
-    __device__ void fetch(s16x8 *r)
+    // The next tile, into registers. INSIDE: all of it lies within the operand; the loads are then
+    // unconditional, so that the compiler can count them and waits for no more than it needs.
+    template <bool INSIDE> __device__ void fetch(s16x8 *r)
     {
         typedef s16x8 any __attribute__((aligned(2)));
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
+            if (INSIDE) {
+                r[i] = *reinterpret_cast<const any *>(source(i));
+                continue;
+            }
             r[i] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
             if (!mine(i)) continue;
             const int left = K - t - k[i], n = ACROSS ? (left > 0 ? cnt[i] : 0) : min(8, left);
@@ -359,16 +372,22 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
     if (L == kTN) {
         const int nm = (int)((p.M + S::BM - 1) / S::BM);
         const int64_t per = (int64_t)nm * nn;
-        const int64_t t = tile_of(blockIdx.x, per * max(1, p.groups));
+        // Experts take unequal numbers of rows: their tiles go round the XCDs, not each expert's to one.
+        const int64_t total = per * max(1, p.groups);
+        const int64_t t = p.off ? (blockIdx.x < total ? (int64_t)blockIdx.x : -1) : tile_of(blockIdx.x, total);
         if (t < 0) return;
         e = (int)(t / per);
         tile_place(t % per, nm, nn, mt, nt);
         m0 = mt * S::BM;
         m1 = (int)p.M;
         K = (int)p.K;
-        if (p.groups) {
+        if (p.off) {
             k0 = p.off[e];
             K = p.off[e + 1] - (int)k0;
+        } else if (p.groups) {  // a part of the rows, whole tiles of them
+            const int len = ((K + p.groups - 1) / p.groups + kBK - 1) / kBK * kBK;
+            k0 = min((int64_t)e * len, (int64_t)K);
+            K = min(len, K - (int)k0);
         }
     } else {
         const int nm = p.groups ? *p.n_tiles * p.split : (int)((p.M + S::BM - 1) / S::BM);
@@ -386,7 +405,12 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
         }
         K = (int)p.K;
     }
-    const int n0 = nt * S::BN;
+    // Loads through registers: the last tile of columns (rows of a result by rows) is moved back to
+    // end with the operand, so that its loads need no checks; what it repeats is not written twice.
+    int n0 = nt * S::BN;
+    const int n_from = n0, m_from = m0;
+    if (!ASYNC && p.N >= S::BN) n0 = min(n0, (int)p.N - S::BN);
+    if (!ASYNC && L == kTN && p.M >= S::BM) m0 = min(m0, (int)p.M - S::BM);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave / S::WN, wn = wave % S::WN;
 
@@ -425,11 +449,23 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
 #pragma unroll
         for (int j = 0; j < S::NI; ++j) acc[i][j] = mma(b.f[j], a, acc[i][j]);
     };
-    auto add_sums = [&](int t, const FragsB &b) {
-        Frag ones;
-        const int k = t * kBK + 8 * (((int)threadIdx.x & 63) >> 4);
+    // The fragment that stands for the row of ones, or of the reduction rows' weights: those of tile
+    // t lie in LDS behind the tiles (ASYNC), or are read from memory. Rows of B past the end are
+    // zero, so the ones need no end.
+    constexpr int kWeights = kStages * kStage;  // [kStages][kBK] floats
+    Frag ones;
+    if (L == kTN) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) ones[q] = (T)(k + q < K ? (p.w ? p.w[k0 + k + q] : 1.0f) : 0.0f);
+        for (int q = 0; q < 8; ++q) ones[q] = (T)1.0f;
+    }
+    auto add_sums = [&](int t, const FragsB &b) {
+        if (p.w) {
+            const int octet = ((int)threadIdx.x & 63) >> 4, left = K - t * kBK - 8 * octet;
+            const float *own = reinterpret_cast<const float *>(lds + kWeights) + t % kStages * kBK + 8 * octet;
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                ones[q] = (T)(ASYNC ? own[q] : q < left ? p.w[k0 + t * kBK + 8 * octet + q] : 0.0f);
+        }
 #pragma unroll
         for (int w = 0; w < S::WM; ++w) {
             if (w != wm) continue;
@@ -449,8 +485,18 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
         // chunks than others counts on its own: kLoads is the least).
         constexpr int kLoads = LoadA::kChunks / S::NT + LoadB::kChunks / S::NT;
         static_assert(LoadA::kChunks % 64 == 0 && LoadB::kChunks % 64 == 0, "whole waves load");
+        const bool weights = L == kTN && sums && p.w && threadIdx.x < kBK;  // half of the first wave
+        auto load_weights = [&](int t) {
+            const int k = t * kBK + (int)threadIdx.x;
+            const void *from = k < K ? static_cast<const void *>(p.w + k0 + k) : static_cast<const void *>(g_zero);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                         :
+                         : "s"(base + (uint32_t)(kWeights + t % kStages * kBK * 4)), "v"(from)
+                         : "memory");
+        };
 #pragma unroll
         for (int t = 0; t < kStages - 1; ++t) {
+            if (weights) load_weights(t);
 #pragma unroll
             for (int i = 0; i < LoadA::kPer; ++i) la.template async<false>(i, base + t * kStage);
 #pragma unroll
@@ -471,6 +517,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
             const uint32_t here = base + (uint32_t)(t % kStages) * kStage;
             const uint32_t next = base + (uint32_t)((t + 1) % kStages) * kStage;
             const uint32_t to = base + (uint32_t)((t + kStages - 1) % kStages) * kStage;
+            if (weights) load_weights(t + kStages - 1);
             constexpr int kB = (2 * S::NI + S::MI - 1) / S::MI;  // fragments of B a row: done in the first half
             constexpr int kAll = LoadA::kPer + LoadB::kPer, kOf = (kAll + S::MI - 1) / S::MI;
 #pragma unroll
@@ -507,28 +554,35 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
         s16x8 va[kAhead][LoadA::kPer], vb[kAhead][LoadB::kPer];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            la.fetch(va[i]);
-            lb.fetch(vb[i]);
+            la.template fetch<false>(va[i]);
+            lb.template fetch<false>(vb[i]);
         }
-        for (int t0 = 0; t0 < steps; t0 += kAhead) {
+        auto step = [&](int t, int i, auto inside) {
+            constexpr bool kInside = decltype(inside)::value;
+            char *at = lds + (t % 2) * kStage;
+            LoadA::put(at, va[i]);
+            LoadB::put(at + LoadA::kBytes, vb[i]);
+            __syncthreads();
+            la.template fetch<kInside>(va[i]);
+            lb.template fetch<kInside>(vb[i]);
+            FragsB b;
+            const uint32_t from = base + (uint32_t)(t % 2) * kStage;
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int t = t0 + i;
-                if (t >= steps) break;
-                char *at = lds + (t % 2) * kStage;
-                LoadA::put(at, va[i]);
-                LoadB::put(at + LoadA::kBytes, vb[i]);
-                __syncthreads();
-                la.fetch(va[i]);
-                lb.fetch(vb[i]);
-                FragsB b;
-                const uint32_t from = base + (uint32_t)(t % 2) * kStage;
+            for (int j = 0; j < S::NI; ++j) b.f[j] = rb.read(from + LoadA::kBytes, j);
 #pragma unroll
-                for (int j = 0; j < S::NI; ++j) b.f[j] = rb.read(from + LoadA::kBytes, j);
+            for (int m = 0; m < S::MI; ++m) multiply_row(m, ra.read(from, m), b);
+            if (L == kTN && sums) add_sums(t, b);
+        };
+        int t = 0;
+        if (LoadA::covers(m0, m1) && LoadB::covers(n0, (int)p.N))
+            for (; (t + 2 * kAhead) * kBK <= K; t += kAhead) {
 #pragma unroll
-                for (int m = 0; m < S::MI; ++m) multiply_row(m, ra.read(from, m), b);
-                if (L == kTN && sums) add_sums(t, b);
+                for (int i = 0; i < kAhead; ++i) step(t + i, i, Inside<true>());
             }
+        for (; t < steps; t += kAhead) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (t + i < steps) step(t + i, i, Inside<false>());
         }
     }
 
@@ -541,6 +595,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
     const int row0 = m0 + wm * S::MI * 16, col0 = n0 + wn * kCols;
     const int64_t ob = L == kTN ? (int64_t)e * p.strideC : 0;
     const int sub = lane / kLanes, n = col0 + lane % kLanes * 4, cnt = min(4, (int)p.N - n);
+    const int skip = ASYNC ? 0 : min(4, n_from - n);  // the first of the four that another tile writes
     float *own = reinterpret_cast<float *>(lds) + wave * (16 * kRow);
     float bias[4] = {0, 0, 0, 0};
     if ((EPI == kLinear || EPI == kInner || EPI == kPairs) && p.bias && cnt > 0) {
@@ -553,7 +608,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
     // that its loads are in flight together and its branches are taken once.
     auto rows16 = [&](int i, auto whole) {
         constexpr bool W = decltype(whole)::value;
-        const int c4 = W ? 4 : cnt;
+        const int c4 = W ? 4 : cnt, c0 = W ? 0 : skip;
         float v[kTurns][4], wr[kTurns];
         int m[kTurns];
         bool in[kTurns];
@@ -561,7 +616,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
         for (int r = 0; r < kTurns; ++r) {
             const f32x4 c = *reinterpret_cast<const f32x4 *>(own + (r * kAtOnce + sub) * kRow + lane % kLanes * 4);
             m[r] = row0 + 16 * i + r * kAtOnce + sub;
-            in[r] = W || (m[r] < m1 && cnt > 0);
+            in[r] = W || (m[r] < m1 && m[r] >= m_from && cnt > 0 && skip < 4);
             wr[r] = (EPI == kInner || EPI == kPairs || EPI == kSlope) && p.w && in[r] ? p.w[m[r]] : 1.0f;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -574,7 +629,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
             if (p.pre) {
 #pragma unroll
                 for (int r = 0; r < kTurns; ++r)
-                    if (in[r]) store4(static_cast<T *>(p.pre) + (int64_t)m[r] * p.ldp + n, c4, v[r]);
+                    if (in[r]) store4(static_cast<T *>(p.pre) + (int64_t)m[r] * p.ldp + n, c0, c4, v[r]);
             }
             if (p.act == SOM_ACT_GELU) {
 #pragma unroll
@@ -623,7 +678,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
                     for (int q = 0; q < 4; ++q) {
                         float value, slope;
                         act_both(act, z[r][q], value, slope);
-                        part[r] += in[r] && q < c4 ? value * v[r][q] : 0.0f;
+                        part[r] += in[r] && q < c4 && q >= c0 ? value * v[r][q] : 0.0f;
                         v[r][q] *= wr[r] * slope;
                     }
                 }
@@ -638,16 +693,16 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
                 for (int r = 0; r < kTurns; ++r) part[r] += __shfl_xor(part[r], d);
 #pragma unroll
             for (int r = 0; r < kTurns; ++r)
-                if (in[r] && lane % kLanes == 0) p.parts[(int64_t)m[r] * p.n_parts + col0 / kCols] = part[r];
+                if (m[r] < m1 && lane % kLanes == 0) p.parts[(int64_t)m[r] * p.n_parts + nt * S::WN + wn] = part[r];
         }
-        if (EPI == kPairs || (EPI == kLinear && p.out_f32)) {
+        if (EPI == kPairs || ((EPI == kLinear || EPI == kGrad) && p.out_f32)) {
 #pragma unroll
             for (int r = 0; r < kTurns; ++r)
-                if (in[r]) store4(static_cast<float *>(p.out) + ob + (int64_t)m[r] * p.ldo + n, c4, v[r]);
+                if (in[r]) store4(static_cast<float *>(p.out) + ob + (int64_t)m[r] * p.ldo + n, c0, c4, v[r]);
         } else {
 #pragma unroll
             for (int r = 0; r < kTurns; ++r)
-                if (in[r]) store4(static_cast<T *>(p.out) + ob + (int64_t)m[r] * p.ldo + n, c4, v[r]);
+                if (in[r]) store4(static_cast<T *>(p.out) + ob + (int64_t)m[r] * p.ldo + n, c0, c4, v[r]);
         }
     };
 #pragma unroll 1
@@ -660,7 +715,8 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
             for (int j = 0; j < S::NI; ++j) *reinterpret_cast<f32x4 *>(own + li * kRow + j * 16 + 4 * g) = acc[at][j];
         }
         wave_sync_lds();
-        if (row0 + 16 * i + 16 <= m1 && col0 + kCols <= (int)p.N) rows16(i, Inside<true>());
+        if (row0 + 16 * i + 16 <= m1 && col0 + kCols <= (int)p.N && m0 == m_from && n0 == n_from)
+            rows16(i, Inside<true>());
         else rows16(i, Inside<false>());
         wave_sync_lds();
     }
@@ -694,17 +750,21 @@ template <typename T, Layout L, Epilogue EPI, class S, bool ASYNC, Mapped MAP = 
 hipError_t launch(const Product &p, int64_t tile_rows_total, hipStream_t st)
 {
     constexpr int kStage = (S::BM + S::BN) * kBK * 2;
-    constexpr int tiles = kStage * (ASYNC ? S::STAGES : 2), rows = S::WM * S::WN * 16 * (S::NI * 16 + 4) * 4;
+    constexpr int tiles = (kStage + (L == kTN ? kBK * 4 : 0)) * (ASYNC ? S::STAGES : 2), rows = S::WM * S::WN * 16 * (S::NI * 16 + 4) * 4;
     constexpr int bytes = tiles > rows ? tiles : rows;
     const int64_t nn = (p.N + S::BN - 1) / S::BN;
     const int64_t total = tile_rows_total * nn;
     if (total <= 0) return hipSuccess;
     const int64_t grid = (total + 7) / 8 * 8;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-    if (bytes > 64 << 10) {
+    // The attribute belongs to the function on each device; setting it again changes nothing.
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    if (bytes > 64 << 10 && (hipGetDevice(&dev) != hipSuccess || dev > 63 || !(done.load() >> dev & 1))) {
         const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_product<T, L, EPI, S, ASYNC, MAP>),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (err != hipSuccess) return err;
+        if (dev <= 63) done.fetch_or(1ull << dev);
     }
     hipLaunchKernelGGL((k_product<T, L, EPI, S, ASYNC, MAP>), dim3((unsigned)grid), dim3(S::NT), bytes, st, p);
     return hipGetLastError();

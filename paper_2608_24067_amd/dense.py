@@ -8,6 +8,7 @@ Matrices and rows may have any row stride; the elements of a row must be adjacen
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -38,26 +39,8 @@ def _type(t, name, halves=True):
     return _TYPES[t.dtype]
 
 
-def _mat(t, name, shape, dtype, device):
-    """Pointer and row stride of a matrix whose rows' elements are adjacent."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
-    if t.device != device or not t.is_cuda:
-        raise ValueError(f"{name} must be on the GPU, with the other tensors")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} must be {shape} (got {tuple(t.shape)})")
-    step, inner = t.stride()
-    if inner != 1 and shape[1] > 1:
-        raise ValueError(f"{name}: the elements of a row must be adjacent")
-    if shape[0] > 1 and step < shape[1]:
-        raise ValueError(f"{name}: rows overlap")
-    return t.data_ptr(), max(step, shape[1])
-
-
-def _vec(t, name, shape, dtype, device):
-    """Pointer of a contiguous tensor."""
+def _refuse(t, name, shape, dtype, device):
+    """Says what is wrong with a tensor that is not what it must be."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
@@ -66,6 +49,27 @@ def _vec(t, name, shape, dtype, device):
         raise ValueError(f"{name} must be on the GPU, with the other tensors")
     if tuple(t.shape) != shape:
         raise ValueError(f"{name} must be {shape} (got {tuple(t.shape)})")
+
+
+def _mat(t, name, shape, dtype, device):
+    """Pointer and row stride of a matrix whose rows' elements are adjacent."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape or not t.is_cuda:
+        _refuse(t, name, shape, dtype, device)
+    step, inner = t.stride()
+    if inner != 1 and shape[1] > 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    if step < shape[1]:
+        if shape[0] > 1:
+            raise ValueError(f"{name}: rows overlap")
+        step = shape[1]
+    return t.data_ptr(), step
+
+
+def _vec(t, name, shape, dtype, device):
+    """Pointer of a contiguous tensor of a type, or of one of several."""
+    if (not isinstance(t, torch.Tensor) or (t.dtype not in dtype if isinstance(dtype, tuple) else t.dtype != dtype)
+            or t.device != device or t.shape != shape or not t.is_cuda):
+        _refuse(t, name, shape, dtype, device)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
@@ -132,7 +136,7 @@ def linear_bwd(x, W, dy, pre=None, act: str = "none", out=None, bias_dtype=None,
                torch.empty(M, dtype=bias_dtype or x.dtype, device=dev))
     dx, dW, db = out
     lib = load()
-    ws = _work(workspace, lib.som_linear_bwd_workspace_bytes(N, M, a), dev)
+    ws = _work(workspace, lib.som_linear_bwd_workspace_bytes(N, K, M, a), dev)
     xp, ldx = _mat(x, "x", (N, K), x.dtype, dev)
     wp, ldw = _mat(W, "W", (K, M), x.dtype, dev)
     gp, ldg = _mat(dy, "dy", (N, M), x.dtype, dev)
@@ -148,6 +152,7 @@ def linear_bwd(x, W, dy, pre=None, act: str = "none", out=None, bias_dtype=None,
 
 # ------------------------------------------------------------------ routing
 
+@functools.lru_cache(maxsize=64)
 def _route_config(score, renorm, groups, group_top):
     c = _RouteConfig()
     c.score, c.renorm = _named(_SCORES, score, "score"), 1 if renorm else 0

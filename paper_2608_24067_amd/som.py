@@ -112,7 +112,7 @@ def load():
     # dense rows (dense.py)
     f32 = ctypes.c_float
     lib.som_linear.argtypes = [i32, vp, i64, vp, i64, vp, i32, i32, vp, i64, vp, i64, i32, vp, i64, i64, i64, i64, vp]
-    lib.som_linear_bwd_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.som_linear_bwd_workspace_bytes.argtypes = [i64, i64, i64, i32]
     lib.som_linear_bwd.argtypes = [i32, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp, i64, vp, i32, i64, i64,
                                    i64, vp, sz, vp]
     lib.som_route.argtypes = [i32, vp, i64, vp, i64, i64, i32, vp, vp, i32, vp, vp, vp]
