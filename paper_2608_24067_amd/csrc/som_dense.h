@@ -43,7 +43,7 @@ struct Product {
     // Epilogue.
     const void *bias;
     int32_t bias_f32, act;
-    const void *res;        // residual, rows' type
+    const void *res;        // residual, rows' type (kSlope: w act(pre) as the forward pass left it)
     int64_t ldr;
     void *out;
     int64_t ldo;
@@ -61,7 +61,7 @@ enum Epilogue {
     kLinear,  // out = res + act(acc + bias), pre = acc + bias
     kInner,   // out = w * act(acc + bias), pre = acc + bias
     kPairs,   // out (fp32) = acc + w * bias
-    kSlope,   // out = w * acc * act'(pre), parts = sum over columns of act(pre) * acc
+    kSlope,   // out = w * acc * act'(pre), parts = sum over columns of act(pre) * acc, act(pre) = res / w
     kGrad     // TN: out = acc, db = column sums of B
 };
 

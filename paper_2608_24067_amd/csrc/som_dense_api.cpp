@@ -456,6 +456,7 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
         p.N = F, p.K = D;
         p.act = act, p.w = x.plan.w;
         p.pre = x.pre, p.ldp = F;
+        p.res = x.inner, p.ldr = F;
         p.out = x.dz, p.ldo = F;
         p.parts = x.parts;
         p.n_parts = som::slope_parts(t, F);

@@ -165,7 +165,7 @@ __global__ __launch_bounds__(64) void k_pairs_place(const int32_t *__restrict__ 
     place(idx, w, first, last, k, E, lds, plan);
 }
 
-template <typename T>
+template <typename T, bool SPLIT>
 __global__ __launch_bounds__(256) void k_combine(const float *__restrict__ y, int splits,
                                                  const int32_t *__restrict__ pos,
                                                  int64_t N, int k, int64_t D, const T *__restrict__ res, int64_t ldr,
@@ -182,12 +182,14 @@ __global__ __launch_bounds__(256) void k_combine(const float *__restrict__ y, in
             if (p < 0) continue;
             float v[4];
             load4(y + (int64_t)p * D + d, cnt, v);
+            if (SPLIT) {
 #pragma unroll 8
-            for (int r = 1; r < splits; ++r) {
-                float u[4];
-                load4(y + (r * N * k + p) * D + d, cnt, u);
+                for (int r = 1; r < splits; ++r) {
+                    float u[4];
+                    load4(y + (r * N * k + p) * D + d, cnt, u);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] += u[q];
+                    for (int q = 0; q < 4; ++q) v[q] += u[q];
+                }
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) s[q] += v[q];
@@ -316,13 +318,18 @@ hipError_t launch_combine(bool bf16, const float *y, int splits, const int32_t *
                           const void *res, int64_t ldr, void *out, int64_t ldo, hipStream_t st)
 {
     const unsigned grid = spread((N * ((D + 3) / 4) + 255) / 256);
-    if (bf16)
-        hipLaunchKernelGGL(k_combine<__bf16>, dim3(grid), dim3(256), 0, st, y, splits, pos, N, k, D,
-                           static_cast<const __bf16 *>(res), ldr, static_cast<__bf16 *>(out), ldo);
-    else
-        hipLaunchKernelGGL(k_combine<_Float16>, dim3(grid), dim3(256), 0, st, y, splits, pos, N, k, D,
-                           static_cast<const _Float16 *>(res), ldr, static_cast<_Float16 *>(out), ldo);
-    return hipGetLastError();
+    auto with = [&](auto kernel, const auto *r, auto *o) {
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, y, splits, pos, N, k, D, r, ldr, o, ldo);
+        return hipGetLastError();
+    };
+    if (bf16) {
+        const auto *r = static_cast<const __bf16 *>(res);
+        auto *o = static_cast<__bf16 *>(out);
+        return splits > 1 ? with(&k_combine<__bf16, true>, r, o) : with(&k_combine<__bf16, false>, r, o);
+    }
+    const auto *r = static_cast<const _Float16 *>(res);
+    auto *o = static_cast<_Float16 *>(out);
+    return splits > 1 ? with(&k_combine<_Float16, true>, r, o) : with(&k_combine<_Float16, false>, r, o);
 }
 
 hipError_t launch_weight_grad(bool bf16, const float *parts, int64_t n_parts, const int32_t *pos, const int32_t *idx,

@@ -18,7 +18,7 @@ namespace {
 
 using namespace mm;
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves, kDeep = 4, kCols = 128, kRows = tile_rows(kTileFew);
+constexpr int kDeep = 4, kCols = 128, kRows = tile_rows(kTileFew);
 
 // An 8 x 8 block of 16-bit values turned about: out[j] element k = in[k] element j.
 __device__ inline void turn(const s16x8 *in, s16x8 *out)
@@ -48,7 +48,8 @@ __device__ inline s16x8 load8(const short *p, int n)
     return r;
 }
 
-template <typename T, Epilogue EPI> __global__ __launch_bounds__(kThreads, 2) void k_few(const Product p, int splits)
+template <typename T, Epilogue EPI, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int splits)
 {
     typedef typename Vec8<T>::type Frag;
     __shared__ __align__(16) float lds[kWaves][kRows][kCols + 4];
@@ -128,40 +129,41 @@ template <typename T, Epilogue EPI> __global__ __launch_bounds__(kThreads, 2) vo
             *reinterpret_cast<f32x4 *>(&lds[wave][c][(4 * g + i) * 8 + 4 * h]) =
                 f32x4{acc[4 * h][i], acc[4 * h + 1][i], acc[4 * h + 2][i], acc[4 * h + 3][i]};
     __syncthreads();
-    const int r = threadIdx.x / (kCols / 4), q4 = threadIdx.x % (kCols / 4) * 4;
-    const int m = m0 + r, n = nt * kCols + q4, cnt = min(4, N - n);
-    if (m >= m1 || cnt <= 0) return;
-    f32x4 sum = *reinterpret_cast<const f32x4 *>(&lds[0][r][q4]);
+    const int q4 = threadIdx.x % (kCols / 4) * 4, n = nt * kCols + q4, cnt = min(4, N - n);
+    for (int r = threadIdx.x / (kCols / 4); r < m1 - m0 && cnt > 0; r += 2 * kWaves) {
+        const int m = m0 + r;
+        f32x4 sum = *reinterpret_cast<const f32x4 *>(&lds[0][r][q4]);
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) sum += *reinterpret_cast<const f32x4 *>(&lds[w][r][q4]);
-    float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-    const float wr = EPI != kLinear && p.w ? p.w[m] : 1.0f;
-    if (p.bias && split == 0) {
-        float bias[4];
-        if (p.bias_f32) load4(static_cast<const float *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
-        else load4(static_cast<const T *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
+        for (int w = 1; w < kWaves; ++w) sum += *reinterpret_cast<const f32x4 *>(&lds[w][r][q4]);
+        float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+        const float wr = EPI != kLinear && p.w ? p.w[m] : 1.0f;
+        if (p.bias && split == 0) {
+            float bias[4];
+            if (p.bias_f32) load4(static_cast<const float *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
+            else load4(static_cast<const T *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] += EPI == kPairs ? wr * bias[q] : bias[q];
+            for (int q = 0; q < 4; ++q) v[q] += EPI == kPairs ? wr * bias[q] : bias[q];
+        }
+        if (EPI == kPairs) {
+            store4(static_cast<float *>(p.out) + ((int64_t)split * p.M + m) * p.ldo + n, cnt, v);
+            continue;
+        }
+        if (p.pre) store4(static_cast<T *>(p.pre) + (int64_t)m * p.ldp + n, cnt, v);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = act_value(p.act, v[q]);
+        if (EPI == kInner) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] *= wr;
+        }
+        if (EPI == kLinear && p.res) {
+            float t4[4];
+            load4(static_cast<const T *>(p.res) + (int64_t)m * p.ldr + n, cnt, t4);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] += t4[q];
+        }
+        if (EPI == kLinear && p.out_f32) store4(static_cast<float *>(p.out) + (int64_t)m * p.ldo + n, cnt, v);
+        else store4(static_cast<T *>(p.out) + (int64_t)m * p.ldo + n, cnt, v);
     }
-    if (EPI == kPairs) {
-        store4(static_cast<float *>(p.out) + ((int64_t)split * p.M + m) * p.ldo + n, cnt, v);
-        return;
-    }
-    if (p.pre) store4(static_cast<T *>(p.pre) + (int64_t)m * p.ldp + n, cnt, v);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = act_value(p.act, v[q]);
-    if (EPI == kInner) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] *= wr;
-    }
-    if (EPI == kLinear && p.res) {
-        float t4[4];
-        load4(static_cast<const T *>(p.res) + (int64_t)m * p.ldr + n, cnt, t4);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] += t4[q];
-    }
-    if (EPI == kLinear && p.out_f32) store4(static_cast<float *>(p.out) + (int64_t)m * p.ldo + n, cnt, v);
-    else store4(static_cast<T *>(p.out) + (int64_t)m * p.ldo + n, cnt, v);
 }
 
 template <typename T> hipError_t go(Epilogue e, const Product &p, int splits, hipStream_t st)
@@ -169,11 +171,19 @@ template <typename T> hipError_t go(Epilogue e, const Product &p, int splits, hi
     const int64_t rows = p.groups ? max_tile_rows(p.M, p.groups, kRows) : (p.M + kRows - 1) / kRows;
     const int64_t grid = rows * ((p.N + kCols - 1) / kCols) * splits;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-    auto with = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, st, p, splits);
+    auto with = [&](auto kernel, int waves) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * waves), 0, st, p, splits);
         return hipGetLastError();
     };
-    return e == kLinear ? with(k_few<T, kLinear>) : e == kInner ? with(k_few<T, kInner>) : with(k_few<T, kPairs>);
+    // Eight waves bring a tile's part of the matrix at once; from two tiles a CU on four do, so that
+    // one workgroup's loads run while the other adds up.
+    if (grid >= 512)
+        return e == kLinear ? with(k_few<T, kLinear, 4>, 4)
+               : e == kInner ? with(k_few<T, kInner, 4>, 4)
+                             : with(k_few<T, kPairs, 4>, 4);
+    return e == kLinear ? with(k_few<T, kLinear, 8>, 8)
+           : e == kInner ? with(k_few<T, kInner, 8>, 8)
+                         : with(k_few<T, kPairs, 8>, 8);
 }
 
 }  // namespace

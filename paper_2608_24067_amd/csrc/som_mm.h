@@ -59,6 +59,9 @@ __device__ inline float exp_f32(float x)
     return __builtin_amdgcn_exp2f(t) * fmaf(lost, 0.693147181f, 1.0f);
 }
 
+// exp(x) to |x| 2^-24 of it: enough where the result is rounded to 16 bits.
+__device__ inline float exp_short(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
 // The normal distribution Phi(z) and exp(-z^2 / 2), by formula 7.1.26 of Abramowitz and Stegun's
 // Handbook of Mathematical Functions for the error function: within 1.5e-7, which 16-bit results
 // do not see, for a third of erff's instructions.
@@ -66,7 +69,7 @@ __device__ inline float normal_f32(float z, float &bell)
 {
     const float x = fabsf(z) * 0.707106781f;
     const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
-    bell = exp_f32(-0.5f * z * z);
+    bell = exp_short(-0.5f * z * z);
     float q = fmaf(1.061405429f, t, -1.453152027f);
     q = fmaf(q, t, 1.421413741f);
     q = fmaf(q, t, -0.284496736f);
@@ -84,7 +87,7 @@ __device__ inline void act_both(int act, float z, float &value, float &slope)
         value = z <= 0.0f ? 0.0f : z;
         slope = z <= 0.0f ? 0.0f : z > 0.0f ? 1.0f : z;
     } else if (act == SOM_ACT_SILU) {
-        const float q = __builtin_amdgcn_rcpf(1.0f + exp_f32(fminf(-z, 88.0f)));
+        const float q = __builtin_amdgcn_rcpf(1.0f + exp_short(fminf(-z, 88.0f)));
         value = z * q;
         slope = q * fmaf(z, 1.0f - q, 1.0f);
     } else if (act == SOM_ACT_GELU) {
@@ -606,8 +609,38 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
     constexpr int kTurns = 16 / kAtOnce;
     // 16 rows: a lane's four columns of every kAtOnce-th row. Each stage runs over all of them, so
     // that its loads are in flight together and its branches are taken once.
+    // What it reads besides (residual; z and w act(z)) is loaded sixteen rows ahead.
+    typedef T vec4 __attribute__((ext_vector_type(4)));
+    typedef vec4 any4 __attribute__((aligned(sizeof(T))));
+    const bool cols_in = col0 + kCols <= (int)p.N && n0 == n_from && m0 == m_from;
+    constexpr bool kReads = EPI == kLinear || EPI == kSlope;
+    vec4 ahead[kReads ? kTurns : 1], ahead2[EPI == kSlope ? kTurns : 1];
+    auto is_whole = [&](int i) { return cols_in && row0 + 16 * i + 16 <= m1; };
+    auto fetch16 = [&](int i) {
+        if (!kReads || i >= S::MI || !is_whole(i)) return;
+#pragma unroll
+        for (int r = 0; r < kTurns; ++r) {
+            const int64_t row = row0 + 16 * i + r * kAtOnce + sub;
+            if (EPI == kSlope) {
+                ahead[r] = *reinterpret_cast<const any4 *>(static_cast<const T *>(p.pre) + row * p.ldp + n);
+                ahead2[r] = *reinterpret_cast<const any4 *>(static_cast<const T *>(p.res) + row * p.ldr + n);
+            } else if (p.res) {
+                ahead[r] = *reinterpret_cast<const any4 *>(static_cast<const T *>(p.res) + row * p.ldr + n);
+            }
+        }
+    };
+    fetch16(0);
     auto rows16 = [&](int i, auto whole) {
         constexpr bool W = decltype(whole)::value;
+        vec4 now[kReads ? kTurns : 1], now2[EPI == kSlope ? kTurns : 1];
+        if (W && kReads) {
+#pragma unroll
+            for (int r = 0; r < kTurns; ++r) {
+                now[r] = ahead[r];
+                if (EPI == kSlope) now2[r] = ahead2[r];
+            }
+        }
+        fetch16(i + 1);
         const int c4 = W ? 4 : cnt, c0 = W ? 0 : skip;
         float v[kTurns][4], wr[kTurns];
         int m[kTurns];
@@ -657,27 +690,46 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
         if (EPI == kLinear && p.res) {
             float t[kTurns][4];
 #pragma unroll
-            for (int r = 0; r < kTurns; ++r)
-                if (in[r]) load4(static_cast<const T *>(p.res) + (int64_t)m[r] * p.ldr + n, c4, t[r]);
+            for (int r = 0; r < kTurns; ++r) {
+                if (W) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) t[r][q] = (float)now[r][q];
+                } else if (in[r]) {
+                    load4(static_cast<const T *>(p.res) + (int64_t)m[r] * p.ldr + n, c4, t[r]);
+                }
+            }
 #pragma unroll
             for (int r = 0; r < kTurns; ++r)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) v[r][q] += t[r][q];
         }
         if (EPI == kSlope) {
-            float z[kTurns][4];
+            float z[kTurns][4], h[kTurns][4];
 #pragma unroll
-            for (int r = 0; r < kTurns; ++r)
-                if (in[r]) load4(static_cast<const T *>(p.pre) + (int64_t)m[r] * p.ldp + n, c4, z[r]);
+            for (int r = 0; r < kTurns; ++r) {
+                if (W) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) z[r][q] = (float)now[r][q], h[r][q] = (float)now2[r][q];
+                } else if (in[r]) {
+                    load4(static_cast<const T *>(p.pre) + (int64_t)m[r] * p.ldp + n, c4, z[r]);
+                    load4(static_cast<const T *>(p.res) + (int64_t)m[r] * p.ldr + n, c4, h[r]);
+                }
+            }
             float part[kTurns];
             auto slopes = [&](int act) {
 #pragma unroll
                 for (int r = 0; r < kTurns; ++r) {
+                    // act(z) from w act(z) as the forward pass rounded it: one rounding, where act of
+                    // the rounded z adds what its slope makes of another; not for weights so
+                    // small that the product may have lost bits to fp16's subnormals
+                    const bool held = fabsf(wr[r]) >= 1.0f / 64;
+                    const float over = held ? 1.0f / wr[r] : 0.0f;
                     part[r] = 0.0f;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         float value, slope;
                         act_both(act, z[r][q], value, slope);
+                        value = held ? h[r][q] * over : value;
                         part[r] += in[r] && q < c4 && q >= c0 ? value * v[r][q] : 0.0f;
                         v[r][q] *= wr[r] * slope;
                     }
@@ -715,8 +767,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
             for (int j = 0; j < S::NI; ++j) *reinterpret_cast<f32x4 *>(own + li * kRow + j * 16 + 4 * g) = acc[at][j];
         }
         wave_sync_lds();
-        if (row0 + 16 * i + 16 <= m1 && col0 + kCols <= (int)p.N && m0 == m_from && n0 == n_from)
-            rows16(i, Inside<true>());
+        if (is_whole(i)) rows16(i, Inside<true>());
         else rows16(i, Inside<false>());
         wave_sync_lds();
     }

@@ -1,7 +1,7 @@
 // som_route.hip -- each row's k best units by its logits, their weights, and the gradient.
 //
 // A row is held in the registers of 16 or 64 lanes (LPR), VPL logits a lane, four neighbours at
-// a time. The choice is k rounds of a maximum over order-preserving 32-bit images of
+// a time. The choice is k rounds of a maximum over (closed units: minus infinity)
 // logit + bias, the lowest index among equals; each lane offers its best unit and knows its
 // second, and looks at its units again only when both are taken (one pass of VPL units instead
 // of one a round). Softmax statistics are fp32, shifted by the row's maximum.
@@ -12,6 +12,7 @@ namespace som {
 namespace {
 
 using mm::exp_f32;
+using mm::exp_short;
 using mm::load4;
 using mm::store4;
 
@@ -56,22 +57,13 @@ template <int LPR> __device__ inline float sum_f32(float v)
     }));
 }
 
-// Order-preserving image of a float that is neither NaN nor -inf; 0 stands for a closed unit.
-__device__ inline uint32_t image(float v)
-{
-    const uint32_t u = __float_as_uint(v);
-    return (u >> 31) ? ~u : u | 0x80000000u;
-}
-
 constexpr float kMost = 3.402823466e38f;
 
-// A logit as it is weighed (+inf counts as the largest value), its ranked key's image (0: closed).
-__device__ inline void open_unit(float logit, float bias, float &l, uint32_t &key)
+// What a unit is ranked by: logit + bias (fp32, one rounding; -0 + 0 is 0), -inf for a closed one.
+__device__ inline float rank_key(float logit, float bias)
 {
-    const float s = logit + bias;  // -0 + 0 is 0: the two zeros rank alike
-    const bool open = logit > -__builtin_inff() && s > -__builtin_inff();  // false for NaN
-    l = open ? fminf(logit, kMost) : -__builtin_inff();
-    key = open ? image(s) : 0;
+    const float s = logit + bias;
+    return logit > -__builtin_inff() && s > -__builtin_inff() ? s : -__builtin_inff();  // false for NaN
 }
 
 __device__ inline float score_sigmoid(float l) { return 1.0f / (1.0f + exp_f32(fminf(-l, 88.0f))); }
@@ -108,21 +100,32 @@ template <int LPR, int VPL> struct Row {
     // Logit i of lane `sub` of a row: neighbours of four, the lanes' fours side by side.
     __device__ static int unit(int i, int sub) { return (i >> 2) * 4 * LPR + 4 * sub + (i & 3); }
 
-    float l[VPL];
-    uint32_t key[VPL];
+    float l[VPL];    // logits, at most the largest finite value; -inf for a closed unit
+    float key[VPL];  // what they are ranked by
 
-    template <typename T> __device__ void load(const T *p, const float *bias, int E, int sub)
+    template <bool BIAS, typename T> __device__ void load(const T *p, const float *bias, int E, int sub)
     {
 #pragma unroll
         for (int i = 0; i < VPL; i += 4) {
             const int e = unit(i, sub), n = max(0, min(4, E - e));
-            float v[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0};
-            if (n > 0) load4(p + e, n, v);
-            if (bias && n > 0) load4(bias + e, n, b);
+            float v[4], b[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = -__builtin_inff();
+            if (n == 4) {
+                load4(p + e, 4, v);
+                if (BIAS) load4(bias + e, 4, b);
+            } else if (n > 0) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (q < n) {
+                        v[q] = (float)p[e + q];
+                        if (BIAS) b[q] = bias[e + q];
+                    }
+            }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                open_unit(v[q], b[q], l[i + q], key[i + q]);
-                if (q >= n) l[i + q] = -__builtin_inff(), key[i + q] = 0;
+                key[i + q] = BIAS ? rank_key(v[q], b[q]) : fmaxf(v[q] + 0.0f, -__builtin_inff());  // NaN: -inf; -0: 0
+                l[i + q] = fminf(!BIAS ? key[i + q] : key[i + q] > -__builtin_inff() ? v[q] : key[i + q], kMost);
             }
         }
     }
@@ -141,22 +144,23 @@ template <int LPR, int VPL> struct Row {
         float z = 0;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            l[i] = exp_f32(l[i] - shift);
+            l[i] = exp_short(l[i] - shift);
             z += l[i];
         }
         return sum_f32<LPR>(z);
     }
 
-    // The lane's two best units that rank after (key, e); 0 where there is none.
-    uint32_t v1, v2;
+    // The lane's two best units, -inf where there is none; AGAIN: of those that rank after (after, e).
+    float v1, v2;
     int i1, i2;
-    __device__ void two_best(uint32_t after, int e, int sub)
+    template <bool AGAIN> __device__ void two_best(float after, int e, int sub)
     {
-        v1 = v2 = 0;
+        v1 = v2 = -__builtin_inff();
         i1 = i2 = 0;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            const uint32_t x = key[i] < after || (key[i] == after && unit(i, sub) > e) ? key[i] : 0;
+            const float x =
+                !AGAIN || key[i] < after || (key[i] == after && unit(i, sub) > e) ? key[i] : -__builtin_inff();
             const bool first = x > v1, second = x > v2;
             i2 = first ? i1 : second ? i : i2;
             v2 = first ? v1 : second ? x : v2;
@@ -168,7 +172,26 @@ template <int LPR, int VPL> struct Row {
 
 constexpr int kThreads = 256;
 
-template <typename T, int LPR, int VPL> __global__ __launch_bounds__(kThreads) void k_route(const RouteArgs a)
+// An order-preserving image of a float that is no NaN (and no -0); 0 lies below all, kClosed is -inf's.
+__device__ inline uint32_t image(float v)
+{
+    const uint32_t u = __float_as_uint(v);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+constexpr uint32_t kClosed = 0x007fffffu;
+
+// The lowest unit of the row's lanes that are `in` (one at least): nearly always there is one.
+template <int LPR> __device__ inline int lowest(bool in, int own)
+{
+    if (LPR == 64) {
+        const unsigned long long lanes = __ballot(in);
+        if ((lanes & (lanes - 1)) == 0) return __builtin_amdgcn_readlane(own, __builtin_ctzll(lanes));
+    }
+    return (int)min_u32<LPR>(in ? (uint32_t)own : ~0u);
+}
+
+template <typename T, int LPR, int VPL, bool BIAS>
+__global__ __launch_bounds__(kThreads) void k_route(const RouteArgs a)
 {
     constexpr int kRows = kThreads / LPR;
     __shared__ uint32_t best[kRows][SOM_ROUTE_MAX_GROUPS];
@@ -179,7 +202,7 @@ template <typename T, int LPR, int VPL> __global__ __launch_bounds__(kThreads) v
     const T *p = static_cast<const T *>(a.logits) + (in ? row : 0) * a.ldl;
 
     Row<LPR, VPL> r;
-    r.load(p, a.bias, a.E, sub);
+    r.template load<BIAS>(p, a.bias, a.E, sub);
     float m = 0, z = 1;
     const bool softmax = a.score == SOM_SCORE_SOFTMAX;
     if (softmax && !a.renorm) {
@@ -189,13 +212,26 @@ template <typename T, int LPR, int VPL> __global__ __launch_bounds__(kThreads) v
     if (a.groups > 1) {
         // Groups by their best unit; one is kept if fewer than group_top are better (the lower
         // one first among equals).
-        const float inv = 1.0f / (float)(a.E / a.groups);  // (e + 1/2) inv is never near a whole number
+        const int width = a.E / a.groups;
+        const float inv = 1.0f / (float)width;  // (e + 1/2) inv is never near a whole number
+        const bool fours = width % 4 == 0;      // a lane's four neighbours are of one group
         for (int g = sub; g < a.groups; g += LPR) best[slot][g] = 0;
         if (sub == 0) kept[slot] = 0;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (r.key[i]) atomicMax(&best[slot][(int)((Row<LPR, VPL>::unit(i, sub) + 0.5f) * inv)], r.key[i]);
+        for (int i = 0; i < VPL; i += 4) {
+            const int e = Row<LPR, VPL>::unit(i, sub);
+            if (e >= a.E) continue;
+            if (fours) {
+                const float v = fmaxf(fmaxf(r.key[i], r.key[i + 1]), fmaxf(r.key[i + 2], r.key[i + 3]));
+                if (v > -__builtin_inff()) atomicMax(&best[slot][(int)((e + 0.5f) * inv)], image(v));
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (r.key[i + q] > -__builtin_inff())
+                        atomicMax(&best[slot][(int)((e + q + 0.5f) * inv)], image(r.key[i + q]));
+            }
+        }
         __syncthreads();
         for (int g = sub; g < a.groups; g += LPR) {
             const uint32_t own = best[slot][g];
@@ -209,32 +245,41 @@ template <typename T, int LPR, int VPL> __global__ __launch_bounds__(kThreads) v
         __syncthreads();
         const unsigned long long keep = kept[slot];
 #pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (!(keep >> (int)((Row<LPR, VPL>::unit(i, sub) + 0.5f) * inv) & 1)) r.key[i] = 0;
+        for (int i = 0; i < VPL; i += 4) {
+            const int e = Row<LPR, VPL>::unit(i, sub);
+            if (e >= a.E) continue;
+            const bool in4 = keep >> (int)((e + 0.5f) * inv) & 1;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bool keep1 = fours ? in4 : keep >> (int)((e + q + 0.5f) * inv) & 1;
+                r.key[i + q] = keep1 ? r.key[i + q] : -__builtin_inff();
+            }
+        }
     }
 
     // Place j is held by lane j of the row.
     int unit = -1;
-    r.two_best(~0u, 0, sub);
+    r.template two_best<false>(0.0f, 0, sub);
     int left = 2;  // units the lane offers before it must look again
-    uint32_t last = ~0u;
+    float last = 0.0f;
     int last_e = 0;
     for (int j = 0; j < a.k; ++j) {
         const int own = Row<LPR, VPL>::unit(r.i1, sub);
-        const uint32_t w = max_u32<LPR>(r.v1);
-        const int e = (int)min_u32<LPR>(r.v1 == w ? (uint32_t)own : ~0u);
-        if (sub == j) unit = w ? e : -1;
-        if (w && own == e && r.v1 == w) {
-            last = w;
+        const uint32_t offer = image(r.v1), w = max_u32<LPR>(offer);
+        const bool some = w > kClosed;
+        const int e = lowest<LPR>(offer == w, own);
+        if (sub == j) unit = some ? e : -1;
+        if (some && own == e && offer == w) {
+            last = r.v1;
             last_e = e;
             r.v1 = r.v2;
             r.i1 = r.i2;
-            r.v2 = 0;
+            r.v2 = -__builtin_inff();
             --left;
         }
-        if (__any(left == 0) && j + 1 < a.k) {
+        if (j + 1 < a.k && __any(left == 0)) {
             if (left == 0) {
-                r.two_best(last, last_e, sub);
+                r.template two_best<true>(last, last_e, sub);
                 left = 2;
             }
         }
@@ -282,7 +327,8 @@ __global__ __launch_bounds__(1024) void k_counts(const int32_t *__restrict__ idx
 // softmax: dl = p (dw - sum dw p) over all open units (dw is 0 where a unit was not taken);
 // renormalised: dl = w (dw - sum dw w) over the taken ones; sigmoid: dl = dw s (1 - s);
 // renormalised: dl = w (1 - s) (dw - sum dw w).
-template <typename T, int LPR, int VPL> __global__ __launch_bounds__(kThreads) void k_route_bwd(const RouteArgs a)
+template <typename T, int LPR, int VPL, bool BIAS>
+__global__ __launch_bounds__(kThreads) void k_route_bwd(const RouteArgs a)
 {
     constexpr int kRows = kThreads / LPR;
     const int sub = threadIdx.x % LPR, slot = threadIdx.x / LPR;
@@ -296,9 +342,8 @@ template <typename T, int LPR, int VPL> __global__ __launch_bounds__(kThreads) v
     int unit = sub < a.k ? a.idx[at * a.k + sub] : -1;
     float l = -__builtin_inff();
     if (unit >= 0 && unit < a.E) {
-        uint32_t key;
-        open_unit((float)p[unit], a.bias ? a.bias[unit] : 0.0f, l, key);
-        if (!key) unit = -1;
+        l = fminf((float)p[unit], kMost);
+        if (!(rank_key((float)p[unit], BIAS ? a.bias[unit] : 0.0f) > -__builtin_inff())) unit = -1, l = -__builtin_inff();
     } else {
         unit = -1;
     }
@@ -308,7 +353,7 @@ template <typename T, int LPR, int VPL> __global__ __launch_bounds__(kThreads) v
     Row<LPR, VPL> r;
     float m = 0, z = 1;
     if (shares) {
-        r.load(p, a.bias, a.E, sub);
+        r.template load<BIAS>(p, a.bias, a.E, sub);
         m = r.top();
         z = r.total(m);
     }
@@ -357,36 +402,41 @@ __global__ void k_zero(int32_t *p, int n)
     if (i < n) p[i] = 0;
 }
 
-// Lanes that hold a row, and the rows of a workgroup.
-int lanes_of(const RouteArgs &a) { return a.E <= 256 && a.k <= 16 ? 16 : 64; }
+// Lanes that hold a row: 16 for up to 64 units (four rows a wave), else 64. (256 units and 8 taken:
+// 16 lanes of 16 units look at them again in most rounds, 64 lanes of four hardly ever.)
+int lanes_of(const RouteArgs &a) { return a.E <= 64 && a.k <= 16 ? 16 : 64; }
 int rows_of_one(const RouteArgs &a) { return kThreads / lanes_of(a); }
 
-template <typename T, bool BWD> hipError_t pick(const RouteArgs &a, hipStream_t st)
+template <typename T, bool BWD, bool BIAS> hipError_t pick(const RouteArgs &a, hipStream_t st)
 {
-    auto go = [&](auto kernel, int lpr) {
-        const int64_t rows = kThreads / lpr, grid = (a.N + rows - 1) / rows;
+    auto go = [&](auto kernel) {
+        const int64_t rows = rows_of_one(a), grid = (a.N + rows - 1) / rows;
         if (grid > INT32_MAX) return hipErrorInvalidValue;
         hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, st, a);
         return hipGetLastError();
     };
-    const bool few = lanes_of(a) == 16;
-    if (BWD) {
-        if (few && a.E <= 64) return go(k_route_bwd<T, 16, 4>, 16);
-        if (few) return go(k_route_bwd<T, 16, 16>, 16);
-        if (a.E <= 1024) return go(k_route_bwd<T, 64, 16>, 64);
-        return go(k_route_bwd<T, 64, 64>, 64);
+    if constexpr (BWD) {
+        if (lanes_of(a) == 16) return go(k_route_bwd<T, 16, 4, BIAS>);
+        if (a.E <= 256) return go(k_route_bwd<T, 64, 4, BIAS>);
+        if (a.E <= 1024) return go(k_route_bwd<T, 64, 16, BIAS>);
+        return go(k_route_bwd<T, 64, 64, BIAS>);
+    } else {
+        if (lanes_of(a) == 16) return go(k_route<T, 16, 4, BIAS>);
+        if (a.E <= 256) return go(k_route<T, 64, 4, BIAS>);
+        if (a.E <= 1024) return go(k_route<T, 64, 16, BIAS>);
+        return go(k_route<T, 64, 64, BIAS>);
     }
-    if (few && a.E <= 64) return go(k_route<T, 16, 4>, 16);
-    if (few) return go(k_route<T, 16, 16>, 16);
-    if (a.E <= 1024) return go(k_route<T, 64, 16>, 64);
-    return go(k_route<T, 64, 64>, 64);
 }
 
 template <bool BWD> hipError_t typed(int type, const RouteArgs &a, hipStream_t st)
 {
-    return type == SOM_F32   ? pick<float, BWD>(a, st)
-           : type == SOM_F16 ? pick<_Float16, BWD>(a, st)
-                             : pick<__bf16, BWD>(a, st);
+    if (a.bias)
+        return type == SOM_F32   ? pick<float, BWD, true>(a, st)
+               : type == SOM_F16 ? pick<_Float16, BWD, true>(a, st)
+                                 : pick<__bf16, BWD, true>(a, st);
+    return type == SOM_F32   ? pick<float, BWD, false>(a, st)
+           : type == SOM_F16 ? pick<_Float16, BWD, false>(a, st)
+                             : pick<__bf16, BWD, false>(a, st);
 }
 
 }  // namespace

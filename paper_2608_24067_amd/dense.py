@@ -12,12 +12,29 @@ import functools
 
 import torch
 
-from .som import SomError, _check, _stream, load  # noqa: F401
+from .som import SOM_OK, SomError, load  # noqa: F401
+from .som import _check as _raise
 
 F32, F16, BF16 = 0, 1, 2
 _TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 _SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _check(status, where):
+    if status != SOM_OK:
+        _raise(status, where)
+
+
+_current = torch.cuda.current_stream
+try:  # the stream's handle without an object around it, where torch offers it
+    _handle = torch._C._cuda_getCurrentRawStream
+except AttributeError:
+    _handle = None
+
+
+def _stream(t):
+    return _handle(t.device.index) if _handle is not None else _current(t.device).cuda_stream
 
 
 class _RouteConfig(ctypes.Structure):
@@ -297,15 +314,18 @@ def clip(tensors, max_norm: float, out=None, norm=None, workspace=None):
             raise ValueError("no tensors: pass norm")
         norm = torch.empty(1, dtype=torch.float32, device=tensors[0].device)
     n, dev = len(tensors), norm.device
-    ins, tos = (ctypes.c_void_p * n)(), (ctypes.c_void_p * n)()
-    sizes, types = (ctypes.c_int64 * n)(), (ctypes.c_int32 * n)()
-    for i, (t, o) in enumerate(zip(tensors, outs)):
-        types[i] = _type(t, "tensors", halves=False)
-        if not t.is_contiguous() or t.device != dev or not t.is_cuda:
+    for t, o in zip(tensors, outs):
+        if not isinstance(t, torch.Tensor) or t.dtype not in _TYPES:
+            _type(t, "tensors", halves=False)
+        if t.device != dev or not t.is_contiguous() or not t.is_cuda:
             raise ValueError("tensors must be contiguous and on one GPU")
-        if o is not t and (o.dtype != t.dtype or o.shape != t.shape or not o.is_contiguous() or o.device != dev):
+        if o is not t and (not isinstance(o, torch.Tensor) or o.dtype != t.dtype or o.shape != t.shape
+                           or o.device != dev or not o.is_contiguous()):
             raise ValueError("out must hold contiguous tensors of the same shapes and types")
-        ins[i], tos[i], sizes[i] = t.data_ptr(), o.data_ptr(), t.numel()
+    pointers, longs, ints = ctypes.c_void_p * n, ctypes.c_int64 * n, ctypes.c_int32 * n
+    ins = pointers(*[t.data_ptr() for t in tensors])
+    tos = ins if out is None else pointers(*[o.data_ptr() for o in outs])
+    sizes, types = longs(*[t.numel() for t in tensors]), ints(*[_TYPES[t.dtype] for t in tensors])
     lib = load()
     ws = _work(workspace, lib.som_clip_workspace_bytes(sizes, n), dev)
     _check(lib.som_clip(ins, tos, sizes, types, n, float(max_norm), _vec(norm, "norm", (1,), torch.float32, dev),
