@@ -81,6 +81,12 @@ __global__ __launch_bounds__(kThreads) void k_squares(const ClipTable t, double 
     if (threadIdx.x == 0) partial[chunk] = s;
 }
 
+// The scale of a norm; an infinite or NaN norm, or one within the limit, scales nothing.
+__device__ inline float scale_of(double r, float max_norm)
+{
+    return r > (double)max_norm && r < __builtin_inf() ? (float)((double)max_norm / r) : 1.0f;
+}
+
 __global__ __launch_bounds__(1024) void k_norm(const double *__restrict__ partial, int64_t n, float max_norm,
                                                float *__restrict__ norm, float *__restrict__ scale)
 {
@@ -91,8 +97,7 @@ __global__ __launch_bounds__(1024) void k_norm(const double *__restrict__ partia
     if (threadIdx.x == 0) {
         const double r = sqrt(s);
         *norm = (float)r;
-        // an infinite or NaN norm, or one within the limit, scales nothing
-        *scale = r > (double)max_norm && r < __builtin_inf() ? (float)((double)max_norm / r) : 1.0f;
+        *scale = scale_of(r, max_norm);
     }
 }
 
@@ -117,11 +122,23 @@ template <typename T> __device__ inline void scaled(const void *in, void *out, i
     });
 }
 
-__global__ __launch_bounds__(kThreads) void k_scale(const ClipTable t, const float *__restrict__ scale)
+__global__ __launch_bounds__(kThreads) void k_scale(const ClipTable t, const float *__restrict__ scale,
+                                                    const double *__restrict__ partial, int64_t n, float max_norm,
+                                                    float *__restrict__ norm)
 {
+    __shared__ double lds[kThreads / 64];
     const int chunk = blockIdx.x, i = tensor_of(t, chunk);
     const int64_t from = (int64_t)(chunk - t.first[i]) * kClipChunk, to = min(t.size[i], from + kClipChunk);
-    const float c = *scale;
+    float c;
+    if (scale) {
+        c = *scale;
+    } else {
+        double s = 0;
+        for (int64_t j = threadIdx.x; j < n; j += kThreads) s += partial[j];
+        const double r = sqrt(block_sum(s, lds));
+        c = scale_of(r, max_norm);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)r;
+    }
     if (t.type[i] == SOM_F32) scaled<float>(t.in[i], t.out[i], from, to, c);
     else if (t.type[i] == SOM_F16) scaled<_Float16>(t.in[i], t.out[i], from, to, c);
     else scaled<__bf16>(t.in[i], t.out[i], from, to, c);
@@ -142,10 +159,12 @@ hipError_t launch_norm(const double *partial, int64_t n, float max_norm, float *
     return hipGetLastError();
 }
 
-hipError_t launch_scale(const ClipTable &t, const float *scale, hipStream_t st)
+hipError_t launch_scale(const ClipTable &t, const float *scale, const double *partial, int64_t n, float max_norm,
+                        float *norm, hipStream_t st)
 {
     if (t.first[t.count] == 0) return hipSuccess;
-    hipLaunchKernelGGL(k_scale, dim3((unsigned)t.first[t.count]), dim3(kThreads), 0, st, t, scale);
+    hipLaunchKernelGGL(k_scale, dim3((unsigned)t.first[t.count]), dim3(kThreads), 0, st, t, scale,
+                       partial, n, max_norm, norm);
     return hipGetLastError();
 }
 

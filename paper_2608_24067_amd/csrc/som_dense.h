@@ -37,6 +37,12 @@ struct Product {
     const TileRow *tiles;
     const int32_t *n_tiles;
     int32_t split;          // workgroup tiles in the height of a tile row
+    int32_t tile_height;    // rows of a tile row at most
+    // Few pairs without a plan (launch_few): pair m is a tile of its own, for expert pairs[m], its
+    // row of A is m / pair_rows and its weight pair_w[m].
+    const int32_t *pairs;
+    const void *pair_w;
+    int32_t pair_rows;
     const int32_t *off;
     int32_t groups;         // 0: not grouped
     int64_t strideB, strideBias, strideC;
@@ -132,8 +138,8 @@ hipError_t launch_pairs(bool bf16, const int32_t *idx, const void *w, int64_t P,
                         const PairPlan &plan, hipStream_t st);
 
 // out[n] = res[n] + the rows y[pos[n, j]] (fp32, D wide) in the order of j, each the sum of
-// `splits` rows N k apart.
-hipError_t launch_combine(bool bf16, const float *y, int splits, const int32_t *pos, int64_t N, int32_t k, int64_t D,
+// `splits` rows N k apart. Without a plan `pos` are the pairs' experts and a pair's row is its own.
+hipError_t launch_combine(bool bf16, const float *y, int splits, const int32_t *pos, int32_t no_plan_E, int64_t N, int32_t k, int64_t D,
                           const void *res, int64_t ldr, void *out, int64_t ldo, hipStream_t st);
 
 // dw[n, j] = the sum of parts[pos] plus <b2[idx], dout[n]>; 0 for a pair without an expert.
@@ -166,6 +172,9 @@ struct ClipTable {
 
 hipError_t launch_squares(const ClipTable &t, double *partial, hipStream_t st);
 hipError_t launch_norm(const double *partial, int64_t n, float max_norm, float *norm, float *scale, hipStream_t st);
-hipError_t launch_scale(const ClipTable &t, const float *scale, hipStream_t st);
+// scale: what launch_norm wrote; or null and the n partial sums, which every workgroup then adds
+// itself (the first also writes norm).
+hipError_t launch_scale(const ClipTable &t, const float *scale, const double *partial, int64_t n, float max_norm,
+                        float *norm, hipStream_t st);
 
 }  // namespace som

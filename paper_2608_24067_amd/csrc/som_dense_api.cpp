@@ -46,6 +46,10 @@ bool chunks(const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) 
 // Experts (and whole calls) of up to this many rows go to the kernel for few rows.
 constexpr int64_t kFewRows = 8;
 
+// Up to this many pairs are not ordered by expert first (a launch of 5 us): each reads its
+// expert's weights for itself.
+constexpr int64_t kFewPairs = 16;
+
 // The tile of a product of `rows` rows a group and `cols` columns. Large tiles read each
 // operand least often but need enough of them to fill the 256 CUs.
 som::TileSize pick_tile(int64_t rows, int64_t groups, int64_t cols, bool whole)
@@ -83,6 +87,7 @@ struct ExpertsLayout {
     size_t off, n_tiles, tiles, row, w, pos, counts, inner, y, pre, dz, parts, total;
     som::TileSize tile;
     int splits;  // of the second product's reduction (few rows)
+    bool plan;   // the pairs are ordered by expert
     int64_t n_parts;
 };
 
@@ -98,9 +103,11 @@ ExpertsLayout experts_layout(int64_t N, int32_t k, int64_t E, int64_t D, int64_t
     const int64_t P = N * k, met = P < E ? (P < 1 ? 1 : P) : E;
     L.tile = pick_tile(P / met, met, D < F ? D : F, D % 8 == 0 && F % 8 == 0);
     L.splits = 1;
-    if (!keep && P / met <= kFewRows) {
+    L.plan = true;
+    if (P / met <= kFewRows) {
         // Few rows: fill the CUs by splitting the second reduction, a step of 32 a wave at least.
         L.tile = som::kTileFew;
+        L.plan = keep || P > kFewPairs;
         const int64_t tiles = met * ((D + 127) / 128), most = (F + 255) / 256;
         while (L.splits < 16 && tiles * L.splits < 256 && L.splits * 2 <= most) L.splits *= 2;
     }
@@ -152,6 +159,12 @@ Experts carve(void *ws, const ExpertsLayout &L)
     return x;
 }
 
+// The tile of a backward product: large ones need whole chunks, and few rows have no kernel of their own.
+som::TileSize bwd_tile(som::TileSize t, bool whole)
+{
+    return t == som::kTileFew ? som::kTileSmall : t == som::kTileLarge && !whole ? som::kTileMid : t;
+}
+
 // A product over the plan's tile rows, by tiles of the plan's height or a part of it.
 struct Grouped {
     const ExpertsLayout &L;
@@ -163,7 +176,8 @@ struct Grouped {
         p.M = P;
         p.tiles = plan.tiles;
         p.n_tiles = plan.n_tiles;
-        p.split = tile_rows(L.tile) / tile_rows(t);
+        p.tile_height = tile_rows(L.tile);
+        p.split = p.tile_height > tile_rows(t) ? p.tile_height / tile_rows(t) : 1;
         p.groups = (int32_t)E;
         return p;
     }
@@ -385,7 +399,8 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool bf16 = type == SOM_BF16;
     const int64_t P = N * k;
-    hipError_t e = som::launch_pairs(bf16, idx, w, P, k, (int32_t)E, tile_rows(L.tile), x.plan, s);
+    hipError_t e = hipSuccess;
+    if (L.plan) e = som::launch_pairs(bf16, idx, w, P, k, (int32_t)E, tile_rows(L.tile), x.plan, s);
     if (e != hipSuccess) return hip_fail(e, who);
     const Grouped g{L, x.plan, P, E};
     {
@@ -398,6 +413,7 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
         p.bias = b1, p.strideBias = F, p.act = act;
         p.w = x.plan.w;
         p.out = x.inner, p.ldo = F;
+        if (!L.plan) p.pairs = idx, p.pair_w = w, p.pair_rows = k;
         if (keep) p.pre = x.pre, p.ldp = F;
         e = t == som::kTileFew ? som::launch_few(bf16, som::kInner, p, 1, s) : som::launch_nn(bf16, som::kInner, t, p, s);
         if (e != hipSuccess) return hip_fail(e, who);
@@ -411,11 +427,12 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
         p.bias = b2, p.strideBias = D;
         p.w = x.plan.w;
         p.out = x.y, p.ldo = D;
+        if (!L.plan) p.pairs = idx, p.pair_w = w, p.pair_rows = 1;
         e = t == som::kTileFew ? som::launch_few(bf16, som::kPairs, p, L.splits, s)
                                : som::launch_nn(bf16, som::kPairs, t, p, s);
         if (e != hipSuccess) return hip_fail(e, who);
     }
-    e = som::launch_combine(bf16, x.y, L.splits, x.plan.pos, N, k, D, residual, ldr, out, ldo, s);
+    e = som::launch_combine(bf16, x.y, L.splits, L.plan ? x.plan.pos : idx, L.plan ? 0 : (int32_t)E, N, k, D, residual, ldr, out, ldo, s);
     return e == hipSuccess ? ok() : hip_fail(e, who);
 }
 
@@ -449,7 +466,7 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
     }
     if (N > 0 && (dX || dw || dW1 || db1)) {  // dz, and the weights' gradients in parts
         const bool whole = chunks(W2, D) && chunks(dout, lddo);
-        const som::TileSize t = L.tile == som::kTileLarge && !whole ? som::kTileMid : L.tile;
+        const som::TileSize t = bwd_tile(L.tile, whole);
         Product p = g.product(t);
         p.A = dout, p.lda = lddo, p.amap = x.plan.row;
         p.B = W2, p.ldb = D, p.strideB = D * F;
@@ -468,7 +485,7 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
         }
     }
     if (dX && N > 0) {
-        const som::TileSize t = L.tile == som::kTileLarge && !chunks(W1, F) ? som::kTileMid : L.tile;
+        const som::TileSize t = bwd_tile(L.tile, chunks(W1, F));
         Product p = g.product(t);
         p.A = x.dz, p.lda = F;
         p.B = W1, p.ldb = F, p.strideB = D * F;
@@ -476,7 +493,7 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
         p.out = x.y, p.ldo = D;
         e = som::launch_nt(bf16, som::kPairs, t, p, s);
         if (e != hipSuccess) return hip_fail(e, who);
-        e = som::launch_combine(bf16, x.y, 1, x.plan.pos, N, k, D, nullptr, 0, dX, lddx, s);
+        e = som::launch_combine(bf16, x.y, 1, x.plan.pos, 0, N, k, D, nullptr, 0, dX, lddx, s);
         if (e != hipSuccess) return hip_fail(e, who);
     }
     if (dW1 || db1) {
@@ -542,6 +559,8 @@ som_status som_clip(const void *const *tensors, void *const *outs, const int64_t
     hipStream_t s = static_cast<hipStream_t>(stream);
     float *scale = static_cast<float *>(workspace);
     double *partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + 256);
+    // Few chunks: one launch less, each workgroup of the last pass adds them for itself.
+    const bool few = chunks_total > 0 && chunks_total <= 512 && count <= som::kClipTensors;
     for (int pass = 0; pass < 2; ++pass) {
         int64_t done = 0;
         for (int64_t i = 0; i < count; i += som::kClipTensors) {
@@ -553,11 +572,13 @@ som_status som_clip(const void *const *tensors, void *const *outs, const int64_t
                 t.size[j] = sizes[i + j], t.type[j] = types[i + j];
                 t.first[j + 1] = t.first[j] + (int32_t)((t.size[j] + som::kClipChunk - 1) / som::kClipChunk);
             }
-            const hipError_t e = pass == 0 ? som::launch_squares(t, partial + done, s) : som::launch_scale(t, scale, s);
+            const hipError_t e = pass == 0 ? som::launch_squares(t, partial + done, s)
+                                 : few     ? som::launch_scale(t, nullptr, partial, chunks_total, max_norm, norm, s)
+                                           : som::launch_scale(t, scale, nullptr, 0, max_norm, norm, s);
             if (e != hipSuccess) return hip_fail(e, who);
             done += t.first[t.count];
         }
-        if (pass == 0) {
+        if (pass == 0 && !few) {
             const hipError_t e = som::launch_norm(partial, chunks_total, max_norm, norm, scale, s);
             if (e != hipSuccess) return hip_fail(e, who);
         }

@@ -167,8 +167,7 @@ __global__ __launch_bounds__(64) void k_pairs_place(const int32_t *__restrict__ 
 
 template <typename T, bool SPLIT>
 __global__ __launch_bounds__(256) void k_combine(const float *__restrict__ y, int splits,
-                                                 const int32_t *__restrict__ pos,
-                                                 int64_t N, int k, int64_t D, const T *__restrict__ res, int64_t ldr,
+                                                 const int32_t *__restrict__ pos, int no_plan_E, int64_t N, int k, int64_t D, const T *__restrict__ res, int64_t ldr,
                                                  T *out, int64_t ldo)
 {
     const int64_t per = (D + 3) / 4, total = N * per;
@@ -178,7 +177,8 @@ __global__ __launch_bounds__(256) void k_combine(const float *__restrict__ y, in
         float s[4] = {0, 0, 0, 0};
         if (res) load4(res + n * ldr + d, cnt, s);
         for (int j = 0; j < k; ++j) {
-            const int p = pos[n * k + j];
+            int p = pos[n * k + j];
+            if (no_plan_E) p = (unsigned)p < (unsigned)no_plan_E ? (int)(n * k + j) : -1;
             if (p < 0) continue;
             float v[4];
             load4(y + (int64_t)p * D + d, cnt, v);
@@ -314,12 +314,12 @@ hipError_t launch_pairs(bool bf16, const int32_t *idx, const void *w, int64_t P,
                 : with(&k_pairs<_Float16>, &k_pairs_place<_Float16>, static_cast<const _Float16 *>(w));
 }
 
-hipError_t launch_combine(bool bf16, const float *y, int splits, const int32_t *pos, int64_t N, int32_t k, int64_t D,
+hipError_t launch_combine(bool bf16, const float *y, int splits, const int32_t *pos, int32_t no_plan_E, int64_t N, int32_t k, int64_t D,
                           const void *res, int64_t ldr, void *out, int64_t ldo, hipStream_t st)
 {
     const unsigned grid = spread((N * ((D + 3) / 4) + 255) / 256);
     auto with = [&](auto kernel, const auto *r, auto *o) {
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, y, splits, pos, N, k, D, r, ldr, o, ldo);
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, y, splits, pos, no_plan_E, N, k, D, r, ldr, o, ldo);
         return hipGetLastError();
     };
     if (bf16) {

@@ -54,12 +54,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
     typedef typename Vec8<T>::type Frag;
     __shared__ __align__(16) float lds[kWaves][kRows][kCols + 4];
     const int nn = (int)((p.N + kCols - 1) / kCols);
-    const int nm = p.groups ? *p.n_tiles : (int)((p.M + kRows - 1) / kRows);
+    const int nm = p.pairs ? (int)p.M : p.groups ? *p.n_tiles : (int)((p.M + kRows - 1) / kRows);
     const int64_t t = blockIdx.x;
     if (t >= (int64_t)nm * nn * splits) return;
     const int split = (int)(t % splits), nt = (int)(t / splits % nn), mt = (int)(t / splits / nn);
     int e = 0, m0 = mt * kRows, m1 = min((int)p.M, m0 + kRows);
-    if (p.groups) {
+    if (p.pairs) {
+        e = p.pairs[mt];
+        if ((unsigned)e >= (unsigned)p.groups) return;
+        m0 = mt;
+        m1 = mt + 1;
+    } else if (p.groups) {
         const TileRow r = p.tiles[mt];
         e = r.e;
         m0 = r.row;
@@ -73,7 +78,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
     const int s0 = (int)((int64_t)steps * own / parts), s1 = (int)((int64_t)steps * (own + 1) / parts);
 
     const int row = min(m0 + c, m1 - 1);
-    const short *a = static_cast<const short *>(p.A) + (p.amap ? (int64_t)p.amap[row] : (int64_t)row) * p.lda + 8 * g;
+    const int64_t at = p.pairs ? row / p.pair_rows : p.amap ? p.amap[row] : row;
+    const short *a = static_cast<const short *>(p.A) + at * p.lda + 8 * g;
     const int col = nt * kCols + 8 * c, cols = min(8, N - col);
     const short *b = static_cast<const short *>(p.B) + (int64_t)e * p.strideB + 8 * (int64_t)g * p.ldb + (cols > 0 ? col : 0);
 
@@ -136,7 +142,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) sum += *reinterpret_cast<const f32x4 *>(&lds[w][r][q4]);
         float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-        const float wr = EPI != kLinear && p.w ? p.w[m] : 1.0f;
+        const float wr = EPI == kLinear ? 1.0f : p.pairs ? (float)static_cast<const T *>(p.pair_w)[m] : p.w[m];
         if (p.bias && split == 0) {
             float bias[4];
             if (p.bias_f32) load4(static_cast<const float *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
@@ -168,7 +174,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
 
 template <typename T> hipError_t go(Epilogue e, const Product &p, int splits, hipStream_t st)
 {
-    const int64_t rows = p.groups ? max_tile_rows(p.M, p.groups, kRows) : (p.M + kRows - 1) / kRows;
+    const int64_t rows = p.pairs    ? p.M
+                         : p.groups ? max_tile_rows(p.M, p.groups, kRows)
+                                    : (p.M + kRows - 1) / kRows;
     const int64_t grid = rows * ((p.N + kCols - 1) / kCols) * splits;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
     auto with = [&](auto kernel, int waves) {

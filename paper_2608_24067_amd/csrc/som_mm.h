@@ -316,8 +316,9 @@ template <typename T, int BR, bool ACROSS> struct Reader {
     }
 };
 
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int PER_CU_> struct Shape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, PER_CU = PER_CU_;
+// STAGES: tiles' places in LDS (loads straight there); AHEAD: tiles in registers (loads through them).
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int AHEAD_, int PER_CU_> struct Shape {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, AHEAD = AHEAD_, PER_CU = PER_CU_;
     static constexpr int NT = 64 * WM * WN;
     static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
 };
@@ -403,7 +404,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
             const TileRow r = p.tiles[mt / p.split];
             e = r.e;
             m0 = r.row + mt % p.split * S::BM;
-            m1 = r.end;
+            m1 = min(r.end, r.row + p.tile_height);
             if (m0 >= m1) return;
         }
         K = (int)p.K;
@@ -553,7 +554,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // nothing lands in LDS after the workgroup left it
     } else {
         // Tiles go through registers, kAhead of them in flight, into two places of LDS.
-        constexpr int kAhead = 3;
+        constexpr int kAhead = S::AHEAD;
         s16x8 va[kAhead][LoadA::kPer], vb[kAhead][LoadB::kPer];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -821,9 +822,11 @@ hipError_t launch(const Product &p, int64_t tile_rows_total, hipStream_t st)
     return hipGetLastError();
 }
 
-typedef Shape<32, 128, 1, 4, 4, 4> Small;
-typedef Shape<128, 128, 2, 2, 4, 2> Mid;
-typedef Shape<256, 256, 2, 4, 4, 1> Large;
+// Small tiles are for few rows, of which there are seldom more than one a CU: they keep more
+// tiles in flight.
+typedef Shape<32, 128, 1, 4, 8, 6, 2> Small;
+typedef Shape<128, 128, 2, 2, 4, 3, 2> Mid;
+typedef Shape<256, 256, 2, 4, 4, 3, 1> Large;
 
 }  // namespace mm
 }  // namespace som

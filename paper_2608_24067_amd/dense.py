@@ -314,18 +314,24 @@ def clip(tensors, max_norm: float, out=None, norm=None, workspace=None):
             raise ValueError("no tensors: pass norm")
         norm = torch.empty(1, dtype=torch.float32, device=tensors[0].device)
     n, dev = len(tensors), norm.device
-    for t, o in zip(tensors, outs):
-        if not isinstance(t, torch.Tensor) or t.dtype not in _TYPES:
+    types, lengths = [], []
+    for t in tensors:
+        kind = _TYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+        if kind is None:
             _type(t, "tensors", halves=False)
-        if t.device != dev or not t.is_contiguous() or not t.is_cuda:
+        if t.device != dev or not t.is_contiguous():
             raise ValueError("tensors must be contiguous and on one GPU")
-        if o is not t and (not isinstance(o, torch.Tensor) or o.dtype != t.dtype or o.shape != t.shape
-                           or o.device != dev or not o.is_contiguous()):
-            raise ValueError("out must hold contiguous tensors of the same shapes and types")
-    pointers, longs, ints = ctypes.c_void_p * n, ctypes.c_int64 * n, ctypes.c_int32 * n
+        types.append(kind)
+        lengths.append(t.numel())
+    if out is not None:
+        for o, t, m in zip(outs, tensors, lengths):
+            if (not isinstance(o, torch.Tensor) or o.dtype != t.dtype or o.numel() != m or o.device != dev
+                    or not o.is_contiguous()):
+                raise ValueError("out must hold contiguous tensors of the same sizes and types")
+    pointers = ctypes.c_void_p * n
     ins = pointers(*[t.data_ptr() for t in tensors])
     tos = ins if out is None else pointers(*[o.data_ptr() for o in outs])
-    sizes, types = longs(*[t.numel() for t in tensors]), ints(*[_TYPES[t.dtype] for t in tensors])
+    sizes, types = (ctypes.c_int64 * n)(*lengths), (ctypes.c_int32 * n)(*types)
     lib = load()
     ws = _work(workspace, lib.som_clip_workspace_bytes(sizes, n), dev)
     _check(lib.som_clip(ins, tos, sizes, types, n, float(max_norm), _vec(norm, "norm", (1,), torch.float32, dev),
