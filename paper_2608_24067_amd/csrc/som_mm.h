@@ -175,7 +175,7 @@ template <typename T, int BR, bool ACROSS, bool MAPPED, int NT> struct Loader {
         if (MAPPED) map = (Scalar)(rows + k0);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int c = i * NT + (int)threadIdx.x;
+            const int c = (i * NT + (int)threadIdx.x) % kChunks;  // threads without a chunk repeat others'
             const int row = c / kRowChunks, s = c % kRowChunks;
             if (ACROSS) {
                 int col = r0 + 8 * (s ^ (unit_xor<BR>(row) << 1));
@@ -231,7 +231,7 @@ template <typename T, int BR, bool ACROSS, bool MAPPED, int NT> struct Loader {
     }
 
     // Whether all chunks' rows (columns) are inside; the same for every thread of the workgroup.
-    __device__ static bool covers(int r0, int r1) { return kChunks % NT == 0 && (!ACROSS || r0 + BR <= r1); }
+    __device__ static bool covers(int r0, int r1) { return !ACROSS || r0 + BR <= r1; }
 
     // Chunk i of the next tile, straight to LDS; INSIDE: the tile ends within the operand. The
     // instruction is written out because the compiler waits for every such load of its own before
