@@ -146,6 +146,8 @@ template <int BR> __device__ inline int unit_xor(int k)
     return 0;
 }
 
+enum Fetch { kPlain, kClamped, kChecked };
+
 // One operand's tile of kBK steps by BR rows (along) or columns (across), loaded by NT threads,
 // tile after tile. A chunk past the last row (column) is read from inside the operand instead:
 // it only reaches results that are not written. A chunk past the last step must be zero.
@@ -230,8 +232,8 @@ template <typename T, int BR, bool ACROSS, bool MAPPED, int NT> struct Loader {
         look_up();
     }
 
-    // Whether all chunks' rows (columns) are inside; the same for every thread of the workgroup.
-    __device__ static bool covers(int r0, int r1) { return !ACROSS || r0 + BR <= r1; }
+    // Whether every chunk can be loaded without a check (kClamped); the same for every thread.
+    __device__ bool covers(int r0, int r1) const { return ACROSS ? r0 + BR <= r1 : K >= 8; }
 
     // Chunk i of the next tile, straight to LDS; INSIDE: the tile ends within the operand. The
     // instruction is written out because the compiler waits for every such load of its own before
@@ -249,37 +251,61 @@ template <typename T, int BR, bool ACROSS, bool MAPPED, int NT> struct Loader {
                      : "memory");
     }
 
-    // The next tile, into registers. INSIDE: all of it lies within the operand; the loads are then
-    // unconditional, so that the compiler can count them and waits for no more than it needs.
-    template <bool INSIDE> __device__ void fetch(s16x8 *r)
+    // The next tile, into registers. Where the loads are unconditional the compiler counts them and
+    // waits for no more than it needs: kPlain for a tile within the operand; kClamped for any
+    // tile, a chunk past the end is read from the last whole one before it (put sets that right);
+    // kChecked reads value by value at the edges.
+    template <Fetch HOW> __device__ void fetch(s16x8 *r)
     {
         typedef s16x8 any __attribute__((aligned(2)));
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            if (INSIDE) {
-                r[i] = *reinterpret_cast<const any *>(source(i));
-                continue;
-            }
-            r[i] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
-            if (!mine(i)) continue;
-            const int left = K - t - k[i], n = ACROSS ? (left > 0 ? cnt[i] : 0) : min(8, left);
             const short *src = reinterpret_cast<const short *>(source(i));
-            if (n >= 8) {
+            const int left = K - t - k[i];
+            if (HOW == kPlain) {
                 r[i] = *reinterpret_cast<const any *>(src);
-            } else if (n > 0) {
+            } else if (HOW == kClamped) {
+                if (!ACROSS) src += min(0, left - 8);
+                else if (!MAPPED) src += min(0, left - 1) * ld;
+                r[i] = *reinterpret_cast<const any *>(src);
+            } else {
+                r[i] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                if (!mine(i)) continue;
+                const int n = ACROSS ? (left > 0 ? cnt[i] : 0) : min(8, left);
+                if (n >= 8) {
+                    r[i] = *reinterpret_cast<const any *>(src);
+                } else if (n > 0) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < n) r[i][j] = src[j];
+                    for (int j = 0; j < 8; ++j)
+                        if (j < n) r[i][j] = src[j];
+                }
             }
         }
         advance();
     }
 
-    __device__ static void put(char *lds, const s16x8 *r)
+    // Tile `tile` from registers to LDS. CLAMPED: the values past the end are shifted out.
+    template <bool CLAMPED> __device__ void put(int tile, char *lds, const s16x8 *r) const
     {
+        const bool ends = CLAMPED && (tile + 1) * kBK > K;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (mine(i)) *reinterpret_cast<s16x8 *>(lds + (i * NT + (int)threadIdx.x) * 16) = r[i];
+        for (int i = 0; i < kPer; ++i) {
+            s16x8 v = r[i];
+            if (ends) {
+                typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
+                u64x2 x = __builtin_bit_cast(u64x2, v);
+                const int left = K - tile * kBK - k[i];
+                if (ACROSS) {
+                    if (left <= 0) x = u64x2{0, 0};
+                } else if (left < 8) {
+                    const int s = 16 * min(8, 8 - left);  // bits, 16 to 128
+                    const unsigned long long lo = s < 64 ? x[0] >> s | x[1] << (64 - s) : s < 128 ? x[1] >> (s - 64) : 0;
+                    x = u64x2{lo, s < 64 ? x[1] >> s : 0};
+                }
+                v = __builtin_bit_cast(s16x8, x);
+            }
+            if (mine(i)) *reinterpret_cast<s16x8 *>(lds + (i * NT + (int)threadIdx.x) * 16) = v;
+        }
     }
 };
 
@@ -355,6 +381,10 @@ enum Layout { kNN, kNT, kTN };
 
 template <bool V> struct Inside {
     static constexpr bool value = V;
+};
+
+template <Fetch V> struct How {
+    static constexpr Fetch value = V;
 };
 
 // Which operand of a product over rows (TN) goes through a map of its rows.
@@ -556,19 +586,16 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
         // Tiles go through registers, kAhead of them in flight, into two places of LDS.
         constexpr int kAhead = S::AHEAD;
         s16x8 va[kAhead][LoadA::kPer], vb[kAhead][LoadB::kPer];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            la.template fetch<false>(va[i]);
-            lb.template fetch<false>(vb[i]);
-        }
-        auto step = [&](int t, int i, auto inside) {
-            constexpr bool kInside = decltype(inside)::value;
+        auto fetch = [&](int i, auto how) {
+            la.template fetch<decltype(how)::value>(va[i]);
+            lb.template fetch<decltype(how)::value>(vb[i]);
+        };
+        auto step = [&](int t, int i, auto how, auto ends) {
             char *at = lds + (t % 2) * kStage;
-            LoadA::put(at, va[i]);
-            LoadB::put(at + LoadA::kBytes, vb[i]);
+            la.template put<decltype(ends)::value>(t, at, va[i]);
+            lb.template put<decltype(ends)::value>(t, at + LoadA::kBytes, vb[i]);
             __syncthreads();
-            la.template fetch<kInside>(va[i]);
-            lb.template fetch<kInside>(vb[i]);
+            fetch(i, how);
             FragsB b;
             const uint32_t from = base + (uint32_t)(t % 2) * kStage;
 #pragma unroll
@@ -578,15 +605,24 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
             if (L == kTN && sums) add_sums(t, b);
         };
         int t = 0;
-        if (LoadA::covers(m0, m1) && LoadB::covers(n0, (int)p.N))
+        if (steps > 0 && la.covers(m0, m1) && lb.covers(n0, (int)p.N)) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) fetch(i, How<kClamped>());
             for (; (t + 2 * kAhead) * kBK <= K; t += kAhead) {
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) step(t + i, i, Inside<true>());
+                for (int i = 0; i < kAhead; ++i) step(t + i, i, How<kPlain>(), Inside<false>());
             }
-        for (; t < steps; t += kAhead) {
+            for (; t < steps; t += kAhead) {  // past the last tile they multiply zeros
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (t + i < steps) step(t + i, i, Inside<false>());
+                for (int i = 0; i < kAhead; ++i) step(t + i, i, How<kClamped>(), Inside<true>());
+            }
+        } else if (steps > 0) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) fetch(i, How<kChecked>());
+            for (; t < steps; t += kAhead) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) step(t + i, i, How<kChecked>(), Inside<false>());
+            }
         }
     }
 
