@@ -125,12 +125,12 @@ struct PairPlan {
 };
 
 // Up to this many pairs are ordered by one workgroup (2,048 pairs: one launch of about 8 us
-// against three of 4); more in stretches of 512 pairs, at most 256 of them.
+// against three of 4); more in stretches of 256 pairs, at most 256 of them.
 constexpr int64_t kPairsOfOne = 2048;
 inline int pair_stretches(int64_t P)
 {
     if (P <= kPairsOfOne) return 0;
-    const int64_t n = (P + 511) / 512;
+    const int64_t n = (P + 255) / 256;
     return (int)(n < 256 ? n : 256);
 }
 

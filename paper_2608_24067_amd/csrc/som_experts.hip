@@ -15,20 +15,24 @@ using mm::store4;
 // order is the pairs' own within an expert, so sums over it are the same on every run. Few pairs
 // take one workgroup for all three (16 stretches at most); more take a kernel each.
 
-// A stretch's pairs to count[e]; its indexes are loaded eight chunks at a time.
-template <typename F> __device__ inline void chunks_of(const int32_t *idx, int64_t first, int64_t last, int E, F f)
+// f(pair, expert or -1, weight) for a stretch, 64 pairs at a time; what is read of them is loaded
+// eight times 64 at a time. w may be null.
+template <typename T, typename F>
+__device__ inline void chunks_of(const int32_t *idx, const T *w, int64_t first, int64_t last, int E, F f)
 {
     const int lane = threadIdx.x % 64;
     for (int64_t i0 = first; i0 < last; i0 += 512) {
         int x[8];
+        T v[8];
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
             const int64_t i = i0 + c * 64 + lane;
             x[c] = i < last ? idx[i] : -1;
+            v[c] = w && i < last ? w[i] : (T)0.0f;
         }
 #pragma unroll
         for (int c = 0; c < 8; ++c)
-            if (i0 + c * 64 < last) f(i0 + c * 64 + lane, (unsigned)x[c] < (unsigned)E ? x[c] : -1);
+            if (i0 + c * 64 < last) f(i0 + c * 64 + lane, (unsigned)x[c] < (unsigned)E ? x[c] : -1, v[c]);
     }
 }
 
@@ -66,7 +70,7 @@ __device__ inline void place(const int32_t *idx, const T *w, int64_t first, int6
                              volatile int *next, const PairPlan &plan)
 {
     const int lane = threadIdx.x % 64;
-    chunks_of(idx, first, last, E, [&](int64_t i, int x) {
+    chunks_of(idx, w, first, last, E, [&](int64_t i, int x, T weight) {
         const bool ok = x >= 0;
         unsigned long long same = __ballot(ok);
         for (int bit = 0; 1 << bit < E; ++bit) {
@@ -82,8 +86,8 @@ __device__ inline void place(const int32_t *idx, const T *w, int64_t first, int6
             const int p = ok ? base + before : -1;
             plan.pos[i] = p;
             if (ok) {
-                plan.row[p] = (int)(i / k);
-                plan.w[p] = (float)w[i];
+                plan.row[p] = (int)i / k;  // fewer than 2^30 pairs
+                plan.w[p] = (float)weight;
             }
         }
     });
@@ -101,7 +105,7 @@ __global__ __launch_bounds__(1024) void k_pairs(const int32_t *__restrict__ idx,
     for (int i = threadIdx.x; i < waves * E; i += blockDim.x) count[i] = 0;
     __syncthreads();
     const int64_t first = wave * stretch_of(P, waves), last = min(P, first + stretch_of(P, waves));
-    chunks_of(idx, first, last, E, [&](int64_t, int x) {
+    chunks_of(idx, (const T *)nullptr, first, last, E, [&](int64_t, int x, T) {
         if (x >= 0) atomicAdd(&count[wave * E + x], 1);
     });
     __syncthreads();
@@ -126,7 +130,7 @@ __global__ __launch_bounds__(64) void k_pairs_count(const int32_t *__restrict__ 
     for (int i = threadIdx.x; i < E; i += 64) lds[i] = 0;
     __syncthreads();
     const int64_t len = stretch_of(P, gridDim.x), first = blockIdx.x * len, last = min(P, first + len);
-    chunks_of(idx, first, last, E, [&](int64_t, int x) {
+    chunks_of(idx, (const float *)nullptr, first, last, E, [&](int64_t, int x, float) {
         if (x >= 0) atomicAdd(&lds[x], 1);
     });
     __syncthreads();

@@ -6,7 +6,9 @@
 // values about in registers into eight operands of v_mfma_f32_16x16x32: operand j holds column
 // 8c + j of every lane. The matrix goes from memory to registers with no LDS and no barrier in
 // between, kDeep steps (32 KB a wave) in flight. The waves' sums meet in LDS, added in the waves'
-// order. Rows past the tile repeat its last one; features past the end count as zeros.
+// order. Rows past the tile repeat its last one; columns past the end are read again from inside
+// (the last tile is moved back to end with the matrix, or the last lanes' columns are); features
+// past the end count as zeros.
 //
 // Where the tiles are fewer than the CUs the reduction is also split over workgroups, whose
 // results (kPairs only) are added by the kernel that combines a row's pairs.
@@ -80,8 +82,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
     const int row = min(m0 + c, m1 - 1);
     const int64_t at = p.pairs ? row / p.pair_rows : p.amap ? p.amap[row] : row;
     const short *a = static_cast<const short *>(p.A) + at * p.lda + 8 * g;
-    const int col = nt * kCols + 8 * c, cols = min(8, N - col);
-    const short *b = static_cast<const short *>(p.B) + (int64_t)e * p.strideB + 8 * (int64_t)g * p.ldb + (cols > 0 ? col : 0);
+    const int n_from = nt * kCols, n0 = N >= kCols ? min(n_from, N - kCols) : 0;
+    const int last = N - n0 - 8;  // where the last lane's eight columns start (negative: fewer than 8 in all)
+    const int cols = min(8, N - n0 - 8 * c);
+    const short *b = static_cast<const short *>(p.B) + (int64_t)e * p.strideB + 8 * (int64_t)g * p.ldb + n0 +
+                     (last >= 0 ? min(8 * c, last) : cols > 0 ? 8 * c : 0);
 
     f32x4 acc[8];
 #pragma unroll
@@ -94,8 +99,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
             acc[j] = mma(__builtin_bit_cast(Frag, f[j]), __builtin_bit_cast(Frag, va), acc[j]);
     };
     int s = s0;
-    if (nt * kCols + kCols <= N) {
-        typedef s16x8 any __attribute__((aligned(2)));
+    typedef s16x8 any __attribute__((aligned(2)));
+    if (last >= 0 && K >= 8) {
         const int whole = min(s1, K / 32);  // steps with all their features
         for (; s + kDeep <= whole; s += kDeep) {
             s16x8 va[kDeep], vb[kDeep][8];
@@ -109,18 +114,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
 #pragma unroll
             for (int d = 0; d < kDeep; ++d) multiply(va[d], vb[d]);
         }
-        for (; s < whole; ++s) {
+        for (; s < s1; ++s) {
             const int64_t k = (int64_t)s * 32;
-            s16x8 vb[8];
+            const int left = K - s * 32 - 8 * g;  // features of the lane's eight
+            s16x8 va = *reinterpret_cast<const any *>(a + k + min(0, left - 8)), vb[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) vb[q] = *reinterpret_cast<const any *>(b + (k + q) * p.ldb);
-            const s16x8 va = *reinterpret_cast<const any *>(a + k);
+            for (int q = 0; q < 8; ++q) vb[q] = *reinterpret_cast<const any *>(b + (k + min(q, left - 1)) * p.ldb);
+            if (left < 8) {
+                va = shift_out(va, left);
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (q >= left) vb[q] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+            }
             multiply(va, vb);
         }
     }
-    for (; s < s1; ++s) {
+    for (; s < s1; ++s) {  // fewer than eight columns or features
         const int64_t k = (int64_t)s * 32;
-        const int left = K - s * 32 - 8 * g;  // features of the lane's eight
+        const int left = K - s * 32 - 8 * g;
         s16x8 vb[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) vb[q] = load8(b + (k + q) * p.ldb, q < left ? cols : 0);
@@ -128,15 +139,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
     }
 
     // Lane (m, g) has columns (4g + i) 8 + j of row m in acc[j][i].
+    if (n0 + kCols <= N) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            *reinterpret_cast<f32x4 *>(&lds[wave][c][(4 * g + i) * 8 + 4 * h]) =
-                f32x4{acc[4 * h][i], acc[4 * h + 1][i], acc[4 * h + 2][i], acc[4 * h + 3][i]};
+            for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<f32x4 *>(&lds[wave][c][(4 * g + i) * 8 + 4 * h]) =
+                    f32x4{acc[4 * h][i], acc[4 * h + 1][i], acc[4 * h + 2][i], acc[4 * h + 3][i]};
+    } else {  // lanes moved back leave the same sums in the same places
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                lds[wave][c][(last >= 0 ? min((4 * g + i) * 8, last) : (4 * g + i) * 8) + j] = acc[j][i];
+    }
     __syncthreads();
-    const int q4 = threadIdx.x % (kCols / 4) * 4, n = nt * kCols + q4, cnt = min(4, N - n);
-    for (int r = threadIdx.x / (kCols / 4); r < m1 - m0 && cnt > 0; r += 2 * kWaves) {
+    const int q4 = threadIdx.x % (kCols / 4) * 4, n = n0 + q4, cnt = min(4, N - n);
+    const int skip = max(0, n_from - n);  // of the four, columns that the tile before writes
+    for (int r = threadIdx.x / (kCols / 4); r < m1 - m0 && cnt > skip; r += 2 * kWaves) {
         const int m = m0 + r;
         f32x4 sum = *reinterpret_cast<const f32x4 *>(&lds[0][r][q4]);
 #pragma unroll
@@ -151,10 +171,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
             for (int q = 0; q < 4; ++q) v[q] += EPI == kPairs ? wr * bias[q] : bias[q];
         }
         if (EPI == kPairs) {
-            store4(static_cast<float *>(p.out) + ((int64_t)split * p.M + m) * p.ldo + n, cnt, v);
+            store4(static_cast<float *>(p.out) + ((int64_t)split * p.M + m) * p.ldo + n, skip, cnt, v);
             continue;
         }
-        if (p.pre) store4(static_cast<T *>(p.pre) + (int64_t)m * p.ldp + n, cnt, v);
+        if (p.pre) store4(static_cast<T *>(p.pre) + (int64_t)m * p.ldp + n, skip, cnt, v);
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = act_value(p.act, v[q]);
         if (EPI == kInner) {
@@ -167,8 +187,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] += t4[q];
         }
-        if (EPI == kLinear && p.out_f32) store4(static_cast<float *>(p.out) + (int64_t)m * p.ldo + n, cnt, v);
-        else store4(static_cast<T *>(p.out) + (int64_t)m * p.ldo + n, cnt, v);
+        if (EPI == kLinear && p.out_f32) store4(static_cast<float *>(p.out) + (int64_t)m * p.ldo + n, skip, cnt, v);
+        else store4(static_cast<T *>(p.out) + (int64_t)m * p.ldo + n, skip, cnt, v);
     }
 }
 

@@ -146,6 +146,16 @@ template <int BR> __device__ inline int unit_xor(int k)
     return 0;
 }
 
+// Values whose last `left` (below 8) are wanted, moved to the front, zeros after them.
+__device__ inline s16x8 shift_out(const s16x8 &v, int left)
+{
+    typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
+    u64x2 x = __builtin_bit_cast(u64x2, v);
+    const int s = 16 * min(8, 8 - left);  // bits, 16 to 128
+    const unsigned long long lo = s < 64 ? x[0] >> s | x[1] << (64 - s) : s < 128 ? x[1] >> (s - 64) : 0;
+    return __builtin_bit_cast(s16x8, u64x2{lo, s < 64 ? x[1] >> s : 0});
+}
+
 enum Fetch { kPlain, kClamped, kChecked };
 
 // One operand's tile of kBK steps by BR rows (along) or columns (across), loaded by NT threads,
@@ -292,17 +302,12 @@ template <typename T, int BR, bool ACROSS, bool MAPPED, int NT> struct Loader {
         for (int i = 0; i < kPer; ++i) {
             s16x8 v = r[i];
             if (ends) {
-                typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
-                u64x2 x = __builtin_bit_cast(u64x2, v);
                 const int left = K - tile * kBK - k[i];
                 if (ACROSS) {
-                    if (left <= 0) x = u64x2{0, 0};
+                    if (left <= 0) v = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
                 } else if (left < 8) {
-                    const int s = 16 * min(8, 8 - left);  // bits, 16 to 128
-                    const unsigned long long lo = s < 64 ? x[0] >> s | x[1] << (64 - s) : s < 128 ? x[1] >> (s - 64) : 0;
-                    x = u64x2{lo, s < 64 ? x[1] >> s : 0};
+                    v = shift_out(v, left);
                 }
-                v = __builtin_bit_cast(s16x8, x);
             }
             if (mine(i)) *reinterpret_cast<s16x8 *>(lds + (i * NT + (int)threadIdx.x) * 16) = v;
         }

@@ -449,8 +449,10 @@ hipError_t launch_route(int logit_type, const RouteArgs &a, hipStream_t st)
     }
     const hipError_t e = typed<false>(logit_type, a, st);
     if (e != hipSuccess || !a.counts || a.N <= rows_of_one(a)) return e;
-    const int64_t n = a.N * a.k, blocks = (n + 8191) / 8192;
-    hipLaunchKernelGGL(k_counts, dim3((unsigned)(blocks < 32 ? blocks : 32)), dim3(1024), 0, st, a.idx, n, a.E, a.counts);
+    // as many workgroups as the choices fill, while those add at most 8,192 counts of a cache line's 16
+    const int64_t n = a.N * a.k, most = a.E < 256 ? 8192 / a.E < 128 ? 8192 / a.E : 128 : 32;
+    const int64_t blocks = (n + 8191) / 8192 < most ? (n + 8191) / 8192 : most;
+    hipLaunchKernelGGL(k_counts, dim3((unsigned)blocks), dim3(1024), 0, st, a.idx, n, a.E, a.counts);
     return hipGetLastError();
 }
 
