@@ -52,7 +52,7 @@ typedef enum { SOM_SCORE_SOFTMAX = 0, SOM_SCORE_SIGMOID = 1 } som_score;
  *   Y         device [N, M], ldy >= M, written; y_type is `type`, or SOM_F32 for scores.
  *   pre       device [N, M], ldp >= M, written, or NULL: X W + bias, rounded to `type`, which the
  *             backward pass of an activation needs.
- * N >= 0, 1 <= K, M < 2^31. N == 0 is a no-op.
+ * 0 <= N < 2^30, 1 <= K, M < 2^30. N == 0 is a no-op.
  */
 som_status som_linear(int32_t type, const void *X, int64_t ldx, const void *W, int64_t ldw, const void *bias,
                       int32_t bias_type, int32_t act, const void *residual, int64_t ldr, void *Y, int64_t ldy,
@@ -104,7 +104,7 @@ typedef struct {
  * A unit is closed to a row whose logit, or logit + bias, is NaN or minus infinity: it is not
  * taken and has no share in the softmax. Plus infinity counts as the largest fp32 value. Where fewer
  * than k units are open the last places hold index -1 and weight 0.
- * N >= 0; 1 <= E <= SOM_ROUTE_MAX_UNITS; 1 <= k <= min(E, SOM_ROUTE_MAX_TAKEN).
+ * 0 <= N < 2^30; 1 <= E <= SOM_ROUTE_MAX_UNITS; 1 <= k <= min(E, SOM_ROUTE_MAX_TAKEN).
  */
 som_status som_route(int32_t logit_type, const void *logits, int64_t ldl, const float *bias, int64_t N, int64_t E,
                      int32_t k, const som_route_config *config, int32_t *idx, int32_t weight_type, void *weights,

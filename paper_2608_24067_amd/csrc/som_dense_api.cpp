@@ -38,7 +38,8 @@ som_status check_workspace(const char *who, const void *ws, size_t bytes, size_t
     return SOM_OK;
 }
 
-bool dim_ok(int64_t v) { return v >= 1 && v < INT32_MAX; }
+constexpr int64_t kMostDim = (int64_t)1 << 30;  // kernels number rows and columns in 32 bits, past the end too
+bool dim_ok(int64_t v) { return v >= 1 && v < kMostDim; }
 
 // Whether an operand's rows can be moved in whole 16-byte chunks.
 bool chunks(const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0; }
@@ -193,7 +194,7 @@ som_status som_linear(int32_t type, const void *X, int64_t ldx, const void *W, i
 {
     const char *who = "som_linear";
     if (!half_type(type)) return bad(who, "type must be SOM_F16 or SOM_BF16");
-    if (N < 0 || N >= INT32_MAX || !dim_ok(K) || !dim_ok(M)) return bad(who, "need 0 <= N, 1 <= K, M, all below 2^31 - 1");
+    if (N < 0 || N >= kMostDim || !dim_ok(K) || !dim_ok(M)) return bad(who, "need 0 <= N, 1 <= K, M, all below 2^30");
     if (!act_ok(act)) return bad(who, "unknown activation");
     if (y_type != SOM_F32 && y_type != type) return bad(who, "y_type must be SOM_F32 or type");
     if (bias && bias_type != SOM_F32 && bias_type != type) return bad(who, "bias_type must be SOM_F32 or type");
@@ -228,7 +229,7 @@ static size_t slope_bytes(int64_t N, int64_t M, int32_t act)
 
 size_t som_linear_bwd_workspace_bytes(int64_t N, int64_t K, int64_t M, int32_t act)
 {
-    if (N < 0 || N >= INT32_MAX || !dim_ok(K) || !dim_ok(M) || !act_ok(act)) return 0;
+    if (N < 0 || N >= kMostDim || !dim_ok(K) || !dim_ok(M) || !act_ok(act)) return 0;
     const int parts = grad_parts(N, K, M);
     return slope_bytes(N, M, act) + (parts > 1 ? align256((size_t)parts * (size_t)(K + 1) * (size_t)M * 4) : 0);
 }
@@ -240,7 +241,7 @@ som_status som_linear_bwd(int32_t type, const void *X, int64_t ldx, const void *
 {
     const char *who = "som_linear_bwd";
     if (!half_type(type)) return bad(who, "type must be SOM_F16 or SOM_BF16");
-    if (N < 0 || N >= INT32_MAX || !dim_ok(K) || !dim_ok(M)) return bad(who, "need 0 <= N, 1 <= K, M, all below 2^31 - 1");
+    if (N < 0 || N >= kMostDim || !dim_ok(K) || !dim_ok(M)) return bad(who, "need 0 <= N, 1 <= K, M, all below 2^30");
     if (!act_ok(act)) return bad(who, "unknown activation");
     if (dbias && bias_type != SOM_F32 && bias_type != type) return bad(who, "bias_type must be SOM_F32 or type");
     const bool slope = act != SOM_ACT_NONE;
@@ -303,7 +304,7 @@ static som_status check_route(const char *who, int32_t logit_type, const void *l
                               int32_t weight_type, const void *weights, som::RouteArgs *a)
 {
     if (!any_type(logit_type) || !any_type(weight_type)) return bad(who, "unknown type");
-    if (N < 0 || N >= INT32_MAX) return bad(who, "need 0 <= N < 2^31 - 1");
+    if (N < 0 || N >= kMostDim) return bad(who, "need 0 <= N < 2^30");
     if (E < 1 || E > SOM_ROUTE_MAX_UNITS) return bad(who, "need 1 <= E <= SOM_ROUTE_MAX_UNITS");
     if (k < 1 || k > SOM_ROUTE_MAX_TAKEN || k > E) return bad(who, "need 1 <= k <= min(E, SOM_ROUTE_MAX_TAKEN)");
     som_route_config c{};

@@ -36,6 +36,12 @@ template <int LPR, typename F> __device__ inline uint32_t reduce(uint32_t v, F f
     return v;
 }
 
+// The value of lane i of the row.
+template <int LPR> __device__ inline float of_lane(float v, int i)
+{
+    return LPR == 64 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), i)) : __shfl(v, i, LPR);
+}
+
 template <int LPR> __device__ inline uint32_t max_u32(uint32_t v)
 {
     return reduce<LPR>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
@@ -360,8 +366,12 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const RouteArgs a)
     const float over = z > 0.0f ? 1.0f / z : 0.0f;
     float g, sum = 0;  // g: the taken unit's gradient
     if (a.renorm) {
+        // the shares add up to 1: dw - sum dw w = sum over i of w_i (dw - dw_i), which loses nothing
+        // where one share is nearly all
         const float w = share<LPR>(softmax, l);
-        g = w * (dw - sum_f32<LPR>(dw * w));
+        float left = 0;
+        for (int i = 0; i < a.k; ++i) left = fmaf(of_lane<LPR>(w, i), dw - of_lane<LPR>(dw, i), left);
+        g = w * left;
         if (!softmax && took) g *= score_sigmoid(-l);
     } else if (softmax) {
         const float s = took ? exp_f32(l - m) * over : 0.0f;
@@ -375,7 +385,7 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const RouteArgs a)
     for (int j = 0; j < a.k; ++j) {  // the taken units in their lanes
         if (LPR == 64) {
             const int u = __builtin_amdgcn_readlane(unit, j);
-            const float gj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), j));
+            const float gj = of_lane<LPR>(g, j);
             if (u < 0) continue;
             const int at = (u / (4 * LPR)) * 4 + u % 4;  // the same register in every lane
             const bool mine = u / 4 % LPR == sub;
@@ -384,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const RouteArgs a)
                 if (i == at) r.l[i] = mine ? gj : r.l[i];
         } else {
             const int u = __shfl(unit, j, LPR);
-            const float gj = __shfl(g, j, LPR);
+            const float gj = of_lane<LPR>(g, j);
 #pragma unroll
             for (int i = 0; i < VPL; ++i) r.l[i] = Row<LPR, VPL>::unit(i, sub) == u ? gj : r.l[i];
         }
