@@ -130,7 +130,7 @@ som_status som_route_bwd(int32_t logit_type, const void *logits, int64_t ldl, co
  *   keep      1: the workspace is laid out for the backward pass and keeps what it needs.
  *   workspace device, som_experts_workspace_bytes(N, k, E, D, F, keep) bytes, 256-byte aligned.
  * w act(...) is rounded to `type` between the two products; the experts' results are added in fp32,
- * in the order of the row's places.
+ * in a fixed order.
  * 0 <= N; 1 <= k <= SOM_ROUTE_MAX_TAKEN; 1 <= E <= SOM_MAX_EXPERTS; N k < 2^30; 1 <= D, F < 2^24.
  */
 size_t som_experts_workspace_bytes(int64_t N, int32_t k, int64_t E, int64_t D, int64_t F, int32_t keep);

@@ -72,7 +72,7 @@ __global__ __launch_bounds__(kThreads) void k_squares(const ClipTable t, double 
 {
     __shared__ double lds[kThreads / 64];
     const int chunk = blockIdx.x, i = tensor_of(t, chunk);
-    const int64_t from = (int64_t)(chunk - t.first[i]) * kClipChunk, to = min(t.size[i], from + kClipChunk);
+    const int64_t from = (int64_t)(chunk - t.first[i]) * t.chunk, to = min(t.size[i], from + t.chunk);
     double s;
     if (t.type[i] == SOM_F32) s = squares<float>(t.in[i], from, to);
     else if (t.type[i] == SOM_F16) s = squares<_Float16>(t.in[i], from, to);
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kThreads) void k_scale(const ClipTable t, const flo
 {
     __shared__ double lds[kThreads / 64];
     const int chunk = blockIdx.x, i = tensor_of(t, chunk);
-    const int64_t from = (int64_t)(chunk - t.first[i]) * kClipChunk, to = min(t.size[i], from + kClipChunk);
+    const int64_t from = (int64_t)(chunk - t.first[i]) * t.chunk, to = min(t.size[i], from + t.chunk);
     float c;
     if (scale) {
         c = *scale;

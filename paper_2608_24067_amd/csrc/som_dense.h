@@ -43,6 +43,10 @@ struct Product {
     const int32_t *pairs;
     const void *pair_w;
     int32_t pair_rows;
+    // Then A may be z in fp32, z_parts arrays of M rows to be added up: what is multiplied is
+    // w act(z + z_bias[e]), rounded to the rows' type.
+    int32_t z_parts;
+    const void *z_bias;
     const int32_t *off;
     int32_t groups;         // 0: not grouped
     int64_t strideB, strideBias, strideC;
@@ -159,7 +163,13 @@ hipError_t launch_slope(bool bf16, const void *dy, int64_t lddy, const void *pre
 // ---------------------------------------------------------------- clipping
 
 constexpr int kClipTensors = 48;      // tensors of one launch
-constexpr int64_t kClipChunk = 65536; // elements of a workgroup
+
+// Elements of a workgroup: 2,048 workgroups where the tensors hold that many, 64K elements at most.
+inline int64_t clip_chunk(int64_t total)
+{
+    const int64_t n = (total / 2048 + 2047) / 2048 * 2048;
+    return n < 2048 ? 2048 : n > 65536 ? 65536 : n;
+}
 
 struct ClipTable {
     const void *in[kClipTensors];
@@ -168,6 +178,7 @@ struct ClipTable {
     int32_t first[kClipTensors + 1];  // chunks before each tensor
     int32_t type[kClipTensors];
     int32_t count;
+    int64_t chunk;
 };
 
 hipError_t launch_squares(const ClipTable &t, double *partial, hipStream_t st);

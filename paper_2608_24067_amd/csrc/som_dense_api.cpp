@@ -89,6 +89,7 @@ struct ExpertsLayout {
     som::TileSize tile;
     int splits;  // of the second product's reduction (few rows)
     bool plan;   // the pairs are ordered by expert
+    int inner_splits;  // of the first product's reduction (without a plan)
     int64_t n_parts;
 };
 
@@ -105,12 +106,18 @@ ExpertsLayout experts_layout(int64_t N, int32_t k, int64_t E, int64_t D, int64_t
     L.tile = pick_tile(P / met, met, D < F ? D : F, D % 8 == 0 && F % 8 == 0);
     L.splits = 1;
     L.plan = true;
+    L.inner_splits = 1;
     if (P / met <= kFewRows) {
         // Few rows: fill the CUs by splitting the second reduction, a step of 32 a wave at least.
         L.tile = som::kTileFew;
         L.plan = keep || P > kFewPairs;
         const int64_t tiles = met * ((D + 127) / 128), most = (F + 255) / 256;
         while (L.splits < 16 && tiles * L.splits < 256 && L.splits * 2 <= most) L.splits *= 2;
+        if (!L.plan) {  // the first one too: its parts are added where the second reads them
+            const int64_t inner_tiles = met * ((F + 127) / 128), inner_most = (D + 255) / 256;
+            while (L.inner_splits < 8 && inner_tiles * L.inner_splits < 256 && L.inner_splits * 2 <= inner_most)
+                L.inner_splits *= 2;
+        }
     }
     L.n_parts = som::slope_parts(som::kTileSmall, F);  // the most of any tile
     size_t at = 0;
@@ -126,7 +133,7 @@ ExpertsLayout experts_layout(int64_t N, int32_t k, int64_t E, int64_t D, int64_t
     L.w = take(P * 4);
     L.pos = take(P * 4);
     L.counts = take(som::pair_stretches(P) * E * 4);
-    L.inner = take(P * F * 2);
+    L.inner = take(P * F * (L.inner_splits > 1 ? 4 * L.inner_splits : 2));
     L.y = take(L.splits * P * D * 4);
     L.pre = take(keep ? P * F * 2 : 0);
     L.dz = take(keep ? P * F * 2 : 0);
@@ -415,9 +422,15 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
         p.w = x.plan.w;
         p.out = x.inner, p.ldo = F;
         if (!L.plan) p.pairs = idx, p.pair_w = w, p.pair_rows = k;
-        if (keep) p.pre = x.pre, p.ldp = F;
-        e = t == som::kTileFew ? som::launch_few(bf16, som::kInner, p, 1, s) : som::launch_nn(bf16, som::kInner, t, p, s);
-        if (e != hipSuccess) return hip_fail(e, who);
+        if (L.inner_splits > 1) {  // z in parts, without bias
+            p.bias = nullptr;
+            e = som::launch_few(bf16, som::kPairs, p, L.inner_splits, s);
+            if (e != hipSuccess) return hip_fail(e, who);
+        } else {
+            if (keep) p.pre = x.pre, p.ldp = F;
+            e = t == som::kTileFew ? som::launch_few(bf16, som::kInner, p, 1, s) : som::launch_nn(bf16, som::kInner, t, p, s);
+            if (e != hipSuccess) return hip_fail(e, who);
+        }
     }
     {
         const som::TileSize t = L.tile == som::kTileLarge && !chunks(W2, D) ? som::kTileMid : L.tile;
@@ -429,6 +442,7 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
         p.w = x.plan.w;
         p.out = x.y, p.ldo = D;
         if (!L.plan) p.pairs = idx, p.pair_w = w, p.pair_rows = 1;
+        if (L.inner_splits > 1) p.z_parts = L.inner_splits, p.z_bias = b1, p.act = act;
         e = t == som::kTileFew ? som::launch_few(bf16, som::kPairs, p, L.splits, s)
                                : som::launch_nn(bf16, som::kPairs, t, p, s);
         if (e != hipSuccess) return hip_fail(e, who);
@@ -522,22 +536,24 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
     return ok();
 }
 
-// Chunks of all tensors; negative if a size is out of range.
-static int64_t clip_chunks(const int64_t *sizes, int64_t count)
+// Chunks of all tensors and their size; negative if a size is out of range.
+static int64_t clip_chunks(const int64_t *sizes, int64_t count, int64_t *chunk)
 {
     if (count < 0 || count > INT32_MAX || (count > 0 && !sizes)) return -1;
-    int64_t n = 0;
+    int64_t total = 0, n = 0;
     for (int64_t i = 0; i < count; ++i) {
-        if (sizes[i] < 0 || sizes[i] > ((int64_t)1 << 40)) return -1;
-        n += (sizes[i] + som::kClipChunk - 1) / som::kClipChunk;
-        if (n > INT32_MAX) return -1;
+        if (sizes[i] < 0 || sizes[i] > ((int64_t)1 << 40) || total > ((int64_t)1 << 45)) return -1;
+        total += sizes[i];
     }
-    return n;
+    *chunk = som::clip_chunk(total);
+    for (int64_t i = 0; i < count; ++i) n += (sizes[i] + *chunk - 1) / *chunk;
+    return n > INT32_MAX ? -1 : n;
 }
 
 size_t som_clip_workspace_bytes(const int64_t *sizes, int64_t count)
 {
-    const int64_t n = clip_chunks(sizes, count);
+    int64_t chunk;
+    const int64_t n = clip_chunks(sizes, count, &chunk);
     return n < 0 ? 0 : 256 + align256((size_t)n * 8);
 }
 
@@ -545,7 +561,8 @@ som_status som_clip(const void *const *tensors, void *const *outs, const int64_t
                     int64_t count, float max_norm, float *norm, void *workspace, size_t workspace_bytes, void *stream)
 {
     const char *who = "som_clip";
-    const int64_t chunks_total = clip_chunks(sizes, count);
+    int64_t chunk;
+    const int64_t chunks_total = clip_chunks(sizes, count, &chunk);
     if (chunks_total < 0) return bad(who, "count or a size is out of range");
     if (!norm || (count > 0 && (!tensors || !outs || !types))) return bad(who, "null pointer");
     if (!(max_norm > 0.0f) || std::isinf(max_norm)) return bad(who, "max_norm must be positive and finite");
@@ -561,17 +578,18 @@ som_status som_clip(const void *const *tensors, void *const *outs, const int64_t
     float *scale = static_cast<float *>(workspace);
     double *partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + 256);
     // Few chunks: one launch less, each workgroup of the last pass adds them for itself.
-    const bool few = chunks_total > 0 && chunks_total <= 512 && count <= som::kClipTensors;
+    const bool few = chunks_total > 0 && chunks_total <= 4096 && count <= som::kClipTensors;
     for (int pass = 0; pass < 2; ++pass) {
         int64_t done = 0;
         for (int64_t i = 0; i < count; i += som::kClipTensors) {
             som::ClipTable t;
             t.count = (int32_t)(count - i < som::kClipTensors ? count - i : som::kClipTensors);
+            t.chunk = chunk;
             t.first[0] = 0;
             for (int j = 0; j < t.count; ++j) {
                 t.in[j] = tensors[i + j], t.out[j] = outs[i + j];
                 t.size[j] = sizes[i + j], t.type[j] = types[i + j];
-                t.first[j + 1] = t.first[j] + (int32_t)((t.size[j] + som::kClipChunk - 1) / som::kClipChunk);
+                t.first[j + 1] = t.first[j] + (int32_t)((t.size[j] + chunk - 1) / chunk);
             }
             const hipError_t e = pass == 0 ? som::launch_squares(t, partial + done, s)
                                  : few     ? som::launch_scale(t, nullptr, partial, chunks_total, max_norm, norm, s)

@@ -137,20 +137,32 @@ __global__ __launch_bounds__(64) void k_pairs_count(const int32_t *__restrict__ 
     for (int i = threadIdx.x; i < E; i += 64) counts[(int64_t)blockIdx.x * E + i] = lds[i];
 }
 
-// The counts become each stretch's first places.
-__global__ __launch_bounds__(1024) void k_pairs_scan(int32_t *counts, int stretches, int E, int rows, const PairPlan plan)
+// The counts become each stretch's first places. A thread takes an expert's counts of a part of the
+// stretches (parts * lanes = 1,024 threads, lanes a power of two of E at least).
+__global__ __launch_bounds__(1024) void k_pairs_scan(int32_t *counts, int stretches, int E, int lanes, int rows,
+                                                     const PairPlan plan)
 {
-    __shared__ int scan[2 * 1024];
-    const int e = threadIdx.x;
+    __shared__ int scan[2 * 1024], part[1024], start[1024];
+    const int e = threadIdx.x & (lanes - 1), at_part = threadIdx.x / lanes, parts = 1024 / lanes;
+    const int len = (stretches + parts - 1) / parts, v0 = min(stretches, at_part * len), v1 = min(stretches, v0 + len);
     int own = 0;
     if (e < E) {
 #pragma unroll 8
-        for (int v = 0; v < stretches; ++v) own += counts[v * E + e];
+        for (int v = v0; v < v1; ++v) own += counts[v * E + e];
     }
-    int at = lay_out(own, E, rows, scan, plan);
+    part[threadIdx.x] = own;
+    __syncthreads();
+    int total = 0;
+    if ((int)threadIdx.x < E)
+        for (int q = 0; q < parts; ++q) total += part[q * lanes + threadIdx.x];
+    const int first = lay_out(total, E, rows, scan, plan);
+    if ((int)threadIdx.x < E) start[threadIdx.x] = first;
+    __syncthreads();
     if (e < E) {
+        int at = start[e];
+        for (int q = 0; q < at_part; ++q) at += part[q * lanes + e];
 #pragma unroll 8
-        for (int v = 0; v < stretches; ++v) {
+        for (int v = v0; v < v1; ++v) {
             const int c = counts[v * E + e];
             counts[v * E + e] = at;
             at += c;
@@ -200,6 +212,34 @@ __global__ __launch_bounds__(256) void k_combine(const float *__restrict__ y, in
         }
         store4(out + n * ldo + d, cnt, s);
     }
+}
+
+// The same for few rows of many parts (k * splits): 64 columns a workgroup, each of its four waves
+// a quarter of the parts, their sums added in order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_combine_few(const float *__restrict__ y, int splits,
+                                                     const int32_t *__restrict__ pos, int no_plan_E, int64_t N, int k,
+                                                     int64_t D, const T *__restrict__ res, int64_t ldr, T *out,
+                                                     int64_t ldo)
+{
+    __shared__ float part[4][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t per = (D + 63) / 64, n = blockIdx.x / per, d = blockIdx.x % per * 64 + lane;
+    const int all = k * splits, len = (all + 3) / 4, i1 = min(all, (wave + 1) * len);
+    float s = 0;
+    if (d < D) {
+#pragma unroll 8
+        for (int i = wave * len; i < i1; ++i) {
+            int p = pos[n * k + i / splits];
+            if (no_plan_E) p = (unsigned)p < (unsigned)no_plan_E ? (int)(n * k + i / splits) : -1;
+            s += p >= 0 ? y[((int64_t)(i % splits) * N * k + p) * D + d] : 0.0f;
+        }
+    }
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && d < D)
+        out[n * ldo + d] = (T)((res ? (float)res[n * ldr + d] : 0.0f) + part[0][lane] + part[1][lane] + part[2][lane] +
+                               part[3][lane]);
 }
 
 // A wave a row.
@@ -309,7 +349,9 @@ hipError_t launch_pairs(bool bf16, const int32_t *idx, const void *w, int64_t P,
         hipLaunchKernelGGL(k_pairs_count, dim3(n), dim3(64), E * sizeof(int), st, idx, P, E, plan.counts);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(k_pairs_scan, dim3(1), dim3(E <= 256 ? 256 : 1024), 0, st, plan.counts, n, E, rows, plan);
+        int lanes = 16;
+        while (lanes < E) lanes *= 2;
+        hipLaunchKernelGGL(k_pairs_scan, dim3(1), dim3(1024), 0, st, plan.counts, n, E, lanes, rows, plan);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         hipLaunchKernelGGL(many, dim3(n), dim3(64), E * sizeof(int), st, idx, weights, P, k, E, plan.counts, plan);
         return hipGetLastError();
@@ -322,10 +364,16 @@ hipError_t launch_combine(bool bf16, const float *y, int splits, const int32_t *
                           const void *res, int64_t ldr, void *out, int64_t ldo, hipStream_t st)
 {
     const unsigned grid = spread((N * ((D + 3) / 4) + 255) / 256);
+    // From eight parts on, where four columns a thread do not fill the CUs (one row of 1,024 columns,
+    // two places, 16 splits: 10.6 us).
+    const bool few = k * splits >= 8 && N * D < 256 * 1024;
     auto with = [&](auto kernel, const auto *r, auto *o) {
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, y, splits, pos, no_plan_E, N, k, D, r, ldr, o, ldo);
+        hipLaunchKernelGGL(kernel, dim3(few ? (unsigned)(N * ((D + 63) / 64)) : grid), dim3(256), 0, st, y, splits, pos,
+                           no_plan_E, N, k, D, r, ldr, o, ldo);
         return hipGetLastError();
     };
+    if (few && bf16) return with(&k_combine_few<__bf16>, static_cast<const __bf16 *>(res), static_cast<__bf16 *>(out));
+    if (few) return with(&k_combine_few<_Float16>, static_cast<const _Float16 *>(res), static_cast<_Float16 *>(out));
     if (bf16) {
         const auto *r = static_cast<const __bf16 *>(res);
         auto *o = static_cast<__bf16 *>(out);

@@ -50,7 +50,7 @@ __device__ inline s16x8 load8(const short *p, int n)
     return r;
 }
 
-template <typename T, Epilogue EPI, int kWaves>
+template <typename T, Epilogue EPI, int kWaves, bool Z = false>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int splits)
 {
     typedef typename Vec8<T>::type Frag;
@@ -81,12 +81,36 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
 
     const int row = min(m0 + c, m1 - 1);
     const int64_t at = p.pairs ? row / p.pair_rows : p.amap ? p.amap[row] : row;
-    const short *a = static_cast<const short *>(p.A) + at * p.lda + 8 * g;
+    const short *a = static_cast<const short *>(p.A) + (Z ? 0 : at * p.lda + 8 * g);
     const int n_from = nt * kCols, n0 = N >= kCols ? min(n_from, N - kCols) : 0;
     const int last = N - n0 - 8;  // where the last lane's eight columns start (negative: fewer than 8 in all)
     const int cols = min(8, N - n0 - 8 * c);
     const short *b = static_cast<const short *>(p.B) + (int64_t)e * p.strideB + 8 * (int64_t)g * p.ldb + n0 +
                      (last >= 0 ? min(8 * c, last) : cols > 0 ? 8 * c : 0);
+
+    // Eight values of w act(z + bias) from the parts of z (one pair: every lane's row is the same).
+    const float pair_w = p.pairs ? (float)static_cast<const T *>(p.pair_w)[m0] : 0.0f;
+    auto inner8 = [&](int k0) {
+        typedef T vec __attribute__((ext_vector_type(8)));
+        vec r;
+#pragma unroll
+        for (int h = 0; h < 8; h += 4) {
+            const int n = max(0, min(4, K - k0 - h));
+            float z[4] = {0, 0, 0, 0}, b4[4] = {0, 0, 0, 0};
+            if (n > 0) {
+                for (int q = 0; q < p.z_parts; ++q) {
+                    float v[4];
+                    load4(static_cast<const float *>(p.A) + ((int64_t)q * p.M + m0) * p.lda + k0 + h, n, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[i] += v[i];
+                }
+                if (p.z_bias) load4(static_cast<const T *>(p.z_bias) + (int64_t)e * K + k0 + h, n, b4);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[h + i] = i < n ? (T)(pair_w * act_value(p.act, z[i] + b4[i])) : (T)0.0f;
+        }
+        return __builtin_bit_cast(s16x8, r);
+    };
 
     f32x4 acc[8];
 #pragma unroll
@@ -107,21 +131,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
 #pragma unroll
             for (int d = 0; d < kDeep; ++d) {
                 const int64_t k = (int64_t)(s + d) * 32;
-                va[d] = *reinterpret_cast<const any *>(a + k);
+                if (!Z) va[d] = *reinterpret_cast<const any *>(a + k);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) vb[d][q] = *reinterpret_cast<const any *>(b + (k + q) * p.ldb);
             }
 #pragma unroll
-            for (int d = 0; d < kDeep; ++d) multiply(va[d], vb[d]);
+            for (int d = 0; d < kDeep; ++d) {
+                if (Z) va[d] = inner8((s + d) * 32 + 8 * g);
+                multiply(va[d], vb[d]);
+            }
         }
         for (; s < s1; ++s) {
             const int64_t k = (int64_t)s * 32;
             const int left = K - s * 32 - 8 * g;  // features of the lane's eight
-            s16x8 va = *reinterpret_cast<const any *>(a + k + min(0, left - 8)), vb[8];
+            s16x8 va, vb[8];
+            if (!Z) va = *reinterpret_cast<const any *>(a + k + min(0, left - 8));
 #pragma unroll
             for (int q = 0; q < 8; ++q) vb[q] = *reinterpret_cast<const any *>(b + (k + min(q, left - 1)) * p.ldb);
+            if (Z) va = inner8(s * 32 + 8 * g);
             if (left < 8) {
-                va = shift_out(va, left);
+                if (!Z) va = shift_out(va, left);
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
                     if (q >= left) vb[q] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
@@ -135,7 +164,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
         s16x8 vb[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) vb[q] = load8(b + (k + q) * p.ldb, q < left ? cols : 0);
-        multiply(load8(a + k, left), vb);
+        multiply(Z ? inner8(s * 32 + 8 * g) : load8(a + k, left), vb);
     }
 
     // Lane (m, g) has columns (4g + i) 8 + j of row m in acc[j][i].
@@ -203,6 +232,7 @@ template <typename T> hipError_t go(Epilogue e, const Product &p, int splits, hi
         hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * waves), 0, st, p, splits);
         return hipGetLastError();
     };
+    if (p.z_parts) return with(k_few<T, kPairs, 8, true>, 8);
     // Eight waves bring a tile's part of the matrix at once; from two tiles a CU on four do, so that
     // one workgroup's loads run while the other adds up.
     if (grid >= 512)

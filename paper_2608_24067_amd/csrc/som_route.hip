@@ -18,7 +18,7 @@ using mm::store4;
 
 template <int CTRL> __device__ inline uint32_t lane_swap(uint32_t v)
 {
-    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);  // every lane has a source
 }
 
 // Over the LPR lanes of a row, in every lane: pairs, quads, half rows, rows of 16, then the wave.

@@ -314,18 +314,20 @@ def clip(tensors, max_norm: float, out=None, norm=None, workspace=None):
             raise ValueError("no tensors: pass norm")
         norm = torch.empty(1, dtype=torch.float32, device=tensors[0].device)
     n, dev = len(tensors), norm.device
-    types, lengths = [], []
+    if not norm.is_cuda:
+        raise ValueError("norm must be on the GPU")
+    at, types, lengths = dev.index, [], []
     for t in tensors:
         kind = _TYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
         if kind is None:
             _type(t, "tensors", halves=False)
-        if t.device != dev or not t.is_contiguous():
+        if t.get_device() != at or not t.is_contiguous():
             raise ValueError("tensors must be contiguous and on one GPU")
         types.append(kind)
         lengths.append(t.numel())
     if out is not None:
         for o, t, m in zip(outs, tensors, lengths):
-            if (not isinstance(o, torch.Tensor) or o.dtype != t.dtype or o.numel() != m or o.device != dev
+            if (not isinstance(o, torch.Tensor) or o.dtype is not t.dtype or o.numel() != m or o.get_device() != at
                     or not o.is_contiguous()):
                 raise ValueError("out must hold contiguous tensors of the same sizes and types")
     pointers = ctypes.c_void_p * n
