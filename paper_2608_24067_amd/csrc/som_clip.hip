@@ -1,8 +1,11 @@
 // som_clip.hip -- the norm of many tensors together, and their scaling to a largest norm.
 //
-// Three passes: every workgroup sums the squares of one chunk of one tensor (fp64, the threads'
-// sums joined in a fixed order), one workgroup adds the chunks' sums and forms the scale, and the
-// chunks are scaled. Both large passes are bound by the bytes they move.
+// Three passes: every workgroup sums the squares of one chunk of one tensor (fp64, so that no
+// square of an fp32 value overflows or vanishes; the threads' sums joined in a fixed order), one
+// workgroup adds the chunks' sums and forms the scale, and the chunks are scaled. Few chunks: the
+// second pass is done by every workgroup of the third. Both large passes are bound by the bytes
+// they move: 2.3 GB in three types are summed at 5.6 TB/s and read and written at 5.1 TB/s
+// (415 + 900 us); the scale needs the norm, so the tensors are read twice.
 
 #include "som_mm.h"
 
@@ -113,7 +116,7 @@ template <typename T> __device__ inline void scaled(const void *in, void *out, i
             vec x;
 #pragma unroll
             for (int q = 0; q < V; ++q) x[q] = (T)(c == 1.0f ? v[q] : v[q] * c);
-            *reinterpret_cast<any *>(o + i) = x;
+            __builtin_nontemporal_store(x, reinterpret_cast<any *>(o + i));
         } else {
 #pragma unroll
             for (int q = 0; q < V; ++q)
@@ -127,7 +130,9 @@ __global__ __launch_bounds__(kThreads) void k_scale(const ClipTable t, const flo
                                                     float *__restrict__ norm)
 {
     __shared__ double lds[kThreads / 64];
-    const int chunk = blockIdx.x, i = tensor_of(t, chunk);
+    // From the last chunk to the first: the last ones summed are still in the 256 MB cache, which the
+    // results pass by (372 million values in three types: 1,333 -> 1,315 us).
+    const int chunk = (int)(gridDim.x - 1 - blockIdx.x), i = tensor_of(t, chunk);
     const int64_t from = (int64_t)(chunk - t.first[i]) * t.chunk, to = min(t.size[i], from + t.chunk);
     float c;
     if (scale) {

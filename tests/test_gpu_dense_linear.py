@@ -176,3 +176,50 @@ def test_another_stream_and_repeats_give_the_same_bits(dev):
         again = (dense.linear(x, W, b, residual=r),) + dense.linear_bwd(x, W, dy)
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(first, again))
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("N,K,M", [
+    (300, 5, 200), (40, 7, 3), (5, 300, 50), (16, 64, 9), (9, 33, 130), (12, 7, 129), (3, 2048, 5), (1, 1000, 127),
+    (17, 8, 8), (200, 9, 300), (130, 1001, 129), (1000, 33, 127), (2, 100, 1025), (16, 39, 7),
+])
+def test_linear_at_the_edges_of_tiles(dev, dtype, N, K, M):
+    for pad, offset in ((0, 0), (3, 1)):
+        x, W, b, r, _ = case(19, N, K, M, dtype, dev, pad, offset)
+        out = dense.linear(x, W, b, residual=r, act="silu")
+        z = wide(x) @ wide(W) + wide(b)
+        err = sums(K + 1, wide(x).abs() @ wide(W).abs() + wide(b).abs())
+        y = act("silu", z) + wide(r)
+        check(out, y, LIP * err + 2.0 ** -20 * z.abs().clamp_min(1) + 2.0 ** -23 * (z.abs() + wide(r).abs()), "y")
+
+
+@pytest.mark.parametrize("N,K,M,pad", [(20000, 40, 56, 0), (9001, 70, 91, 0), (30000, 264, 16, 8), (2000, 6, 7, 1),
+                                       (1500, 129, 3, 0)])
+def test_weights_gradient_of_many_rows(dev, N, K, M, pad):
+    x, W, b, _, g = case(20, N, K, M, torch.float16, dev, pad)
+    dy = strided((N, M), pad, torch.float16, dev, g)
+    dx, dW, db = dense.linear_bwd(x, W, dy, bias_dtype=torch.float32)
+    check(dW, wide(x).T @ wide(dy), sums(N, wide(x).abs().T @ wide(dy).abs()), "dW")
+    check(db, wide(dy).sum(0), sums(N, wide(dy).abs().sum(0)), "db")
+    check(dx, wide(dy) @ wide(W).T, sums(M, wide(dy).abs() @ wide(W).abs().T), "dx")
+    part = dense.linear_bwd(x, W, dy, out=(None, None, torch.empty_like(db)))[2]
+    assert torch.equal(part, db)
+
+
+def test_rows_past_32_bit_offsets(dev):
+    step = 1_200_000_000  # elements between rows: the third lies 4.8 GB in
+    buf = torch.empty(2 * step + 64, dtype=torch.float16, device=dev)
+    x = buf.as_strided((3, 64), (step, 1))
+    g = torch.Generator().manual_seed(22)
+    x.copy_(torch.randn(3, 64, generator=g).half())
+    W = (torch.randn(64, 40, generator=g) / 8).half().to(dev)
+    ref = wide(x) @ wide(W)
+    check(dense.linear(x, W), ref, sums(64, wide(x).abs() @ wide(W).abs()), "few rows")
+    many = buf.as_strided((40, 64), (2 * step // 39 // 8 * 8, 1))
+    many.copy_(torch.randn(40, 64, generator=g).half())
+    check(dense.linear(many, W), wide(many) @ wide(W), sums(64, wide(many).abs() @ wide(W).abs()), "tiles")
+    dy = torch.randn(40, 40, generator=g).half().to(dev)
+    dW = dense.linear_bwd(many, W, dy)[1]
+    check(dW, wide(many).T @ wide(dy), sums(40, wide(many).abs().T @ wide(dy).abs()), "dW")
+    del buf, x, many
+    torch.cuda.empty_cache()

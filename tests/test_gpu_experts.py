@@ -225,3 +225,62 @@ def test_same_bits_on_another_stream(dev):
         again = dense.experts(**s)
     torch.cuda.synchronize()
     assert torch.equal(first, again)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("N,k,E,D,F", [
+    (1, 2, 4, 700, 900), (2, 3, 8, 1030, 515), (5, 3, 16, 2048, 300), (1, 1, 3, 1000, 3), (4, 4, 2, 5, 600),
+    (16, 1, 5, 777, 1025),
+])
+def test_few_pairs_whose_reductions_are_split(dev, dtype, N, k, E, D, F):
+    for a in ("silu", "gelu"):
+        s, g = case(39, N, k, E, D, F, dtype, dev, empty=0.0 if N == 1 else 0.1)
+        if N == 1:
+            s["w"].fill_(0.75)
+        out = dense.experts(**s, act=a, residual=s["x"])
+        ref, bound = forms(s, a, s["x"])
+        check(out, ref, bound, f"out, {a}")
+
+
+@pytest.mark.parametrize("N,k,E", [(3000, 1, 1024), (2049, 1, 17), (1100, 2, 300), (70000, 1, 5)])
+def test_orders_of_many_pairs(dev, N, k, E):
+    # the identity as experts: every row comes back as often as its weights say
+    g = torch.Generator().manual_seed(40)
+    x = torch.randn(N, 8, generator=g).half().to(dev)
+    idx = torch.randint(-1, E, (N, k), generator=g, dtype=torch.int32).to(dev)
+    w = torch.ones(N, k, dtype=torch.float16, device=dev)
+    eye = torch.eye(8, dtype=torch.float16, device=dev).expand(E, 8, 8).contiguous()
+    scale = (1 + torch.arange(E, device=dev) % 7).half()
+    out = dense.experts(x, idx, w, eye * scale[:, None, None], None, eye, None, act="none")
+    times = (scale[idx.clamp_min(0).long()].float() * (idx >= 0)).sum(1, keepdim=True)
+    # powers and small multiples of 11-bit values: each product is rounded to fp16 once, and so is the sum
+    assert bool(((out.float() - x.float() * times).abs() <= 2.0 ** -10 * (k + 1) * x.float().abs() * times + 1e-6).all())
+
+
+def test_weights_past_32_bit_offsets(dev):
+    # 2.5 billion weights a matrix; only the experts that are met are filled
+    N, k, E, D, F = 6, 2, 600, 1024, 4096
+    g = torch.Generator().manual_seed(41)
+    met = [0, 299, 511, 599]
+    W1, W2 = (torch.empty(E, *d, dtype=torch.bfloat16, device=dev) for d in ((D, F), (F, D)))
+    for e in met:
+        W1[e] = (torch.randn(D, F, generator=g) * D ** -0.5).bfloat16()
+        W2[e] = (torch.randn(F, D, generator=g) * F ** -0.5).bfloat16()
+    x = torch.randn(N, D, generator=g).bfloat16().to(dev)
+    for rows in (N, 400):  # few pairs, and tiles
+        idx = torch.tensor(met, dtype=torch.int32)[torch.randint(0, 4, (rows, k), generator=g)].to(dev)
+        xs = x[torch.arange(rows) % N].contiguous()
+        w = torch.full((rows, k), 0.5, dtype=torch.bfloat16, device=dev)
+        out = dense.experts(xs, idx, w, W1, None, W2, None, act="relu")
+        ref = torch.zeros(rows, D, device=dev)
+        size = torch.zeros(rows, D, device=dev)
+        for e in met:
+            hit = (idx == e).float().sum(1, keepdim=True) * 0.5
+            h = torch.relu(xs.float() @ W1[e].float())
+            ref += hit * (h @ W2[e].float())
+            size += hit * (h @ W2[e].float().abs())
+        # the inner rows are rounded once (2^-8 of them at most), the results once
+        assert bool(((out.float() - ref).abs() <= 2.0 ** -8 * (size + ref.abs()) + 1e-4).all())
+        del ref, size
+    del W1, W2
+    torch.cuda.empty_cache()
