@@ -354,6 +354,12 @@ template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int AHEAD_, int PER_C
     static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
 };
 
+// The value of another lane of the 16, by a pattern of data-parallel primitives.
+template <int CTRL> __device__ inline float lane_swap(float v)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+
 // A wave's LDS accesses before this are done before those after it (LDS serves a wave in order;
 // the wait is for the values, the clobber for the compiler). Nothing else is waited for.
 __device__ inline void wave_sync_lds()
@@ -782,9 +788,13 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
             else if (p.act == SOM_ACT_RELU) slopes(SOM_ACT_RELU);
             else slopes(SOM_ACT_NONE);
 #pragma unroll
-            for (int d = 1; d < kLanes; d *= 2)
-#pragma unroll
-                for (int r = 0; r < kTurns; ++r) part[r] += __shfl_xor(part[r], d);
+            for (int r = 0; r < kTurns; ++r) {  // over the row's 8 or 16 lanes: pairs, quads, halves, rows of 16
+                part[r] += lane_swap<0xB1>(part[r]);
+                part[r] += lane_swap<0x4E>(part[r]);
+                part[r] += lane_swap<0x141>(part[r]);
+                if (kLanes == 16) part[r] += lane_swap<0x140>(part[r]);
+            }
+            static_assert(kLanes == 8 || kLanes == 16, "a row's lanes");
 #pragma unroll
             for (int r = 0; r < kTurns; ++r)
                 if (m[r] < m1 && lane % kLanes == 0) p.parts[(int64_t)m[r] * p.n_parts + nt * S::WN + wn] = part[r];
