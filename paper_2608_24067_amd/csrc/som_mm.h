@@ -8,8 +8,9 @@
 // transpose read, which gives a lane four steps of one column.
 //
 // Chunks are placed in LDS so that the lanes of one read touch every bank once:
-//   along:  64-byte rows of 4 chunks, chunk s of row r at s ^ (r / 4 % 4): sixteen rows at
-//           one step octet cover sixteen different 16-byte slots;
+//   along:  64-byte rows of 4 chunks, chunk s of row r at s ^ f(r), f = -(r / 4) mod 4: sixteen
+//           rows at one step octet cover sixteen different 16-byte slots, and so do rows 0-3 and
+//           12-15 of one octet with rows 4-11 of the next, which is what LDS serves together;
 //   across: rows of BR * 2 bytes, the 32-byte unit u (16 columns) of row k at u ^ f(k), f
 //           from bits 0, 1 and 3 of k, so that the eight rows of a half wave's transpose read
 //           lie in different units.
@@ -139,6 +140,9 @@ template <typename T> __device__ inline void store4(T *p, int from, int n, const
 
 template <typename T> __device__ inline void store4(T *p, int n, const float *v) { store4(p, 0, n, v); }
 
+// The place of chunks in an "along" row.
+__device__ inline int chunk_xor(int r) { return -(r >> 2) & 3; }
+
 // The place of 32-byte units in an "across" row.
 template <int BR> __device__ inline int unit_xor(int k)
 {
@@ -196,7 +200,7 @@ template <typename T, int BR, bool ACROSS, bool MAPPED, int NT> struct Loader {
                 if (CHUNKS) col = min(col, r1 - 8);
                 ptr[i] = p + col + (MAPPED ? 0 : (k0 + row) * ld);
             } else {
-                const int src = s ^ ((row >> 2) & 3);
+                const int src = s ^ chunk_xor(row);
                 const int r = min(r0 + row, r1 - 1);
                 k[i] = 8 * src;
                 cnt[i] = 8;
@@ -326,7 +330,7 @@ template <typename T, int BR, bool ACROSS> struct Reader {
             const int row = 8 * g + (i >> 2);
             base = row * (BR * 2) + ((((uint32_t)at >> 4) ^ unit_xor<BR>(row)) << 5) + (i & 3) * 8;
         } else {
-            base = (at + i) * (kBK * 2) + ((g ^ (i >> 2)) << 4);
+            base = (at + i) * (kBK * 2) + ((g ^ chunk_xor(i)) << 4);
         }
     }
 
