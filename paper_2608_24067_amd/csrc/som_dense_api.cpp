@@ -44,41 +44,62 @@ bool dim_ok(int64_t v) { return v >= 1 && v < kMostDim; }
 // Whether an operand's rows can be moved in whole 16-byte chunks.
 bool chunks(const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0; }
 
-// Experts (and whole calls) of up to this many rows go to the kernel for few rows.
+// Tiles of 16 rows and 128 columns, the height of the kernel for few rows.
+int64_t few_tiles(int64_t rows, int64_t cols) { return (rows + 15) / 16 * ((cols + 127) / 128); }
+
+// A product of few rows: all whose tiles are one a CU at most (bf16, us, few rows' kernel against the
+// other: 96 rows 4096 x 4096 20.1 against 23.8, 512 rows 4096 x 1024 21.0 against 24.1; 48 rows
+// 1024 x 16384, 384 tiles, 14.6 against 10.0), and every one of a single tile row.
+bool few_rows(int64_t rows, int64_t cols) { return rows <= 16 || few_tiles(rows, cols) <= 256; }
+
+// Experts go to the kernel for few rows from eight rows each on average down, where that can split
+// the second reduction to fill the CUs (8 experts, D 1024, F 4096, 1 to 6 rows each: 34-48 us against
+// 49-58 by Small tiles; 16 rows each 64 against 60) or rows are no whole chunks (13 experts of 1003 x
+// 2001: 34-44 against 56-58). With a tile a CU without splits Small tiles, which keep six steps of
+// loads in flight, read faster (32 experts, D 1024, F 2048, 1 to 6 rows: 43-68 us against 48-78).
 constexpr int64_t kFewRows = 8;
 
-// Up to this many pairs are not ordered by expert first (a launch of 5 us): each reads its
-// expert's weights for itself.
-constexpr int64_t kFewPairs = 16;
+// Pairs that are not ordered by expert first (a launch of 5 us): each reads its expert's weights for
+// itself. While they are no more than the experts, few share one (64 experts, D 1024, F 2048: 16
+// pairs 33 us against 39, 40 pairs 52 against 57; 16 experts, F 4096: 16 pairs 55 against 61, 24
+// pairs 80 against 64; 4 experts: 16 pairs 40 against 29).
+constexpr int64_t kFewPairs = 64;
 
-// The tile of a product of `rows` rows a group and `cols` columns. Large tiles read each
-// operand least often but need enough of them to fill the 256 CUs.
+// The tile of a product of `rows` rows a group and `cols` columns: the smallest of which two
+// workgroups a CU hold all, since larger ones read each operand less often but take as long for one
+// tile as for a CU's every (bf16, 4096 features, us by Small, Mid and Large tiles: 512 x 4096 38, 38,
+// 80; 1024 x 4096 70, 43, 81; 2048 x 4096 134, 74, 84; 2304 x 4352 -, 102, 86; 2560 x 5120 209, 129,
+// 95; 64 rows x 16384 25, 39, 78).
 som::TileSize pick_tile(int64_t rows, int64_t groups, int64_t cols, bool whole)
 {
     auto tiles = [&](som::TileSize t) {
         return (rows + tile_rows(t) - 1) / tile_rows(t) * groups * ((cols + tile_cols(t) - 1) / tile_cols(t));
     };
-    if (whole && rows >= 192 && tiles(som::kTileLarge) >= 200) return som::kTileLarge;
-    if (rows >= 64 && tiles(som::kTileMid) >= 128) return som::kTileMid;
+    if (whole && rows >= 192 && tiles(som::kTileMid) > 512) return som::kTileLarge;
+    if (rows >= 64 && tiles(som::kTileSmall) > 512) return som::kTileMid;
     return som::kTileSmall;
 }
 
-// The tile of a product over rows (M x N a group). Large tiles pay from one a CU on (8192 rows,
-// 2048 x 4096, 128 of them: 172 us against 135 by Mid tiles; 10,007 rows to 32 experts, 1024 of
-// them: 107 against 143).
+// The tile of a product over rows (M x N a group), by the same rule (8192 rows, us by Mid and Large
+// tiles: 2048 x 4096 135, 173; 2048 x 4352 183, 168; 4096 x 4096 252, 208; 10,007 rows to 32 experts,
+// 1000 x 2048 each: 143, 107).
 som::TileSize pick_tile_tn(int64_t M, int64_t N, int64_t groups)
 {
-    return (M + 255) / 256 * ((N + 255) / 256) * groups >= 256 ? som::kTileLarge : som::kTileMid;
+    return (M + 127) / 128 * ((N + 127) / 128) * groups > 512 ? som::kTileLarge : som::kTileMid;
 }
 
-// Parts that a layer's weights' gradient (K x M from N rows) is computed in, where its tiles do
-// not fill the CUs: 512 rows a part at least, and at most 8 MB of fp32 parts.
+// Parts that a layer's weights' gradient (K x M from N rows) is computed in, where its tiles do not
+// fill the CUs: of 512 rows at least, and of no more bytes (written and read again) than 32 MB and
+// 7 KB a row (bf16, us in one part and in parts: 8192 rows 1024 x 1024 75, 32; 4096 rows 40, 24; 16384
+// rows 256 x 256 144, 22, 2048 x 1024 146, 90; but 1024 rows 1024 x 1024 14, 16; 4096 rows 2048 x
+// 2048 44, 48).
 int grad_parts(int64_t N, int64_t K, int64_t M)
 {
-    const int64_t tiles = (K + 127) / 128 * ((M + 127) / 128), bytes = (K + 1) * M * 4;
+    const int64_t tiles = (K + 127) / 128 * ((M + 127) / 128), bytes = K * M * 4;
     int64_t n = 512 / tiles;
     if (n > N / 512) n = N / 512;
-    if (n > (8 << 20) / bytes) n = (8 << 20) / bytes;
+    const int64_t most = N * 7168 < (32 << 20) ? N * 7168 : 32 << 20;
+    if (n > most / bytes) n = most / bytes;
     return n < 2 ? 1 : (int)n;
 }
 
@@ -103,15 +124,17 @@ ExpertsLayout experts_layout(int64_t N, int32_t k, int64_t E, int64_t D, int64_t
 {
     ExpertsLayout L;
     const int64_t P = N * k, met = P < E ? (P < 1 ? 1 : P) : E;
-    L.tile = pick_tile(P / met, met, D < F ? D : F, D % 8 == 0 && F % 8 == 0);
+    const bool whole = D % 8 == 0 && F % 8 == 0;
+    L.tile = pick_tile(P / met, met, D < F ? D : F, whole);
     L.splits = 1;
     L.plan = true;
     L.inner_splits = 1;
-    if (P / met <= kFewRows) {
+    const int64_t tiles = met * ((D + 127) / 128);
+    if (P / met <= kFewRows && (!whole || tiles < 256)) {
         // Few rows: fill the CUs by splitting the second reduction, a step of 32 a wave at least.
         L.tile = som::kTileFew;
-        L.plan = keep || P > kFewPairs;
-        const int64_t tiles = met * ((D + 127) / 128), most = (F + 255) / 256;
+        L.plan = keep || P > E || P > kFewPairs;
+        const int64_t most = (F + 255) / 256;
         while (L.splits < 16 && tiles * L.splits < 256 && L.splits * 2 <= most) L.splits *= 2;
         if (!L.plan) {  // the first one too: its parts are added where the second reads them
             const int64_t inner_tiles = met * ((F + 127) / 128), inner_most = (D + 255) / 256;
@@ -220,7 +243,7 @@ som_status som_linear(int32_t type, const void *X, int64_t ldx, const void *W, i
     p.out = Y, p.ldo = ldy, p.out_f32 = y_type == SOM_F32;
     p.pre = pre, p.ldp = ldp;
     const bool whole = chunks(X, ldx) && chunks(W, ldw) && K % 8 == 0 && M % 8 == 0;
-    if (N <= 2 * kFewRows) {
+    if (few_rows(N, M)) {
         const hipError_t e = som::launch_few(type == SOM_BF16, som::kLinear, p, 1, static_cast<hipStream_t>(stream));
         return e == hipSuccess ? ok() : hip_fail(e, who);
     }

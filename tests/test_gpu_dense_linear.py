@@ -223,3 +223,23 @@ def test_rows_past_32_bit_offsets(dev):
     check(dW, wide(many).T @ wide(dy), sums(40, wide(many).abs().T @ wide(dy).abs()), "dW")
     del buf, x, many
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("N,K,M,pad,offset,a", [
+    (96, 264, 1024, 0, 0, "silu"),   # one tile of 16 rows a CU at most
+    (500, 130, 1003, 1, 1, "gelu"),
+    (90, 72, 5504, 0, 0, "none"),    # 258 of them: tiles of 32 rows
+    (600, 43, 1000, 3, 1, "gelu"),
+    (1600, 40, 1280, 0, 0, "relu"),  # 500 of those
+    (1640, 40, 1280, 0, 0, "silu"),  # 520: tiles of 128 rows
+    (2050, 64, 3900, 8, 0, "none"),  # 527 of those: tiles of 256
+])
+def test_linear_where_the_tile_changes(dev, dtype, N, K, M, pad, offset, a):
+    x, W, b, r, _ = case(21, N, K, M, dtype, dev, pad, offset)
+    out = dense.linear(x, W, b, residual=r, act=a)
+    z = wide(x) @ wide(W) + wide(b)
+    err = sums(K + 1, wide(x).abs() @ wide(W).abs() + wide(b).abs())
+    y = act(a, z) + wide(r)
+    check(out, y, LIP * err + 2.0 ** -20 * (z.abs().clamp_min(1) if a != "none" else 0) + 2.0 ** -23 * (z.abs() + wide(r).abs()),
+          "y")

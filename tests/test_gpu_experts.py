@@ -284,3 +284,19 @@ def test_weights_past_32_bit_offsets(dev):
         del ref, size
     del W1, W2
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("N,k,E,D,F", [
+    (12, 2, 64, 1024, 136),  # 24 pairs, each by itself, both reductions split
+    (32, 2, 64, 72, 520),    # 64 of them
+    (33, 2, 70, 65, 131),    # 66: ordered
+    (16, 4, 60, 40, 48),     # more than experts: ordered
+    (20, 4, 64, 520, 72),    # a tile a CU: the tiles of 32 rows
+    (21, 4, 64, 515, 75),    # which odd rows do not take
+])
+def test_few_rows_an_expert(dev, dtype, N, k, E, D, F):
+    s, g = case(41, N, k, E, D, F, dtype, dev)
+    out = dense.experts(**s, act="silu", residual=s["x"])
+    ref, bound = forms(s, "silu", s["x"])
+    check(out, ref, bound, "out")
