@@ -64,8 +64,9 @@ __device__ inline float exp_f32(float x)
 __device__ inline float exp_short(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // The normal distribution Phi(z) and exp(-z^2 / 2), by formula 7.1.26 of Abramowitz and Stegun's
-// Handbook of Mathematical Functions for the error function: within 1.5e-7, which 16-bit results
-// do not see, for a third of erff's instructions.
+// Handbook of Mathematical Functions for the error function: within 1.5e-7 of itself (of z Phi(z)
+// for z below about -4 that is more than a 16-bit result's rounding, of values below 2e-4), for a
+// third of erff's instructions.
 __device__ inline float normal_f32(float z, float &bell)
 {
     const float x = fabsf(z) * 0.707106781f;
