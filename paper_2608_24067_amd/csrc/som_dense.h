@@ -83,6 +83,21 @@ constexpr int tile_cols(TileSize t) { return t == kTileLarge ? 256 : 128; }
 // Tile rows of a plan over P pairs of E experts, at most.
 inline int64_t max_tile_rows(int64_t P, int64_t E, int rows) { return P / rows + (E < P ? E : P); }
 
+// Tiles of t in the height of a tile row of a plan laid out for `plan`; a tile higher than that takes
+// one tile row all the same.
+inline int tiles_in_row(TileSize plan, TileSize t)
+{
+    return tile_rows(plan) > tile_rows(t) ? tile_rows(plan) / tile_rows(t) : 1;
+}
+
+// Rows of tiles a product (NN, NT) is launched with. A grouped one may meet any loads, so it needs
+// as many as the plan has tile rows at the height the plan was laid out for: tiles higher than that
+// are no fewer.
+inline int64_t launch_tile_rows(const Product &p, TileSize t)
+{
+    return p.groups ? max_tile_rows(p.M, p.groups, p.tile_height) * p.split : (p.M + tile_rows(t) - 1) / tile_rows(t);
+}
+
 hipError_t launch_nn(bool bf16, Epilogue e, TileSize t, const Product &p, hipStream_t st);
 // The same (kLinear, kInner, kPairs) for few rows. splits: workgroups that share out a tile's
 // reduction (kPairs only, else 1); split s of row m is written to row s * M + m of the result.

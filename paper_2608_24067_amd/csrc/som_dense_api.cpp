@@ -208,7 +208,7 @@ struct Grouped {
         p.tiles = plan.tiles;
         p.n_tiles = plan.n_tiles;
         p.tile_height = tile_rows(L.tile);
-        p.split = p.tile_height > tile_rows(t) ? p.tile_height / tile_rows(t) : 1;
+        p.split = som::tiles_in_row(L.tile, t);
         p.groups = (int32_t)E;
         return p;
     }

@@ -223,9 +223,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
 
 template <typename T> hipError_t go(Epilogue e, const Product &p, int splits, hipStream_t st)
 {
-    const int64_t rows = p.pairs    ? p.M
-                         : p.groups ? max_tile_rows(p.M, p.groups, kRows)
-                                    : (p.M + kRows - 1) / kRows;
+    const int64_t rows = p.pairs ? p.M : launch_tile_rows(p, kTileFew);
     const int64_t grid = rows * ((p.N + kCols - 1) / kCols) * splits;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
     auto with = [&](auto kernel, int waves) {

@@ -8,8 +8,7 @@ namespace {
 template <typename T, Epilogue E> hipError_t pick(TileSize t, const Product &p, hipStream_t st)
 {
     using namespace mm;
-    const int64_t rows = p.groups ? max_tile_rows(p.M, p.groups, tile_rows(t) * p.split) * p.split
-                                  : (p.M + tile_rows(t) - 1) / tile_rows(t);
+    const int64_t rows = launch_tile_rows(p, t);
     const bool async = chunked(kNT, p);
     if (t == kTileLarge) return async ? launch<T, kNT, E, Large, true>(p, rows, st) : hipErrorInvalidValue;
     if (t == kTileMid)

@@ -300,3 +300,23 @@ def test_few_rows_an_expert(dev, dtype, N, k, E, D, F):
     out = dense.experts(**s, act="silu", residual=s["x"])
     ref, bound = forms(s, "silu", s["x"])
     check(out, ref, bound, "out")
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("N,k,E,D,F", [
+    (127, 1, 16, 1024, 520), (128, 2, 32, 512, 512), (116, 1, 13, 515, 777), (70, 2, 24, 264, 1032),
+    (40, 1, 12, 136, 1100), (1300, 2, 9, 128, 264), (2600, 2, 5, 1024, 2056),
+])
+def test_gradients_where_one_expert_takes_most_rows(dev, dtype, N, k, E, D, F):
+    # few rows an expert on average (the first five), tiles of 32, 128 and 256; a workspace that holds no number
+    s, g = case(44, N, k, E, D, F, dtype, dev, empty=0.0)
+    loads = torch.full((N * k,), E // 2, dtype=torch.int32)
+    loads[:E - 1] = torch.tensor([e for e in range(E) if e != E // 2], dtype=torch.int32)
+    s["idx"] = loads[torch.randperm(N * k, generator=g)].view(N, k).to(dev)
+    dout = torch.randn(N, D, generator=g).to(dtype).to(dev)
+    ws = torch.full((dense.experts_workspace_bytes(N, k, E, D, F, keep=True),), 255, dtype=torch.uint8, device=dev)
+    dense.experts(**s, act="silu", keep=True, workspace=ws)
+    got = dense.experts_bwd(s["x"], s["idx"], s["w"], s["W1"], s["W2"], s["b2"], dout, act="silu", workspace=ws)
+    ref, off = gradients(s, "silu", dout, None)
+    for name, t in zip(("x", "w", "W1", "b1", "W2", "b2"), got):
+        check(t, ref[name], off[name], f"d{name}")
