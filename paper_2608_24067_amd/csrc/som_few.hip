@@ -84,7 +84,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
     const short *a = static_cast<const short *>(p.A) + (Z ? 0 : at * p.lda + 8 * g);
     const int n_from = nt * kCols, n0 = N >= kCols ? min(n_from, N - kCols) : 0;
     const int last = N - n0 - 8;  // where the last lane's eight columns start (negative: fewer than 8 in all)
-    const int cols = min(8, N - n0 - 8 * c);
+    const int cols = last >= 0 ? 8 : min(8, N - n0 - 8 * c);  // of a lane's eight (moved back: all)
     const short *b = static_cast<const short *>(p.B) + (int64_t)e * p.strideB + 8 * (int64_t)g * p.ldb + n0 +
                      (last >= 0 ? min(8 * c, last) : cols > 0 ? 8 * c : 0);
 

@@ -243,3 +243,17 @@ def test_linear_where_the_tile_changes(dev, dtype, N, K, M, pad, offset, a):
     y = act(a, z) + wide(r)
     check(out, y, LIP * err + 2.0 ** -20 * (z.abs().clamp_min(1) if a != "none" else 0) + 2.0 ** -23 * (z.abs() + wide(r).abs()),
           "y")
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("N,K,M", [(5, 5, 12), (3, 4, 64), (16, 7, 100), (1, 1, 8), (40, 3, 127), (300, 2, 31),
+                                   (2, 6, 9), (17, 1, 128), (8, 7, 200)])
+def test_fewer_than_eight_features(dev, dtype, N, K, M):
+    # widths below a tile, whose last lanes' columns are read from further back
+    for pad, offset in ((0, 0), (3, 1)):
+        x, W, b, r, _ = case(23, N, K, M, dtype, dev, pad, offset)
+        out = dense.linear(x, W, b, residual=r, act="silu")
+        z = wide(x) @ wide(W) + wide(b)
+        err = sums(K + 1, wide(x).abs() @ wide(W).abs() + wide(b).abs())
+        y = act("silu", z) + wide(r)
+        check(out, y, LIP * err + 2.0 ** -20 * z.abs().clamp_min(1) + 2.0 ** -23 * (z.abs() + wide(r).abs()), "y")

@@ -320,3 +320,13 @@ def test_gradients_where_one_expert_takes_most_rows(dev, dtype, N, k, E, D, F):
     ref, off = gradients(s, "silu", dout, None)
     for name, t in zip(("x", "w", "W1", "b1", "W2", "b2"), got):
         check(t, ref[name], off[name], f"d{name}")
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("D,F", [(3, 12), (5, 64), (7, 100), (12, 5), (64, 3), (100, 7), (7, 8), (300, 5), (6, 700)])
+@pytest.mark.parametrize("N", [2, 40])  # few pairs, and ordered ones
+def test_fewer_than_eight_features(dev, dtype, N, D, F):
+    s, g = case(45, N, 2, 9, D, F, dtype, dev, empty=0.0)
+    out = dense.experts(**s, act="gelu", residual=s["x"])
+    ref, bound = forms(s, "gelu", s["x"])
+    check(out, ref, bound, "out")
