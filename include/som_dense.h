@@ -159,8 +159,9 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
  *                  the tensor itself. The arrays are read during the call.
  *   norm           device fp32 [1], written: the norm before scaling.
  *   workspace      device, som_clip_workspace_bytes(sizes, count) bytes, 256-byte aligned.
- * Squares are summed in fp64 in a fixed order. A norm that is infinite or NaN scales nothing:
- * outputs equal their tensors, and the caller sees it in `norm`. max_norm > 0 and finite.
+ * Squares are summed in fp64 in a fixed order. A norm that is infinite (also by its rounding to
+ * fp32) or NaN scales nothing: outputs equal their tensors, and the caller sees it in `norm`.
+ * max_norm > 0 and finite.
  */
 size_t som_clip_workspace_bytes(const int64_t *sizes, int64_t count);
 

@@ -84,10 +84,11 @@ __global__ __launch_bounds__(kThreads) void k_squares(const ClipTable t, double 
     if (threadIdx.x == 0) partial[chunk] = s;
 }
 
-// The scale of a norm; an infinite or NaN norm, or one within the limit, scales nothing.
+// The scale of a norm; an infinite or NaN norm, or one within the limit, scales nothing. Infinite is
+// what the caller reads as such: the fp32 value of the fp64 norm.
 __device__ inline float scale_of(double r, float max_norm)
 {
-    return r > (double)max_norm && r < __builtin_inf() ? (float)((double)max_norm / r) : 1.0f;
+    return r > (double)max_norm && (float)r < __builtin_inff() ? (float)((double)max_norm / r) : 1.0f;
 }
 
 __global__ __launch_bounds__(1024) void k_norm(const double *__restrict__ partial, int64_t n, float max_norm,

@@ -76,3 +76,14 @@ def test_same_bits_on_repeats(dev):
     runs = [dense.clip(ts, 0.5, out=[torch.empty_like(t) for t in ts]) for _ in range(3)]
     for outs, norm in runs[1:]:
         assert torch.equal(norm, runs[0][1]) and all(torch.equal(a, b) for a, b in zip(outs, runs[0][0]))
+
+
+@pytest.mark.parametrize("count,each", [(4, 3), (300, 3), (2, 5_000_000)])
+def test_norm_beyond_fp32_scales_nothing(dev, count, each):
+    # finite values whose norm is none: two launches, three, and many chunks
+    ts = [torch.full((each,), 3e38, device=dev) for _ in range(count)]
+    outs, norm = dense.clip(ts, 1.0, out=[torch.empty_like(t) for t in ts])
+    assert math.isinf(float(norm)) and all(torch.equal(t, o) for t, o in zip(ts, outs))
+    before = ts[0].clone()
+    dense.clip(ts, 1.0)
+    assert all(torch.equal(t, before) for t in ts)
