@@ -85,14 +85,19 @@ __global__ __launch_bounds__(kThreads) void k_squares(const ClipTable t, double 
 }
 
 // The scale of a norm; an infinite or NaN norm, or one within the limit, scales nothing. Infinite is
-// what the caller reads as such: the fp32 value of the fp64 norm.
-__device__ inline float scale_of(double r, float max_norm)
+// what the caller reads as such: the fp32 value of the fp64 norm. The scale is an fp32 value, unless
+// that would be subnormal and lose bits (norms of 1e36 and more).
+constexpr double kLeastNormal = 0x1p-126;
+
+__device__ inline double scale_of(double r, float max_norm)
 {
-    return r > (double)max_norm && (float)r < __builtin_inff() ? (float)((double)max_norm / r) : 1.0f;
+    if (!(r > (double)max_norm && (float)r < __builtin_inff())) return 1.0;
+    const double c = (double)max_norm / r;
+    return c < kLeastNormal ? c : (double)(float)c;
 }
 
 __global__ __launch_bounds__(1024) void k_norm(const double *__restrict__ partial, int64_t n, float max_norm,
-                                               float *__restrict__ norm, float *__restrict__ scale)
+                                               float *__restrict__ norm, double *__restrict__ scale)
 {
     __shared__ double lds[16];
     double s = 0;
@@ -105,28 +110,39 @@ __global__ __launch_bounds__(1024) void k_norm(const double *__restrict__ partia
     }
 }
 
-template <typename T> __device__ inline void scaled(const void *in, void *out, int64_t from, int64_t to, float c)
+// times: the value to write for one read.
+template <typename T, typename F>
+__device__ inline void scaled_by(const void *in, void *out, int64_t from, int64_t to, F times)
 {
     constexpr int V = 16 / sizeof(T);
     typedef T vec __attribute__((ext_vector_type(V)));
     typedef vec any __attribute__((aligned(sizeof(T))));
     T *o = static_cast<T *>(out);
-    if (c == 1.0f && in == out) return;
     over(static_cast<const T *>(in), from, to, [&](int64_t i, int n, const float *v) {
         if (n == V) {
             vec x;
 #pragma unroll
-            for (int q = 0; q < V; ++q) x[q] = (T)(c == 1.0f ? v[q] : v[q] * c);
+            for (int q = 0; q < V; ++q) x[q] = (T)times(v[q]);
             __builtin_nontemporal_store(x, reinterpret_cast<any *>(o + i));
         } else {
 #pragma unroll
             for (int q = 0; q < V; ++q)
-                if (q < n) o[i + q] = (T)(c == 1.0f ? v[q] : v[q] * c);
+                if (q < n) o[i + q] = (T)times(v[q]);
         }
     });
 }
 
-__global__ __launch_bounds__(kThreads) void k_scale(const ClipTable t, const float *__restrict__ scale,
+template <typename T> __device__ inline void scaled(const void *in, void *out, int64_t from, int64_t to, double scale)
+{
+    const float c = (float)scale;
+    if (scale < kLeastNormal) {
+        scaled_by<T>(in, out, from, to, [&](float v) { return (float)((double)v * scale); });
+    } else if (c != 1.0f || in != out) {
+        scaled_by<T>(in, out, from, to, [&](float v) { return c == 1.0f ? v : v * c; });
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void k_scale(const ClipTable t, const double *__restrict__ scale,
                                                     const double *__restrict__ partial, int64_t n, float max_norm,
                                                     float *__restrict__ norm)
 {
@@ -135,7 +151,7 @@ __global__ __launch_bounds__(kThreads) void k_scale(const ClipTable t, const flo
     // results pass by (372 million values in three types: 1,333 -> 1,315 us).
     const int chunk = (int)(gridDim.x - 1 - blockIdx.x), i = tensor_of(t, chunk);
     const int64_t from = (int64_t)(chunk - t.first[i]) * t.chunk, to = min(t.size[i], from + t.chunk);
-    float c;
+    double c;
     if (scale) {
         c = *scale;
     } else {
@@ -159,13 +175,13 @@ hipError_t launch_squares(const ClipTable &t, double *partial, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_norm(const double *partial, int64_t n, float max_norm, float *norm, float *scale, hipStream_t st)
+hipError_t launch_norm(const double *partial, int64_t n, float max_norm, float *norm, double *scale, hipStream_t st)
 {
     hipLaunchKernelGGL(k_norm, dim3(1), dim3(1024), 0, st, partial, n, max_norm, norm, scale);
     return hipGetLastError();
 }
 
-hipError_t launch_scale(const ClipTable &t, const float *scale, const double *partial, int64_t n, float max_norm,
+hipError_t launch_scale(const ClipTable &t, const double *scale, const double *partial, int64_t n, float max_norm,
                         float *norm, hipStream_t st)
 {
     if (t.first[t.count] == 0) return hipSuccess;

@@ -197,10 +197,10 @@ struct ClipTable {
 };
 
 hipError_t launch_squares(const ClipTable &t, double *partial, hipStream_t st);
-hipError_t launch_norm(const double *partial, int64_t n, float max_norm, float *norm, float *scale, hipStream_t st);
+hipError_t launch_norm(const double *partial, int64_t n, float max_norm, float *norm, double *scale, hipStream_t st);
 // scale: what launch_norm wrote; or null and the n partial sums, which every workgroup then adds
 // itself (the first also writes norm).
-hipError_t launch_scale(const ClipTable &t, const float *scale, const double *partial, int64_t n, float max_norm,
+hipError_t launch_scale(const ClipTable &t, const double *scale, const double *partial, int64_t n, float max_norm,
                         float *norm, hipStream_t st);
 
 }  // namespace som

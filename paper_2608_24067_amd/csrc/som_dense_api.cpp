@@ -598,7 +598,7 @@ som_status som_clip(const void *const *tensors, void *const *outs, const int64_t
     const som_status st = check_workspace(who, workspace, workspace_bytes, som_clip_workspace_bytes(sizes, count));
     if (st != SOM_OK) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    float *scale = static_cast<float *>(workspace);
+    double *scale = static_cast<double *>(workspace);
     double *partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + 256);
     // Few chunks: one launch less, each workgroup of the last pass adds them for itself.
     const bool few = chunks_total > 0 && chunks_total <= 4096 && count <= som::kClipTensors;

@@ -87,3 +87,16 @@ def test_norm_beyond_fp32_scales_nothing(dev, count, each):
     before = ts[0].clone()
     dense.clip(ts, 1.0)
     assert all(torch.equal(t, before) for t in ts)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("count", [1, 60])
+@pytest.mark.parametrize("limit", [1.0, 1e-3, 1e-5])
+def test_scales_below_the_smallest_normal(dev, dtype, count, limit):
+    # limit / norm is a subnormal fp32 value of few bits, or none; the results are ordinary values
+    ts = tensors(44, [700] * count, dev, scale=1e36, types=[dtype])
+    outs, norm = dense.clip(ts, limit, out=[torch.empty_like(t) for t in ts])
+    ref = math.sqrt(sum(float(wide(t).square().sum()) for t in ts))
+    assert abs(float(norm) - ref) <= 2.0 ** -23 * ref
+    for t, o in zip(ts, outs):
+        check(o, wide(t) * (limit / ref), 2.0 ** -23 * wide(t).abs() * (limit / ref), "scaled")
