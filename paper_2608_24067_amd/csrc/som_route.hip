@@ -65,10 +65,11 @@ template <int LPR> __device__ inline float sum_f32(float v)
 
 constexpr float kMost = 3.402823466e38f;
 
-// What a unit is ranked by: logit + bias (fp32, one rounding; -0 + 0 is 0), -inf for a closed one.
+// What a unit is ranked by: logit + bias (fp32, one rounding; + 0 makes -0, which a logit and a bias
+// of -0 add up to, the 0 that it equals), -inf for a closed one.
 __device__ inline float rank_key(float logit, float bias)
 {
-    const float s = logit + bias;
+    const float s = logit + bias + 0.0f;
     return logit > -__builtin_inff() && s > -__builtin_inff() ? s : -__builtin_inff();  // false for NaN
 }
 

@@ -160,3 +160,19 @@ def test_many_rows_and_no_rows(dev):
     assert idx.shape == (0, 3) and not counts.any()
     assert dense.route_bwd(l[:0], idx, w).shape == (0, 48)
     assert U[torch.float16] and TINY[torch.float16]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,groups", [(24, 1), (24, 4), (300, 1), (300, 10), (2000, 8)])
+def test_zeros_of_both_signs_are_equal(dev, dtype, E, groups):
+    l = torch.zeros(4, E, dtype=dtype, device=dev)
+    l[:, ::2] = -0.0
+    l[3] = -0.0
+    bias = torch.full((E,), -0.0, device=dev)
+    bias[E // 2] = 0.0
+    how = dict(groups=groups, group_top=max(1, groups // 2))
+    for b in (bias, None):
+        idx, w = dense.route(l, 5, bias=b, **how)
+        ri, rw = route(l, 5, b, **how)
+        assert torch.equal(idx.cpu(), ri)
+        close(w, rw, "weights")
