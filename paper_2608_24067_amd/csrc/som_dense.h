@@ -13,6 +13,18 @@ namespace som {
 
 som_status set_error(som_status st, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 
+// A launch of `blocks` workgroups, numbered by block_number. HIP takes fewer than 2^32 threads along x,
+// so beyond 2^21 workgroups (of 1,024 threads at most) they go on along y; the last row of them
+// reaches past `blocks`, which every kernel launched so checks. 0 blocks along x: more than a grid holds.
+constexpr int64_t kBlocksAlongX = (int64_t)1 << 21;
+
+inline dim3 grid_of(int64_t blocks)
+{
+    if (blocks <= kBlocksAlongX) return dim3((unsigned)blocks);
+    const int64_t rows = (blocks + kBlocksAlongX - 1) / kBlocksAlongX;
+    return rows < 65536 ? dim3((unsigned)kBlocksAlongX, (unsigned)rows) : dim3(0);
+}
+
 // ---------------------------------------------------------------- matrix products
 
 // One tile row of a grouped product: the rows [row, end) of the ordered pairs belong to

@@ -6,6 +6,7 @@
 namespace som {
 namespace {
 
+using mm::block_number;
 using mm::load4;
 using mm::store4;
 
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(256) void k_weight_grad(const float *__restrict__ p
                                                      int64_t N, int k, int64_t D, T *__restrict__ dw)
 {
     const int lane = threadIdx.x % 64;
-    const int64_t n = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    const int64_t n = block_number() * 4 + threadIdx.x / 64;
     if (n >= N) return;
     for (int j = 0; j < k; ++j) {
         const int p = pos[n * k + j];
@@ -388,13 +389,13 @@ hipError_t launch_weight_grad(bool bf16, const float *parts, int64_t n_parts, co
                               const void *b2, const void *dout, int64_t lddo, int64_t N, int32_t k, int64_t D,
                               void *dw, hipStream_t st)
 {
-    const unsigned grid = (unsigned)((N + 3) / 4);
+    const dim3 grid = grid_of((N + 3) / 4);  // fewer than 2^28
     if (bf16)
-        hipLaunchKernelGGL(k_weight_grad<__bf16>, dim3(grid), dim3(256), 0, st, parts, n_parts, pos, idx,
+        hipLaunchKernelGGL(k_weight_grad<__bf16>, grid, dim3(256), 0, st, parts, n_parts, pos, idx,
                            static_cast<const __bf16 *>(b2), static_cast<const __bf16 *>(dout), lddo, N, k, D,
                            static_cast<__bf16 *>(dw));
     else
-        hipLaunchKernelGGL(k_weight_grad<_Float16>, dim3(grid), dim3(256), 0, st, parts, n_parts, pos, idx,
+        hipLaunchKernelGGL(k_weight_grad<_Float16>, grid, dim3(256), 0, st, parts, n_parts, pos, idx,
                            static_cast<const _Float16 *>(b2), static_cast<const _Float16 *>(dout), lddo, N, k, D,
                            static_cast<_Float16 *>(dw));
     return hipGetLastError();

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
     __shared__ __align__(16) float lds[kWaves][kRows][kCols + 4];
     const int nn = (int)((p.N + kCols - 1) / kCols);
     const int nm = p.pairs ? (int)p.M : p.groups ? *p.n_tiles : (int)((p.M + kRows - 1) / kRows);
-    const int64_t t = blockIdx.x;
+    const int64_t t = block_number();
     if (t >= (int64_t)nm * nn * splits) return;
     const int split = (int)(t % splits), nt = (int)(t / splits % nn), mt = (int)(t / splits / nn);
     int e = 0, m0 = mt * kRows, m1 = min((int)p.M, m0 + kRows);
@@ -224,16 +224,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
 template <typename T> hipError_t go(Epilogue e, const Product &p, int splits, hipStream_t st)
 {
     const int64_t rows = p.pairs ? p.M : launch_tile_rows(p, kTileFew);
-    const int64_t grid = rows * ((p.N + kCols - 1) / kCols) * splits;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    const int64_t blocks = rows * ((p.N + kCols - 1) / kCols) * splits;
+    const dim3 grid = grid_of(blocks);
+    if (grid.x == 0) return hipErrorInvalidValue;
     auto with = [&](auto kernel, int waves) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * waves), 0, st, p, splits);
+        hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, st, p, splits);
         return hipGetLastError();
     };
     if (p.z_parts) return with(k_few<T, kPairs, 8, true>, 8);
     // Eight waves bring a tile's part of the matrix at once; from two tiles a CU on four do, so that
     // one workgroup's loads run while the other adds up.
-    if (grid >= 512)
+    if (blocks >= 512)
         return e == kLinear ? with(k_few<T, kLinear, 4>, 4)
                : e == kInner ? with(k_few<T, kInner, 4>, 4)
                              : with(k_few<T, kPairs, 4>, 4);

@@ -38,6 +38,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 static __device__ __align__(64) const uint4 g_zero[1] = {{0, 0, 0, 0}};
 
+// The workgroup's number in a launch by grid_of.
+__device__ inline int64_t block_number() { return (int64_t)blockIdx.y * kBlocksAlongX + blockIdx.x; }
+
 constexpr int kBK = 32;  // reduction steps of a tile
 
 __device__ inline f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -424,7 +427,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
         const int64_t per = (int64_t)nm * nn;
         // Experts take unequal numbers of rows: their tiles go round the XCDs, not each expert's to one.
         const int64_t total = per * max(1, p.groups);
-        const int64_t t = p.off ? (blockIdx.x < total ? (int64_t)blockIdx.x : -1) : tile_of(blockIdx.x, total);
+        const int64_t b = block_number(), t = p.off ? (b < total ? b : -1) : tile_of(b, total);
         if (t < 0) return;
         e = (int)(t / per);
         tile_place(t % per, nm, nn, mt, nt);
@@ -441,7 +444,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
         }
     } else {
         const int nm = p.groups ? *p.n_tiles * p.split : (int)((p.M + S::BM - 1) / S::BM);
-        const int64_t t = tile_of(blockIdx.x, (int64_t)nm * nn);
+        const int64_t t = tile_of(block_number(), (int64_t)nm * nn);
         if (t < 0) return;
         tile_place(t, nm, nn, mt, nt);
         m0 = mt * S::BM;
@@ -863,8 +866,8 @@ hipError_t launch(const Product &p, int64_t tile_rows_total, hipStream_t st)
     const int64_t nn = (p.N + S::BN - 1) / S::BN;
     const int64_t total = tile_rows_total * nn;
     if (total <= 0) return hipSuccess;
-    const int64_t grid = (total + 7) / 8 * 8;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 grid = grid_of((total + 7) / 8 * 8);
+    if (grid.x == 0) return hipErrorInvalidValue;
     // The attribute belongs to the function on each device; setting it again changes nothing.
     static std::atomic<uint64_t> done{0};
     int dev = 0;
@@ -874,7 +877,7 @@ hipError_t launch(const Product &p, int64_t tile_rows_total, hipStream_t st)
         if (err != hipSuccess) return err;
         if (dev <= 63) done.fetch_or(1ull << dev);
     }
-    hipLaunchKernelGGL((k_product<T, L, EPI, S, ASYNC, MAP>), dim3((unsigned)grid), dim3(S::NT), bytes, st, p);
+    hipLaunchKernelGGL((k_product<T, L, EPI, S, ASYNC, MAP>), grid, dim3(S::NT), bytes, st, p);
     return hipGetLastError();
 }
 

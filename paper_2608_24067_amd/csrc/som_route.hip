@@ -11,6 +11,7 @@
 namespace som {
 namespace {
 
+using mm::block_number;
 using mm::exp_f32;
 using mm::exp_short;
 using mm::load4;
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void k_route(const RouteArgs a)
     __shared__ uint32_t best[kRows][SOM_ROUTE_MAX_GROUPS];
     __shared__ unsigned long long kept[kRows];
     const int sub = threadIdx.x % LPR, slot = threadIdx.x / LPR;
-    const int64_t row = (int64_t)blockIdx.x * kRows + slot;
+    const int64_t row = block_number() * kRows + slot;
     const bool in = row < a.N;
     const T *p = static_cast<const T *>(a.logits) + (in ? row : 0) * a.ldl;
 
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(kThreads) void k_route(const RouteArgs a)
         store_weight(a.weight_type, a.weights, row * a.k + sub, s);
     }
     // The counts: one workgroup counts its own rows; of more, the first clears them for k_counts.
-    if (a.counts && blockIdx.x == 0) {
+    if (a.counts && block_number() == 0) {
         for (int i = threadIdx.x; i < a.E; i += kThreads) a.counts[i] = 0;
         if (gridDim.x == 1) {
             __threadfence_block();
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const RouteArgs a)
 {
     constexpr int kRows = kThreads / LPR;
     const int sub = threadIdx.x % LPR, slot = threadIdx.x / LPR;
-    const int64_t row = (int64_t)blockIdx.x * kRows + slot;
+    const int64_t row = block_number() * kRows + slot;
     const bool in = row < a.N;
     const int64_t at = in ? row : 0;
     const T *p = static_cast<const T *>(a.logits) + at * a.ldl;
@@ -421,9 +422,8 @@ int rows_of_one(const RouteArgs &a) { return kThreads / lanes_of(a); }
 template <typename T, bool BWD, bool BIAS> hipError_t pick(const RouteArgs &a, hipStream_t st)
 {
     auto go = [&](auto kernel) {
-        const int64_t rows = rows_of_one(a), grid = (a.N + rows - 1) / rows;
-        if (grid > INT32_MAX) return hipErrorInvalidValue;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, st, a);
+        const int64_t rows = rows_of_one(a);
+        hipLaunchKernelGGL(kernel, grid_of((a.N + rows - 1) / rows), dim3(kThreads), 0, st, a);
         return hipGetLastError();
     };
     if constexpr (BWD) {

@@ -15,4 +15,13 @@ int64_t launched(int64_t P, int32_t E, int32_t plan, int32_t tile, int32_t *spli
     p.split = *split = som::tiles_in_row(static_cast<som::TileSize>(plan), static_cast<som::TileSize>(tile));
     return som::launch_tile_rows(p, static_cast<som::TileSize>(tile));
 }
+
+// The grid of a launch of `blocks` workgroups; returns the number of the last one in it.
+int64_t grid(int64_t blocks, int64_t *x, int64_t *y)
+{
+    const dim3 g = som::grid_of(blocks);
+    *x = g.x;
+    *y = g.y;
+    return (int64_t)(g.y - 1) * som::kBlocksAlongX + g.x - 1;  // block_number there
+}
 }

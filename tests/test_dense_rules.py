@@ -55,3 +55,17 @@ def test_the_grid_holds_every_tile_row_of_a_plan(dense_rules, plan, tile):
         assert rows >= planned * split.value, (loads, rows, planned)
     # 16 experts, one with 97 of 127 pairs: 22 tile rows of 16
     assert dense_rules.launched(127, 16, FEW, SMALL, ctypes.byref(split)) >= 22
+
+
+def test_launches_stay_within_the_threads_of_a_grid(dense_rules):
+    x, y = ctypes.c_int64(), ctypes.c_int64()
+    dense_rules.grid.argtypes = [ctypes.c_int64, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64)]
+    dense_rules.grid.restype = ctypes.c_int64
+    along = 1 << 21
+    for blocks in (1, 8, 255, along - 1, along, along + 1, 1 << 22, (1 << 24) + 8, 1 << 28, 65535 * along):
+        last = dense_rules.grid(blocks, ctypes.byref(x), ctypes.byref(y))
+        assert x.value * 1024 < 1 << 32 and 1 <= y.value < 65536
+        assert blocks <= last + 1 == x.value * y.value < blocks + along, blocks
+        assert y.value == 1 or x.value == along
+    dense_rules.grid(65535 * along + 1, ctypes.byref(x), ctypes.byref(y))
+    assert x.value == 0  # refused

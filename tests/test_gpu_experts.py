@@ -330,3 +330,51 @@ def test_fewer_than_eight_features(dev, dtype, N, D, F):
     out = dense.experts(**s, act="gelu", residual=s["x"])
     ref, bound = forms(s, "gelu", s["x"])
     check(out, ref, bound, "out")
+
+
+def test_weights_gradient_of_more_rows_than_a_grid_holds_along_x(dev):
+    # 64 threads a row; whole numbers throughout, so that every value is exact
+    N, D = (1 << 26) + 3, 8
+    x = torch.randint(-2, 3, (N, D), dtype=torch.int8, device=dev).half()
+    dout = torch.randint(-2, 3, (N, D), dtype=torch.int8, device=dev).half()
+    idx = torch.randint(0, 2, (N, 1), dtype=torch.int32, device=dev)
+    w = torch.ones(N, 1, dtype=torch.float16, device=dev)
+    eye = torch.eye(D, dtype=torch.float16, device=dev).expand(2, D, D).contiguous()
+    W1 = eye * torch.tensor([1.0, 2.0], device=dev).half()[:, None, None]
+    ws = torch.empty(dense.experts_workspace_bytes(N, 1, 2, D, D, keep=True), dtype=torch.uint8, device=dev)
+    out = dense.experts(x, idx, w, W1, None, eye, None, act="none", keep=True, workspace=ws)
+    times = (1 + idx).half()
+    assert torch.equal(out, x * times)
+    got = [torch.full_like(x, float("nan")), torch.full_like(w, float("nan"))] + [None] * 4
+    dense.experts_bwd(x, idx, w, W1, eye, None, dout, act="none", out=got, workspace=ws)
+    assert torch.equal(got[0], dout * times)
+    assert torch.equal(got[1], (out * dout).sum(1, keepdim=True))
+    del x, dout, idx, w, ws, out, times, got
+    torch.cuda.empty_cache()
+
+
+def test_gradients_of_more_tiles_than_a_grid_holds_along_x(dev):
+    # 1,024 experts of 2^14 tiles each, two of them met
+    N, E, D, F = 4, 1024, 1, 1 << 21
+    g = torch.Generator().manual_seed(46)
+    W1, W2 = torch.zeros(E, D, F, dtype=torch.float16, device=dev), torch.zeros(E, F, D, dtype=torch.float16, device=dev)
+    for e in (5, E - 1):
+        W1[e, 0] = torch.randint(-2, 3, (F,), generator=g).half()
+        W2[e, :, 0] = torch.randint(-1, 2, (F,), generator=g).half() * 2.0 ** -10
+    idx = torch.tensor([[5], [E - 1], [E - 1], [-1]], dtype=torch.int32, device=dev)
+    x = torch.tensor([[1.0], [2.0], [-1.0], [1.0]], device=dev).half()
+    dout = torch.tensor([[2.0], [-1.0], [1.0], [3.0]], device=dev).half()
+    w = torch.ones(N, 1, dtype=torch.float16, device=dev)
+    ws = torch.empty(dense.experts_workspace_bytes(N, 1, E, D, F, keep=True), dtype=torch.uint8, device=dev)
+    dense.experts(x, idx, w, W1, None, W2, None, act="none", keep=True, workspace=ws)
+    grads = [None, None, torch.full_like(W1, float("nan")), None, torch.full_like(W2, float("nan")), None]
+    dense.experts_bwd(x, idx, w, W1, W2, None, dout, act="none", out=grads, workspace=ws)
+    # by hand: dW1 = x (dout W2), dW2 = (x W1) dout, all exact
+    dW1, dW2 = grads[2], grads[4]
+    assert torch.equal(dW1[5, 0], 2 * W2[5, :, 0]) and torch.equal(dW2[5, :, 0], 2 * W1[5, 0])
+    assert torch.equal(dW1[E - 1, 0], -3 * W2[E - 1, :, 0]) and torch.equal(dW2[E - 1, :, 0], -3 * W1[E - 1, 0])
+    for t in (dW1, dW2):
+        t[5], t[E - 1] = 0, 0
+        assert not t.any()
+    del W1, W2, dW1, dW2, grads, ws
+    torch.cuda.empty_cache()

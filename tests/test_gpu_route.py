@@ -176,3 +176,29 @@ def test_zeros_of_both_signs_are_equal(dev, dtype, E, groups):
         ri, rw = route(l, 5, b, **how)
         assert torch.equal(idx.cpu(), ri)
         close(w, rw, "weights")
+
+
+@pytest.mark.parametrize("N,E", [((1 << 26) + 5, 65), ((1 << 28) + 3, 4)])
+def test_more_threads_than_a_grid_holds_along_x(dev, N, E):
+    # 64 threads a row, or 16: 2^32 of them. One logit of every row stands out
+    best = torch.arange(N, dtype=torch.int32, device=dev).bitwise_xor_(N >> 3).remainder_(E)
+    l = torch.zeros(N, E, dtype=torch.float16, device=dev)
+    l.scatter_(1, best[:, None].long(), 3.0)
+    counts = torch.empty(E, dtype=torch.int32, device=dev)
+    idx, w = dense.route(l, 1, renorm=False, counts=counts)
+    assert torch.equal(idx[:, 0], best)
+    p = math.exp(3) / (math.exp(3) + E - 1)
+    assert float((w - p).abs().max()) <= 2.0 ** -11 * p + 2.0 ** -17
+    assert torch.equal(counts, torch.bincount(best, minlength=E).int())
+    dw = torch.ones(N, 1, dtype=torch.float16, device=dev)
+    dl = dense.route_bwd(l, idx, dw, renorm=False, out=torch.full_like(l, float("nan")))
+    q = p / math.exp(3)  # the others' share: their gradient is -p q, the best one's p (1 - p)
+    top = torch.zeros(N, dtype=torch.float16, device=dev)
+    for a in range(0, N, 1 << 25):
+        b = slice(a, a + (1 << 25))
+        at = best[b, None].long()
+        top[b] = dl[b].gather(1, at)[:, 0]
+        assert float((dl[b].scatter(1, at, -p * q) + p * q).abs().max()) <= 2.0 ** -10 * p * q + 2.0 ** -17
+    assert float((top - p * (1 - p)).abs().max()) <= 2.0 ** -10 * p * (1 - p) + 2.0 ** -17
+    del l, dl, idx, w, best, dw, top
+    torch.cuda.empty_cache()
