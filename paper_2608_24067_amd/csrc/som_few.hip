@@ -205,7 +205,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
         }
         if (p.pre) store4(static_cast<T *>(p.pre) + (int64_t)m * p.ldp + n, skip, cnt, v);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = act_value(p.act, v[q]);
+        for (int q = 0; q < 4; ++q) v[q] = EPI == kLinear && p.out_f32 ? act_fine(p.act, v[q]) : act_value(p.act, v[q]);
         if (EPI == kInner) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] *= wr;

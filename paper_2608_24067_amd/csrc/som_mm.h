@@ -110,6 +110,18 @@ __device__ inline float act_value(int act, float z)
     return value;
 }
 
+// The activations where the result is fp32, to a few units in its last place (gelu far below zero:
+// z^2 of them, from the rounding of erfc's argument). silu by exp(-|z|), which does not overflow.
+__device__ inline float act_fine(int act, float z)
+{
+    if (act == SOM_ACT_GELU) return z * (0.5f * erfcf(z * -0.707106781f));
+    if (act == SOM_ACT_SILU) {
+        const float e = exp_f32(-fabsf(z));
+        return z * ((z < 0.0f ? e : 1.0f) / (1.0f + e));
+    }
+    return act_value(act, z);
+}
+
 // n (1 to 4) consecutive values at p, whose alignment is that of one element.
 template <typename T> __device__ inline void load4(const T *p, int n, float *v)
 {
@@ -720,7 +732,12 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
                 for (int r = 0; r < kTurns; ++r)
                     if (in[r]) store4(static_cast<T *>(p.pre) + (int64_t)m[r] * p.ldp + n, c0, c4, v[r]);
             }
-            if (p.act == SOM_ACT_GELU) {
+            if (EPI == kLinear && p.out_f32 && (p.act == SOM_ACT_GELU || p.act == SOM_ACT_SILU)) {
+#pragma unroll
+                for (int r = 0; r < kTurns; ++r)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[r][q] = act_fine(p.act, v[r][q]);
+            } else if (p.act == SOM_ACT_GELU) {
 #pragma unroll
                 for (int r = 0; r < kTurns; ++r)
 #pragma unroll

@@ -257,3 +257,19 @@ def test_fewer_than_eight_features(dev, dtype, N, K, M):
         err = sums(K + 1, wide(x).abs() @ wide(W).abs() + wide(b).abs())
         y = act("silu", z) + wide(r)
         check(out, y, LIP * err + 2.0 ** -20 * z.abs().clamp_min(1) + 2.0 ** -23 * (z.abs() + wide(r).abs()), "y")
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("a", ["gelu", "silu", "relu"])
+@pytest.mark.parametrize("N,K,M", [(1, 8, 2048), (40, 8, 2000), (100, 9, 20001), (700, 8, 2048), (2100, 8, 4000)])
+def test_activations_of_fp32_results(dev, dtype, a, N, K, M):
+    # z = W's first row, exactly; erfc(x) moves by 2 x^2 = z^2 of its argument's rounding (two of 2^-24),
+    # and the library functions are good to 16 units in the last place
+    W = torch.zeros(K, M, dtype=dtype, device=dev)
+    W[0] = torch.linspace(-12.5, 12.5, M).to(dtype)
+    x = torch.zeros(N, K, dtype=dtype, device=dev)
+    x[:, 0] = 1
+    y = dense.linear(x, W, act=a, out_dtype=torch.float32)
+    z = wide(W[0])
+    ref = act(a, z)
+    check(y, ref.expand(N, M), (2.0 ** -23 * (z * z + 16) * ref.abs()).expand(N, M), a)
