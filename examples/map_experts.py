@@ -35,9 +35,7 @@ class MapExperts:
 
         self.taken, self.units = taken, units
         self.W = prototypes.to(dt).to(device)
-        # the norms of the prototypes as they are held: the search's own pass over the widened codebook
-        norms = som.codebook_norms(self.W.float(), width, units)
-        self.gate_bias = (-0.5 * norms).float()
+        self.gate_bias = None  # of the last forward pass
         self.balance = torch.zeros(units, device=device)
         self.params = [self.W, normal(units, width, inner, scale=width ** -0.5), normal(units, inner, scale=0.02),
                        normal(units, inner, width, scale=inner ** -0.5 * 0.1), normal(units, width, scale=0.02)]
@@ -47,6 +45,8 @@ class MapExperts:
     def forward(self, x, keep=True):
         """(out, what the backward pass needs) of rows x [N, width]."""
         W, W1, b1, W2, b2 = self.params
+        # the norms of the prototypes as they are held now: the search's own pass over the widened codebook
+        self.gate_bias = (-0.5 * som.codebook_norms(W.float(), W.shape[0], W.shape[1])).float()
         scores = dense.linear(x, W, self.gate_bias, out_dtype=torch.float32)
         idx, w = dense.route(scores, self.taken, bias=self.balance, weights_dtype=x.dtype, counts=self.counts)
         need = dense.experts_workspace_bytes(x.shape[0], self.taken, self.units, W1.shape[1], W1.shape[2], keep)
@@ -56,19 +56,25 @@ class MapExperts:
         return out, (scores, idx, w)
 
     def backward(self, x, kept, dout):
-        """The parameters' gradients, in their order."""
+        """The gradients of the parameters, in their order, with the gate's bias held, and that of this bias."""
         W, W1, b1, W2, b2 = self.params
         scores, idx, w = kept
         _, dw, *expert_grads = dense.experts_bwd(x, idx, w, W1, W2, b2, dout, workspace=self.workspace)
         dscores = dense.route_bwd(scores, idx, dw, bias=self.balance).to(x.dtype)
-        _, dW, _ = dense.linear_bwd(x, W, dscores, out=(None, torch.empty_like(W), None))
-        return [dW] + expert_grads
+        dbias = torch.empty_like(self.gate_bias)
+        _, dW, _ = dense.linear_bwd(x, W, dscores, out=(None, torch.empty_like(W), dbias))
+        return [dW] + expert_grads + [dbias]
+
+    def gradients(self, x, kept, dout):
+        """The parameters' gradients: the bias is -|w|^2 / 2, whose share is -w times the bias's gradient."""
+        dW, *expert_grads, dbias = self.backward(x, kept, dout)
+        return [(dW.float() - self.W.float() * dbias).to(dW.dtype)] + expert_grads
 
     def step(self, x, target, rate=0.5, max_norm=1.0):
         """One step of gradient descent on the mean squared distance to target; returns (loss, gradients' norm)."""
         out, kept = self.forward(x)
         miss = out.float() - target.float()
-        grads = self.backward(x, kept, (miss * (2.0 / miss.shape[0])).to(x.dtype))
+        grads = self.gradients(x, kept, (miss * (2.0 / miss.shape[0])).to(x.dtype))
         grads, norm = dense.clip(grads, max_norm)
         for p, g in zip(self.params, grads):
             p.sub_((rate * g.float()).to(p.dtype))

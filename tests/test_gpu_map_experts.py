@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_2608_24067_amd.dense as dense
+from dense_ref import act
 
 pytestmark = pytest.mark.gpu
 
@@ -103,3 +104,34 @@ def test_captured_step_replays(dev):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, results())), i
+
+
+def test_the_gate_follows_its_prototypes(dev, example):
+    """Where the prototypes have changed, too, the best score is the best-matching unit's, and their gradient is that
+    of scores whose bias is -|w|^2 / 2."""
+    prototypes = 0.3 * torch.randn(48, 16, generator=torch.Generator().manual_seed(2))  # near: every share counts
+    model = example.MapExperts(prototypes, inner=72, seed=3)
+    for s in range(3):
+        model.step(*example.rows(200, prototypes, seed=50 + s))
+    with torch.no_grad():  # and further in place, each by another factor
+        model.W.mul_(torch.linspace(0.7, 1.4, 16, device=dev).bfloat16())
+    model.balance.zero_()
+    x, _ = example.rows(200, prototypes, seed=4)
+    out, kept = model.forward(x)
+    scores, idx, w = kept
+    xs, at = x.cpu().double(), idx.cpu().long()
+    p = model.params[0].cpu().double().requires_grad_(True)
+    d = (xs.unsqueeze(2) - p.detach().unsqueeze(0)).square().sum(1)
+    best = d.min(1).values
+    assert bool((d.gather(1, at[:, :1]).squeeze(1) - best <= 1e-3 * best).all())
+    dout = torch.randn(200, 48, generator=torch.Generator().manual_seed(6)).bfloat16().to(dev)
+    grads = model.gradients(x, kept, dout)
+    assert len(grads) == len(model.params)
+    s = xs @ p - 0.5 * p.square().sum(0)
+    W1, b1, W2, b2 = (t.cpu().double() for t in model.params[1:])
+    y = torch.stack([torch.bmm(act("gelu", torch.bmm(xs.unsqueeze(1), W1[at[:, j]]) + b1[at[:, j]].unsqueeze(1)),
+                               W2[at[:, j]]).squeeze(1) + b2[at[:, j]] for j in range(2)], 1)
+    wt = torch.softmax(s.gather(1, at), 1)
+    (ref,) = torch.autograd.grad((wt.unsqueeze(2) * y * dout.cpu().double().unsqueeze(1)).sum(), p)
+    # as in a step: some eight roundings of bf16, each spread over the sums that follow
+    assert float((grads[0].cpu().double() - ref).norm()) <= 8 * 2.0 ** -9 * float(ref.norm())
