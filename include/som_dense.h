@@ -129,8 +129,8 @@ som_status som_route_bwd(int32_t logit_type, const void *logits, int64_t ldl, co
  *   out       device [N, D], ldo >= D, written; it may be the residual's buffer (with ldo == ldr).
  *   keep      1: the workspace is laid out for the backward pass and keeps what it needs.
  *   workspace device, som_experts_workspace_bytes(N, k, E, D, F, keep) bytes, 256-byte aligned.
- * w act(...) is rounded to `type` between the two products; the experts' results are added in fp32,
- * in a fixed order.
+ * act(...) is rounded to `type` between the two products; the experts' results are weighted and
+ * added in fp32, in a fixed order.
  * 0 <= N; 1 <= k <= SOM_ROUTE_MAX_TAKEN; 1 <= E <= SOM_MAX_EXPERTS; N k < 2^30; 1 <= D, F < 2^24.
  */
 size_t som_experts_workspace_bytes(int64_t N, int32_t k, int64_t E, int64_t D, int64_t F, int32_t keep);
@@ -145,6 +145,8 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
  * db1, dW2, db2 shaped as the weights, each written whole unless NULL (an expert without rows gets
  * zeros). The workspace is the one that som_experts (keep = 1, the same arguments) left; it serves
  * any number of backward passes. The residual's gradient is dout itself. N == 0 writes zeros.
+ * dz = w dout W2^T act'(x W1 + b1) is rounded to `type` before the products that follow, and
+ * w act(...) for dW2; act' is taken at x W1 + b1 rounded to `type`.
  */
 som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32_t *idx, const void *w, const void *W1,
                            const void *W2, const void *b2, int32_t act, const void *dout, int64_t lddo, void *dX,

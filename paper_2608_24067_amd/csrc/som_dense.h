@@ -51,12 +51,12 @@ struct Product {
     int32_t split;          // workgroup tiles in the height of a tile row
     int32_t tile_height;    // rows of a tile row at most
     // Few pairs without a plan (launch_few): pair m is a tile of its own, for expert pairs[m], its
-    // row of A is m / pair_rows and its weight pair_w[m].
+    // row of A is m / pair_rows and its weight pair_w[m] (null: 1).
     const int32_t *pairs;
     const void *pair_w;
     int32_t pair_rows;
     // Then A may be z in fp32, z_parts arrays of M rows to be added up: what is multiplied is
-    // w act(z + z_bias[e]), rounded to the rows' type.
+    // act(z + z_bias[e]), rounded to the rows' type.
     int32_t z_parts;
     const void *z_bias;
     const int32_t *off;
@@ -65,14 +65,16 @@ struct Product {
     // Epilogue.
     const void *bias;
     int32_t bias_f32, act;
-    const void *res;        // residual, rows' type (kSlope: w act(pre) as the forward pass left it)
+    const void *res;        // residual, rows' type (kSlope: act(pre) as the forward pass left it)
     int64_t ldr;
     void *out;
     int64_t ldo;
     int32_t out_f32;
+    void *weighted;         // kInner: w act(...) too, as `out` is laid out; or null
     void *pre;              // value before the activation, rows' type: written by NN, read by kSlope
     int64_t ldp;
-    const float *w;         // a weight for each row (kInner, kPairs, kSlope; TN: of the reduction's rows)
+    const float *w;         // a weight for each row (kInner: with `weighted`; kPairs, kSlope; TN: of the
+                            // reduction's rows)
     float *parts;           // kSlope: per row and column part, the sum of act(pre) * product
     int64_t n_parts;
     void *db;               // TN: the column sums of B (each row times w), as bias_f32 says
@@ -81,9 +83,9 @@ struct Product {
 
 enum Epilogue {
     kLinear,  // out = res + act(acc + bias), pre = acc + bias
-    kInner,   // out = w * act(acc + bias), pre = acc + bias
-    kPairs,   // out (fp32) = acc + w * bias
-    kSlope,   // out = w * acc * act'(pre), parts = sum over columns of act(pre) * acc, act(pre) = res / w
+    kInner,   // out = act(acc + bias), weighted = w * act(acc + bias), pre = acc + bias
+    kPairs,   // out (fp32) = w * (acc + bias)
+    kSlope,   // out = w * acc * act'(pre), parts = sum over columns of act(pre) * acc, act(pre) = res
     kGrad     // TN: out = acc, db = column sums of B
 };
 

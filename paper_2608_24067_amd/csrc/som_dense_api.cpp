@@ -106,7 +106,7 @@ int grad_parts(int64_t N, int64_t K, int64_t M)
 // ---------------------------------------------------------------- experts
 
 struct ExpertsLayout {
-    size_t off, n_tiles, tiles, row, w, pos, counts, inner, y, pre, dz, parts, total;
+    size_t off, n_tiles, tiles, row, w, pos, counts, inner, y, pre, weighted, dz, parts, total;
     som::TileSize tile;
     int splits;  // of the second product's reduction (few rows)
     bool plan;   // the pairs are ordered by expert
@@ -159,6 +159,7 @@ ExpertsLayout experts_layout(int64_t N, int32_t k, int64_t E, int64_t D, int64_t
     L.inner = take(P * F * (L.inner_splits > 1 ? 4 * L.inner_splits : 2));
     L.y = take(L.splits * P * D * 4);
     L.pre = take(keep ? P * F * 2 : 0);
+    L.weighted = take(keep ? P * F * 2 : 0);
     L.dz = take(keep ? P * F * 2 : 0);
     L.parts = take(keep ? P * L.n_parts * 4 : 0);
     L.total = at;
@@ -167,7 +168,7 @@ ExpertsLayout experts_layout(int64_t N, int32_t k, int64_t E, int64_t D, int64_t
 
 struct Experts {
     som::PairPlan plan;
-    void *inner, *pre, *dz;
+    void *inner, *pre, *weighted, *dz;
     float *y, *parts;
 };
 
@@ -185,6 +186,7 @@ Experts carve(void *ws, const ExpertsLayout &L)
     x.inner = b + L.inner;
     x.y = reinterpret_cast<float *>(b + L.y);
     x.pre = b + L.pre;
+    x.weighted = b + L.weighted;
     x.dz = b + L.dz;
     x.parts = reinterpret_cast<float *>(b + L.parts);
     return x;
@@ -442,15 +444,14 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
         p.B = W1, p.ldb = F, p.strideB = D * F;
         p.N = F, p.K = D;
         p.bias = b1, p.strideBias = F, p.act = act;
-        p.w = x.plan.w;
         p.out = x.inner, p.ldo = F;
-        if (!L.plan) p.pairs = idx, p.pair_w = w, p.pair_rows = k;
+        if (!L.plan) p.pairs = idx, p.pair_rows = k;
         if (L.inner_splits > 1) {  // z in parts, without bias
             p.bias = nullptr;
             e = som::launch_few(bf16, som::kPairs, p, L.inner_splits, s);
             if (e != hipSuccess) return hip_fail(e, who);
         } else {
-            if (keep) p.pre = x.pre, p.ldp = F;
+            if (keep) p.pre = x.pre, p.ldp = F, p.weighted = x.weighted, p.w = x.plan.w;
             e = t == som::kTileFew ? som::launch_few(bf16, som::kInner, p, 1, s) : som::launch_nn(bf16, som::kInner, t, p, s);
             if (e != hipSuccess) return hip_fail(e, who);
         }
@@ -462,7 +463,7 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
         p.B = W2, p.ldb = D, p.strideB = D * F;
         p.N = D, p.K = F;
         p.bias = b2, p.strideBias = D;
-        p.w = x.plan.w;
+        if (L.plan) p.w = x.plan.w;
         p.out = x.y, p.ldo = D;
         if (!L.plan) p.pairs = idx, p.pair_w = w, p.pair_rows = 1;
         if (L.inner_splits > 1) p.z_parts = L.inner_splits, p.z_bias = b1, p.act = act;
@@ -547,7 +548,7 @@ som_status som_experts_bwd(int32_t type, const void *X, int64_t ldx, const int32
     }
     if (dW2 || db2) {
         Product p{};
-        p.A = x.inner, p.lda = F;
+        p.A = x.weighted, p.lda = F;
         p.B = dout, p.ldb = lddo, p.bmap = x.plan.row;
         p.M = F, p.N = D, p.split = 1;
         p.off = x.plan.off, p.groups = (int32_t)E;

@@ -88,8 +88,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
     const short *b = static_cast<const short *>(p.B) + (int64_t)e * p.strideB + 8 * (int64_t)g * p.ldb + n0 +
                      (last >= 0 ? min(8 * c, last) : cols > 0 ? 8 * c : 0);
 
-    // Eight values of w act(z + bias) from the parts of z (one pair: every lane's row is the same).
-    const float pair_w = p.pairs ? (float)static_cast<const T *>(p.pair_w)[m0] : 0.0f;
+    // Eight values of act(z + bias) from the parts of z (one pair: every lane's row is the same).
     auto inner8 = [&](int k0) {
         typedef T vec __attribute__((ext_vector_type(8)));
         vec r;
@@ -107,7 +106,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
                 if (p.z_bias) load4(static_cast<const T *>(p.z_bias) + (int64_t)e * K + k0 + h, n, b4);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r[h + i] = i < n ? (T)(pair_w * act_value(p.act, z[i] + b4[i])) : (T)0.0f;
+            for (int i = 0; i < 4; ++i) r[h + i] = i < n ? (T)act_value(p.act, z[i] + b4[i]) : (T)0.0f;
         }
         return __builtin_bit_cast(s16x8, r);
     };
@@ -191,24 +190,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_few(const Product p, int spl
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) sum += *reinterpret_cast<const f32x4 *>(&lds[w][r][q4]);
         float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-        const float wr = EPI == kLinear ? 1.0f : p.pairs ? (float)static_cast<const T *>(p.pair_w)[m] : p.w[m];
+        float wr = 1.0f;
+        if (EPI == kPairs || (EPI == kInner && p.weighted))
+            wr = p.pair_w ? (float)static_cast<const T *>(p.pair_w)[m] : p.w ? p.w[m] : 1.0f;
         if (p.bias && split == 0) {
             float bias[4];
             if (p.bias_f32) load4(static_cast<const float *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
             else load4(static_cast<const T *>(p.bias) + (int64_t)e * p.strideBias + n, cnt, bias);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] += EPI == kPairs ? wr * bias[q] : bias[q];
+            for (int q = 0; q < 4; ++q) v[q] += bias[q];
         }
         if (EPI == kPairs) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] *= wr;
             store4(static_cast<float *>(p.out) + ((int64_t)split * p.M + m) * p.ldo + n, skip, cnt, v);
             continue;
         }
         if (p.pre) store4(static_cast<T *>(p.pre) + (int64_t)m * p.ldp + n, skip, cnt, v);
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = EPI == kLinear && p.out_f32 ? act_fine(p.act, v[q]) : act_value(p.act, v[q]);
-        if (EPI == kInner) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] *= wr;
+        if (EPI == kInner && p.weighted) {
+            const float t[4] = {v[0] * wr, v[1] * wr, v[2] * wr, v[3] * wr};
+            store4(static_cast<T *>(p.weighted) + (int64_t)m * p.ldo + n, skip, cnt, t);
         }
         if (EPI == kLinear && p.res) {
             float t4[4];

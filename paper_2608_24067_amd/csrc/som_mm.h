@@ -677,7 +677,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
     constexpr int kTurns = 16 / kAtOnce;
     // 16 rows: a lane's four columns of every kAtOnce-th row. Each stage runs over all of them, so
     // that its loads are in flight together and its branches are taken once.
-    // What it reads besides (residual; z and w act(z)) is loaded sixteen rows ahead.
+    // What it reads besides (residual; z and act(z)) is loaded sixteen rows ahead.
     typedef T vec4 __attribute__((ext_vector_type(4)));
     typedef vec4 any4 __attribute__((aligned(sizeof(T))));
     const bool cols_in = col0 + kCols <= (int)p.N && n0 == n_from && m0 == m_from;
@@ -718,12 +718,12 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
             const f32x4 c = *reinterpret_cast<const f32x4 *>(own + (r * kAtOnce + sub) * kRow + lane % kLanes * 4);
             m[r] = row0 + 16 * i + r * kAtOnce + sub;
             in[r] = W || (m[r] < m1 && m[r] >= m_from && cnt > 0 && skip < 4);
-            wr[r] = (EPI == kInner || EPI == kPairs || EPI == kSlope) && p.w && in[r] ? p.w[m[r]] : 1.0f;
+            wr[r] = ((EPI == kInner && p.weighted) || EPI == kPairs || EPI == kSlope) && p.w && in[r] ? p.w[m[r]] : 1.0f;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 v[r][q] = c[q];
-                if (EPI == kLinear || EPI == kInner) v[r][q] += bias[q];
-                if (EPI == kPairs) v[r][q] = fmaf(wr[r], bias[q], v[r][q]);
+                if (EPI == kLinear || EPI == kInner || EPI == kPairs) v[r][q] += bias[q];
+                if (EPI == kPairs) v[r][q] *= wr[r];
             }
         }
         if (EPI == kLinear || EPI == kInner) {
@@ -754,11 +754,13 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
                     for (int q = 0; q < 4; ++q) v[r][q] = act_value(SOM_ACT_RELU, v[r][q]);
             }
         }
-        if (EPI == kInner) {
+        if (EPI == kInner && p.weighted) {
 #pragma unroll
-            for (int r = 0; r < kTurns; ++r)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) v[r][q] *= wr[r];
+            for (int r = 0; r < kTurns; ++r) {
+                if (!in[r]) continue;
+                const float t[4] = {v[r][0] * wr[r], v[r][1] * wr[r], v[r][2] * wr[r], v[r][3] * wr[r]};
+                store4(static_cast<T *>(p.weighted) + (int64_t)m[r] * p.ldo + n, c0, c4, t);
+            }
         }
         if (EPI == kLinear && p.res) {
             float t[kTurns][4];
@@ -792,18 +794,14 @@ __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_product(cons
             auto slopes = [&](int act) {
 #pragma unroll
                 for (int r = 0; r < kTurns; ++r) {
-                    // act(z) from w act(z) as the forward pass rounded it: one rounding, where act of
-                    // the rounded z adds what its slope makes of another; not for weights so
-                    // small that the product may have lost bits to fp16's subnormals
-                    const bool held = fabsf(wr[r]) >= 1.0f / 64;
-                    const float over = held ? 1.0f / wr[r] : 0.0f;
+                    // act(z) as the forward pass rounded it: one rounding, where act of the rounded
+                    // z adds what its slope makes of another
                     part[r] = 0.0f;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         float value, slope;
                         act_both(act, z[r][q], value, slope);
-                        value = held ? h[r][q] * over : value;
-                        part[r] += in[r] && q < c4 && q >= c0 ? value * v[r][q] : 0.0f;
+                        part[r] += in[r] && q < c4 && q >= c0 ? h[r][q] * v[r][q] : 0.0f;
                         v[r][q] *= wr[r] * slope;
                     }
                 }

@@ -378,3 +378,33 @@ def test_gradients_of_more_tiles_than_a_grid_holds_along_x(dev):
         assert not t.any()
     del W1, W2, dW1, dW2, grads, ws
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("size", [1e-3, 1e-4, 1e-5, 100.0])
+@pytest.mark.parametrize("N,k,E,D,F", [(2, 2, 4, 264, 520), (30, 2, 64, 200, 136), (33, 2, 20, 128, 96),
+                                       (900, 2, 5, 72, 200), (3000, 2, 2, 1032, 520)])
+def test_weights_of_other_sizes_than_one(dev, size, N, k, E, D, F):
+    # fp16: w act(z) would be subnormal, or beyond the type, where act(z) and the results are neither
+    dtype = torch.float16
+    s, g = case(47, N, k, E, D, F, dtype, dev, empty=0.0)
+    s["x"] = s["x"] * (64 if size > 1 else 1)
+    s["W2"] = (s["W2"].float() * (2.0 ** -9 if size > 1 else 64 if size < 2e-4 else 8)).to(dtype)
+    s["w"] = ((torch.rand(N, k, generator=g) + 0.5) * size * (10 if size > 1 else 1)).to(dtype).to(dev)
+    out = dense.experts(**s, act="relu")
+    ref, bound = forms(s, "relu", None)
+    bound = bound - 2.0 ** -20 + 2.0 ** -40  # no residual: nothing of size one is rounded
+    check(out, ref, bound, "out")
+    dout = torch.randn(N, D, generator=g).to(dtype).to(dev)
+    ws = torch.empty(dense.experts_workspace_bytes(N, k, E, D, F, keep=True), dtype=torch.uint8, device=dev)
+    check(dense.experts(**s, act="relu", keep=True, workspace=ws), ref, bound, "out, kept")
+    dx, dw, dW1, db1, dW2, db2 = dense.experts_bwd(s["x"], s["idx"], s["w"], s["W1"], s["W2"], s["b2"], dout, act="relu",
+                                                   workspace=ws)
+    ref, off = gradients(s, "relu", dout, None)
+    check(dw, ref["w"], off["w"], "dw")
+    if size < 1:  # (sums of large weights lie beyond fp16)
+        check(db2, ref["b2"], off["b2"], "db2")
+        # w act(z) is held in fp16 for dW2: half its smallest subnormal may be lost of each
+        grain = torch.zeros(E, D, dtype=torch.float64)
+        grain.index_add_(0, s["idx"].cpu().reshape(-1).clamp(0, E - 1).long(),
+                         wide(dout).abs().repeat_interleave(k, 0) * 2.0 ** -25)
+        check(dW2, ref["W2"], off["W2"] + grain[:, None, :], "dW2")
