@@ -102,8 +102,9 @@ typedef struct {
  *   weights  device [N, k] of weight_type, written: the scores of these units, without the bias.
  *   counts   device int32 [E], written, or NULL: how many rows took each unit.
  * A unit is closed to a row whose logit, or logit + bias, is NaN or minus infinity: it is not
- * taken and has no share in the softmax. Plus infinity counts as the largest fp32 value. Where fewer
- * than k units are open the last places hold index -1 and weight 0.
+ * taken and has no share in the softmax. Plus infinity ranks above every number; where units are
+ * weighed, an infinite logit counts as the largest fp32 value. Where fewer than k units are open the
+ * last places hold index -1 and weight 0.
  * 0 <= N < 2^30; 1 <= E <= SOM_ROUTE_MAX_UNITS; 1 <= k <= min(E, SOM_ROUTE_MAX_TAKEN).
  */
 som_status som_route(int32_t logit_type, const void *logits, int64_t ldl, const float *bias, int64_t N, int64_t E,

@@ -202,3 +202,23 @@ def test_more_threads_than_a_grid_holds_along_x(dev, N, E):
     assert float((top - p * (1 - p)).abs().max()) <= 2.0 ** -10 * p * (1 - p) + 2.0 ** -17
     del l, dl, idx, w, best, dw, top
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("E,groups", [(24, 1), (24, 4), (300, 10), (2000, 1)])
+def test_infinity_ranks_above_every_number_and_weighs_as_the_largest(dev, E, groups):
+    big, inf = torch.finfo(torch.float32).max, math.inf
+    l, g = logits(26, 4, E, torch.float32, dev)
+    l[0, 3], l[0, 5] = big, inf
+    l[1, E - 1] = inf
+    l[2, 2], l[2, 4] = inf, inf
+    bias = torch.zeros(E, device=dev)
+    bias[E - 1], bias[1] = -1e38, inf  # an infinity stays one; a bias makes one of a number
+    how = dict(groups=groups, group_top=max(1, groups // 2))
+    for b in (None, bias):
+        for score, renorm in (("softmax", True), ("softmax", False), ("sigmoid", True), ("sigmoid", False)):
+            idx, w = dense.route(l, 4, bias=b, score=score, renorm=renorm, **how)
+            ri, rw = route(l, 4, b, score, renorm, **how)
+            assert torch.equal(idx.cpu(), ri)
+            close(w, rw, "weights")
+            if b is None:
+                assert idx[0, :2].tolist() == [5, 3] or groups > 1
