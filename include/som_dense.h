@@ -16,7 +16,9 @@
  *
  * Types. Rows, matrices, residuals and results are all fp16 or all bf16 (`type`, SOM_F16 or
  * SOM_BF16) where nothing else is said. Products are summed in fp32 and rounded once, to the type
- * of what is written; softmax statistics are fp32, the sum of squares of som_clip fp64.
+ * of what is written; softmax statistics are fp32, the sum of squares of som_clip fp64. Activations
+ * of 16-bit results and slopes are good to 2^-20 of max(|z|, 1), those of fp32 results to a few
+ * units in the last place (gelu below zero to z^2 of them).
  *
  * Strides (ldx, ldw, ...) are in elements, between rows; elements of a row are adjacent. Any
  * alignment to the element's size and any sizes are taken; rows that start 16-byte aligned and
@@ -62,8 +64,8 @@ som_status som_linear(int32_t type, const void *X, int64_t ldx, const void *W, i
  * Its gradients, from dY (device [N, M], lddy >= M, of `type`), each written unless NULL:
  *   dX [N, K] = dz W^T, dW [K, M] = X^T dz, dbias [M] (bias_type) = the column sums of dz, where
  *   dz = dY act'(pre); the residual's gradient is dY itself.
- * `pre` is what som_linear wrote; it is not read when act is SOM_ACT_NONE (then NULL will do). dz
- * is held in `type`. The workspace, som_linear_bwd_workspace_bytes(N, K, M, act) bytes, 256-byte
+ * `pre` is what som_linear wrote; it is not read when act is SOM_ACT_NONE (then NULL will do). The
+ * slope is taken at this rounded value, and dz is held in `type`. The workspace, som_linear_bwd_workspace_bytes(N, K, M, act) bytes, 256-byte
  * aligned, holds dz (unless act is SOM_ACT_NONE) and, for many rows of a small dW, parts of it in
  * fp32 (where it needs neither the size is 0 and NULL will do). N == 0 writes zeros to dW, dbias.
  */
@@ -144,8 +146,8 @@ som_status som_experts(int32_t type, const void *X, int64_t ldx, const int32_t *
 /*
  * Its gradients from dout (device [N, D], lddo >= D): dX [N, D] (lddx >= D), dw [N, k], and dW1,
  * db1, dW2, db2 shaped as the weights, each written whole unless NULL (an expert without rows gets
- * zeros). The workspace is the one that som_experts (keep = 1, the same arguments) left; it serves
- * any number of backward passes. The residual's gradient is dout itself. N == 0 writes zeros.
+ * zeros). The workspace is the one that som_experts (keep = 1, the same arguments) left, and that no
+ * other call has been given since (nothing in it tells); it serves any number of backward passes. The residual's gradient is dout itself. N == 0 writes zeros.
  * dz = w dout W2^T act'(x W1 + b1) is rounded to `type` before the products that follow, and
  * w act(...) for dW2; act' is taken at x W1 + b1 rounded to `type`.
  */

@@ -4,8 +4,8 @@
 // square of an fp32 value overflows or vanishes; the threads' sums joined in a fixed order), one
 // workgroup adds the chunks' sums and forms the scale, and the chunks are scaled. Few chunks: the
 // second pass is done by every workgroup of the third. Both large passes are bound by the bytes
-// they move: 2.3 GB in three types are summed at 5.6 TB/s and read and written at 5.1 TB/s
-// (415 + 900 us); the scale needs the norm, so the tensors are read twice.
+// they move: 2.3 GB in three types are summed at 6.2 TB/s and read and written at 5.1 TB/s
+// (375 + 919 us); the scale needs the norm, so the tensors are read twice.
 
 #include "som_mm.h"
 

@@ -81,8 +81,8 @@ som::TileSize pick_tile(int64_t rows, int64_t groups, int64_t cols, bool whole)
 }
 
 // The tile of a product over rows (M x N a group), by the same rule (8192 rows, us by Mid and Large
-// tiles: 2048 x 4096 135, 173; 2048 x 4352 183, 168; 4096 x 4096 252, 208; 10,007 rows to 32 experts,
-// 1000 x 2048 each: 143, 107).
+// tiles: 2048 x 4096 145, 178; 2048 x 4352 184, 167; 4096 x 4096 253, 207; 10,007 rows of two among
+// 32 experts, 2048 x 1000 each: 161, 122).
 som::TileSize pick_tile_tn(int64_t M, int64_t N, int64_t groups)
 {
     return (M + 127) / 128 * ((N + 127) / 128) * groups > 512 ? som::kTileLarge : som::kTileMid;

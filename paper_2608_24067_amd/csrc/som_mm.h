@@ -69,7 +69,7 @@ __device__ inline float exp_short(float x) { return __builtin_amdgcn_exp2f(x * 1
 // The normal distribution Phi(z) and exp(-z^2 / 2), by formula 7.1.26 of Abramowitz and Stegun's
 // Handbook of Mathematical Functions for the error function: within 1.5e-7 of itself (of z Phi(z)
 // for z below about -4 that is more than a 16-bit result's rounding, of values below 2e-4), for a
-// third of erff's instructions.
+// third of erff's instructions. For 16-bit results; fp32 ones take act_fine.
 __device__ inline float normal_f32(float z, float &bell)
 {
     const float x = fabsf(z) * 0.707106781f;

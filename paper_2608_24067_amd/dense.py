@@ -4,6 +4,10 @@ Products of dense rows with a feature-major matrix (a codebook's scores, a layer
 units, the units' experts, and clipping of all gradients to a norm. As in ``som``, every function checks its tensors
 and passes pointers and the current torch stream of the tensors' device to the C entry point of the same name.
 Matrices and rows may have any row stride; the elements of a row must be adjacent.
+
+No function takes part in autograd: results carry no graph, also where an argument requires a gradient (the ``_bwd``
+functions give the gradients), and what is written in place (``out``, ``pre``, clip's tensors) is written without
+autograd's knowledge of it, as if under ``torch.no_grad()`` and without a new version.
 """
 from __future__ import annotations
 
@@ -271,7 +275,8 @@ def experts(x, idx, w, W1, b1, W2, b2, act: str = "gelu", residual=None, out=Non
 def experts_bwd(x, idx, w, W1, W2, b2, dout, act: str = "gelu", out=None, workspace=None):
     """(dx, dw, dW1, db1, dW2, db2) from dout [N, D] and the workspace that experts(keep=True) left.
 
-    The other arguments are those of experts. ``out`` may pass the six tensors; one that is None is not computed.
+    The other arguments are those of experts. ``out`` may pass the six tensors; one that is None is not computed. The
+    workspace must not have been passed to another call in between: nothing in it tells.
     """
     kind, dev, dt = _type(x, "x"), x.device, x.dtype
     N, D, k, E, F = _experts_shapes(x, idx, W1)
