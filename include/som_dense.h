@@ -2,7 +2,7 @@
  * som_dense.h -- dense rows on a map: part of the C ABI of libsom.so (conventions, status codes and
  * som_last_error as in som.h).
  *
- * A map whose rows are dense (document embeddings, hidden states) is used through four operators:
+ * A map whose rows are dense (document embeddings, hidden states) is used through these operators:
  *
  *   som_linear    products of rows with a feature-major matrix, with bias, activation and residual.
  *                 With a codebook W and the bias -|w|^2 / 2 it scores every unit: x.w - |w|^2 / 2
@@ -10,8 +10,11 @@
  *   som_route     each row's best k units by such scores, and their weights.
  *   som_experts   each row through the experts (two-layer networks) of its units, by these weights.
  *   som_clip      the norm of all gradients together, and their scaling to a largest norm.
+ *   som_layer_norm  rows to mean 0 and variance 1, in front of a layer.
+ *   som_adamw     a step of all parameters along their gradients, with states in 32 bits or in 8.
+ *   som_mx4_...   rows and matrices in 4 bits, and products with them.
  *
- * The first three have a backward pass. Matrices are feature-major as codebooks are: W[k * ldw + m]
+ * The first three and som_layer_norm have a backward pass. Matrices are feature-major as codebooks are: W[k * ldw + m]
  * is feature k of column m.
  *
  * Types. Rows, matrices, residuals and results are all fp16 or all bf16 (`type`, SOM_F16 or
@@ -172,6 +175,142 @@ size_t som_clip_workspace_bytes(const int64_t *sizes, int64_t count);
 
 som_status som_clip(const void *const *tensors, void *const *outs, const int64_t *sizes, const int32_t *types,
                     int64_t count, float max_norm, float *norm, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Y = (X - mean) / sqrt(var + eps) * weight + bias, mean and variance (divided by D) over each row.
+ *   X         device [N, D] of `type` (SOM_F32, SOM_F16 or SOM_BF16), ldx >= D.
+ *   weight    device [D] or NULL (ones);   bias  device [D] or NULL (zeros); both of weight_type,
+ *             SOM_F32 or y_type.
+ *   Y         device [N, D], ldy >= D, written; y_type is `type`, or any where that is SOM_F32. It may be
+ *             X's own buffer (with ldy == ldx and y_type == type).
+ *   stats     device fp64 [N, 2], written, or NULL: each row's mean and 1 / sqrt(var + eps), which the
+ *             backward pass reads.
+ * Mean and variance are formed in fp64. A row with an infinity or a NaN is all NaN. eps is at least
+ * 2^-126, and finite. 0 <= N < 2^30, 1 <= D < 2^20. N == 0 is a no-op.
+ */
+som_status som_layer_norm(int32_t type, const void *X, int64_t ldx, const void *weight, const void *bias,
+                          int32_t weight_type, double eps, void *Y, int64_t ldy, int32_t y_type, double *stats,
+                          int64_t N, int64_t D, void *stream);
+
+/*
+ * Its gradients, from dY (device [N, D] of y_type, lddy >= D) and the stats that som_layer_norm wrote,
+ * each written unless NULL:
+ *   dX [N, D] of `type` (lddx >= D): add + (t - mean(t) - h mean(t h)) / std, where t = dY weight and
+ *     h = (X - mean) / std;  dweight [D] = the sum over rows of dY h;  dbias [D] = the sum of dY.
+ *   add       device [N, D] of `type`, ldadd >= D, or NULL: the gradient that reaches X by another way (round the
+ *             layer). It may be dX's own buffer (with ldadd == lddx); so may dY (with lddy == lddx and y_type ==
+ *             type).
+ * Sums are fp32, in a fixed order. The workspace is som_layer_norm_bwd_workspace_bytes(N, D) bytes,
+ * 256-byte aligned. N == 0 writes zeros to dweight and dbias.
+ */
+size_t som_layer_norm_bwd_workspace_bytes(int64_t N, int64_t D);
+
+som_status som_layer_norm_bwd(int32_t type, const void *X, int64_t ldx, const void *weight, int32_t weight_type,
+                              const void *dY, int64_t lddy, int32_t y_type, const double *stats, const void *add,
+                              int64_t ldadd, void *dX, int64_t lddx, void *dweight, void *dbias, int64_t N, int64_t D,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One tensor of a step: `size` elements (at most 2^38), none of which another tensor of the call holds.
+ *   param     device, of `type` (SOM_F32, SOM_F16 or SOM_BF16), updated.
+ *   grad      device, of grad_type (any of the three).
+ *   m, v      device, updated: the running means of the gradient and of its square, fp32 [size]; or,
+ *             with 8-bit states, one code each, uint8 [size].
+ *   m_scales, v_scales  device uint8 [ceil(size / 256)], updated: the scales of 8-bit states' blocks.
+ *   master    device fp32 [size] or NULL: the parameter in fp32. It is what the step reads and updates; param gets its
+ *             value, rounded.
+ * 8-bit states start as zeros, scales too. A block of 256 values has the scale s of a power of two,
+ * 2^(s - 127), at which its largest magnitude is at most 1.875. A code of m is a sign, 4 bits of exponent and 3 behind
+ * the point, exponents from 2^-14 on; one of v 5 bits of exponent and 3 behind the point, from 2^-30 on; the lowest
+ * exponent's codes are subnormal. Scale 0: all are zero (magnitudes below 2^-100 are held so). Scale 255: the block
+ * held an infinity, a NaN or a magnitude above 1.875 * 2^127, and all of it stands for NaN.
+ */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    uint8_t *m_scales, *v_scales;
+    float *master;
+    int64_t size;
+    int32_t type, grad_type;
+} som_adamw_tensor;
+
+/*
+ * How som_adamw steps. lr, weight_decay: finite, >= 0; 0 <= beta1, beta2 < 1; eps: >= 2^-126 and
+ * finite; grad_scale: finite; step: this step's number, 1 ... 2^31 - 1.
+ *   bits      32 or 8: the states.
+ *   seed      for 8-bit states: with the step, the tensor's number in the call and the element's in the tensor it
+ *             decides their rounding.
+ *   lr_at, step_at  device fp32 [1] and int32 [1], or NULL: read instead of lr and step (a captured step's rate
+ *             and number can so change from replay to replay). A *step_at below 1 counts as 1.
+ *   norm      device fp32 [1] or NULL: where it is infinite or NaN (som_clip's norm) nothing is written.
+ */
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay, grad_scale;
+    int64_t step;
+    int32_t bits;
+    uint32_t seed;
+    const float *lr_at;
+    const int32_t *step_at;
+    const float *norm;
+    int64_t reserved[4]; /* must be zero */
+} som_adamw_config;
+
+/*
+ * A step of AdamW (decoupled weight decay) over `count` tensors, with g = grad_scale * grad:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
+ * in fp32. Of 8-bit states the step uses the new values before they are rounded. They are rounded to either of
+ * the codes beside them, by the seed, so that their mean is kept; a v above zero is never rounded to zero. The same
+ * arguments give the same bits.
+ * tensors is a host array, read during the call.
+ */
+som_status som_adamw(const som_adamw_tensor *tensors, int64_t count, const som_adamw_config *config, void *stream);
+
+/*
+ * What 8-bit states stand for: m and v of tensor i as fp32 [size] to m_out[i] and v_out[i] (host arrays of device
+ * pointers). Of the tensors m, v, their scales and the size are read.
+ */
+som_status som_adamw_values(const som_adamw_tensor *tensors, int64_t count, float *const *m_out, float *const *v_out,
+                            void *stream);
+
+/*
+ * Values in 4 bits, microscaled: blocks of 32 features share a power of two.
+ *   codes     device uint8 [n, 16 * ceil(K / 32)], 16-byte aligned, dense: a row's codes, two to a byte, the lower
+ *             feature in the low half; zeros past feature K. A code is a sign (8) and 0 ... 7 for 0, 0.5, 1, 1.5, 2,
+ *             3, 4, 6.
+ *   scales    device uint8 [n, ceil(K / 32)], dense: block b's scale s stands for 2^(s - 127); 255 for NaN.
+ * som_mx4_quantise writes both for X of `type` (SOM_F32, SOM_F16 or SOM_BF16): columns == 0, rows X [n, K]
+ * (ldx >= K); columns == 1, the columns of a feature-major matrix X [K, n] (ldx >= n). s is the exponent of the
+ * block's largest magnitude, less 2, plus 127, at least 0; values are rounded to the nearest, ties to the even code,
+ * and those above 6 to 6. A block with an infinity or a NaN gets 255. som_mx4_values writes what codes and scales
+ * stand for, rounded to `type`, to Y, laid out as X. Scales of 253 and 254 are not made here; magnitudes beyond
+ * fp32 count as infinite.
+ * 0 <= n < 2^30, 1 <= K < 2^30.
+ */
+som_status som_mx4_quantise(int32_t type, const void *X, int64_t ldx, int32_t columns, uint8_t *codes, uint8_t *scales,
+                            int64_t n, int64_t K, void *stream);
+
+som_status som_mx4_values(int32_t type, const uint8_t *codes, const uint8_t *scales, int32_t columns, void *Y,
+                          int64_t ldy, int64_t n, int64_t K, void *stream);
+
+/*
+ * Y = residual + act(X W + bias), as som_linear, with W in 4 bits by its columns: w_codes, w_scales [M, ...] as
+ * som_mx4_quantise (columns == 1) writes them.
+ *   X         device [N, K] of `type` (SOM_F16 or SOM_BF16), ldx >= K, with x_scales NULL; or the rows in
+ *             4 bits: X the codes (ldx is not read), x_scales their scales.
+ *   bias, bias_type, residual, Y, y_type  as in som_linear.
+ * The values that codes stand for are multiplied as they are, without a further rounding, and summed in fp32.
+ * Results that a block of NaN takes part in are NaN. The workspace is som_mx4_linear_workspace_bytes(N, K, M, packed)
+ * bytes, packed 1 for rows in 4 bits, 256-byte aligned.
+ * 0 <= N < 2^30, 1 <= K, M < 2^30. N == 0 is a no-op.
+ */
+size_t som_mx4_linear_workspace_bytes(int64_t N, int64_t K, int64_t M, int32_t packed);
+
+som_status som_mx4_linear(int32_t type, const void *X, int64_t ldx, const uint8_t *x_scales, const uint8_t *w_codes,
+                          const uint8_t *w_scales, const void *bias, int32_t bias_type, int32_t act,
+                          const void *residual, int64_t ldr, void *Y, int64_t ldy, int32_t y_type, int64_t N, int64_t K,
+                          int64_t M, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

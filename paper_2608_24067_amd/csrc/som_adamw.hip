@@ -1,0 +1,282 @@
+// som_adamw.hip -- a step of AdamW over many tensors, with the states in 32 bits or in 8.
+//
+//   m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2
+//   p' = p (1 - lr wd) - lr / (1 - b1^t) * m' / (sqrt(v') / sqrt(1 - b2^t) + eps)
+//
+// One launch takes the chunks of up to 44 tensors; a thread's four or eight elements are loaded in
+// vectors. Bound by the bytes it moves: 28 an element in fp32, 10 of a 16-bit parameter with 8-bit
+// states, whose arithmetic (about 60 instructions an element) stays below that.
+//
+// 8-bit states. A block of 256 values shares a power of two 2^e, the least at which its largest
+// value is at most 1.875, held as e + 127 in a byte (255: the block held an infinity or NaN, and all
+// of it stands for NaN; 0: all values below 2^-100, held as zeros). m is held with a sign, 4 bits
+// of exponent and 3 behind the point, down to 2^-17 of the block's largest value; v, which has no
+// sign and the square of m's range, with 5 bits of exponent, down to 2^-33. Rounding is to either
+// neighbour, the nearer one more often, so that a value's mean is kept: with b2 = 0.999 a state moves
+// by a thousandth of itself a step, and rounding to nearest, in steps of a sixteenth, would leave it
+// where it is. The 16 bits that decide come from a hash of the seed, the step, the tensor's number in
+// the call and the element's in the tensor: the same inputs give the same bits. A v above zero is
+// never rounded to zero, or a later step would divide what is left of m by eps alone.
+
+#include "som_layer_device.h"
+
+namespace som {
+namespace {
+
+using namespace layer;
+
+constexpr int kThreads = 256;
+
+// The bits of h spread over all of them: shifts, and multiplications by the fractional parts of the
+// square roots of 3 and 2.
+__device__ inline uint32_t mix(uint32_t h)
+{
+    h ^= h >> 16;
+    h *= 0xBB67AE85u;
+    h ^= h >> 15;
+    h *= 0x6A09E667u;
+    return h ^ h >> 16;
+}
+
+__device__ inline int tensor_of(const AdamwTable &t, int chunk)
+{
+    int lo = 0, hi = t.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (t.first[mid] <= chunk) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+struct Rates : AdamwRates {
+    // As the host formed them, or with the step or the rate that lie on the device.
+    __device__ explicit Rates(const AdamwArgs &a) : AdamwRates(a.rates)
+    {
+        if (a.step_at || a.lr_at) {
+            const double lr = a.lr_at ? (double)*a.lr_at : a.lr;
+            set(lr, a.beta1, a.beta2, a.weight_decay, a.step_at ? (uint32_t)max(*a.step_at, 1) : step);
+        }
+    }
+    __device__ void apply(float &p, float g, float &m, float &v) const
+    {
+        g *= grad;
+        m = m * b1 + g * c1;
+        v = v * b2 + g * g * c2;
+        p = p * keep - rate * (m / (sqrtf(v) * root + eps));
+    }
+};
+
+// n values of any of the three types.
+template <int V> __device__ inline void load_any(const void *p, int type, int64_t at, int n, float *v)
+{
+    if (type == SOM_F32) load<V>(static_cast<const float *>(p) + at, n, v);
+    else if (type == SOM_F16) load<V>(static_cast<const _Float16 *>(p) + at, n, v);
+    else load<V>(static_cast<const __bf16 *>(p) + at, n, v);
+}
+template <int V> __device__ inline void store_any(void *p, int type, int64_t at, int n, const float *v)
+{
+    if (type == SOM_F32) store<V>(static_cast<float *>(p) + at, n, v);
+    else if (type == SOM_F16) store<V>(static_cast<_Float16 *>(p) + at, n, v);
+    else store<V>(static_cast<__bf16 *>(p) + at, n, v);
+}
+
+__device__ inline float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 ... 127
+
+// x 2^e for -254 <= e <= 254 and x not near the ends of fp32's range on the way.
+__device__ inline float times_power(float x, int e)
+{
+    const int half = e >> 1;
+    return x * power_of_two(half) * power_of_two(e - half);
+}
+
+// What a code stands for, before the block's power: its bits are those of an fp32 value whose exponent
+// is 112 (m) or 96 (v) too small; codes below the first exponent are subnormal there.
+template <bool SIGNED> __device__ inline float code_value(uint32_t c)
+{
+    const float size = __uint_as_float((SIGNED ? c & 127 : c) << 20) * (SIGNED ? 0x1p112f : 0x1p96f);
+    return SIGNED && c & 128 ? -size : size;
+}
+
+// The exponent e of a block's power from the bits of its largest magnitude, as its byte.
+__device__ inline uint32_t block_scale(uint32_t bits)
+{
+    const uint32_t f = (bits + 0xFFFFF) >> 23;  // a NaN may carry past 255
+    return f < 27 ? 0 : min(f, 255u);
+}
+
+// The code of x under the block's byte, by 16 random bits. A block of NaN gets codes of no meaning.
+template <bool SIGNED> __device__ inline uint32_t encode(float x, uint32_t scale, uint32_t random)
+{
+    const float y = times_power(fabsf(x), 127 - (int)scale) * (SIGNED ? 0x1p-112f : 0x1p-96f);
+    uint32_t c = (__float_as_uint(y) + (random << 4)) >> 20;
+    if (SIGNED) c = min(c, 127u) | (x < 0.0f ? 128u : 0u);
+    else c = x > 0.0f ? max(min(c, 255u), 1u) : 0u;
+    return scale ? c : 0u;
+}
+
+__device__ inline float scaled_value(float v, uint32_t scale)
+{
+    return scale == 255 ? __builtin_nanf("") : scale ? times_power(v, (int)scale - 127) : 0.0f;
+}
+
+// The largest over the 32 lanes of a block's half wave.
+__device__ inline uint32_t half_wave_max(uint32_t v)
+{
+    v = max(v, swap32<0xB1>(v));
+    v = max(v, swap32<0x4E>(v));
+    v = max(v, swap32<0x141>(v));
+    v = max(v, swap32<0x140>(v));
+    return max(v, (uint32_t)__shfl_xor((int)v, 16));
+}
+
+// n codes (up to 8) as bytes.
+__device__ inline void load8(const uint8_t *p, int n, uint32_t *c)
+{
+    if (n >= 8) {
+        typedef VecOf<uint32_t, 2>::type two;
+        typedef two any __attribute__((aligned(1)));
+        const two t = *reinterpret_cast<const any *>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = t[i / 4] >> (8 * (i % 4)) & 255;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = i < n ? p[i] : 0;
+    }
+}
+__device__ inline void store8(uint8_t *p, int n, const uint32_t *c)
+{
+    if (n >= 8) {
+        typedef VecOf<uint32_t, 2>::type two;
+        typedef two any __attribute__((aligned(1)));
+        two t;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) t[h] = c[4 * h] | c[4 * h + 1] << 8 | c[4 * h + 2] << 16 | c[4 * h + 3] << 24;
+        *reinterpret_cast<any *>(p) = t;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (uint8_t)c[i];
+    }
+}
+
+template <bool BITS8> __global__ __launch_bounds__(kThreads) void k_adamw(const AdamwTable t, const AdamwArgs a)
+{
+    if (a.norm && !(fabsf(*a.norm) < __builtin_inff())) return;
+    const int chunk = blockIdx.x, i = tensor_of(t, chunk);
+    const int64_t from = (int64_t)(chunk - t.first[i]) * t.chunk, to = min(t.size[i], from + t.chunk);
+    const Rates r(a);
+    const int type = t.type[i], grad_type = t.grad_type[i];
+    float *master = t.master[i];
+    const void *read = master ? static_cast<const void *>(master) : t.param[i];
+    const int read_type = master ? SOM_F32 : type;
+    if (!BITS8) {
+        constexpr int V = 4;
+        float *ms = static_cast<float *>(t.m[i]), *vs = static_cast<float *>(t.v[i]);
+#pragma unroll 2
+        for (int64_t at = from + V * (int64_t)threadIdx.x; at < to; at += V * kThreads) {
+            const int n = (int)min((int64_t)V, to - at);
+            float p[V], g[V], m[V], v[V];
+            load_any<V>(read, read_type, at, n, p);
+            load_any<V>(t.grad[i], grad_type, at, n, g);
+            load<V>(ms + at, n, m);
+            load<V>(vs + at, n, v);
+#pragma unroll
+            for (int q = 0; q < V; ++q) r.apply(p[q], g[q], m[q], v[q]);
+            store<V>(ms + at, n, m);
+            store<V>(vs + at, n, v);
+            if (master) store<V>(master + at, n, p);
+            store_any<V>(t.param[i], type, at, n, p);
+        }
+    } else {
+        constexpr int V = 8;
+        uint8_t *mc = static_cast<uint8_t *>(t.m[i]), *vc = static_cast<uint8_t *>(t.v[i]);
+        const uint32_t key = mix(a.seed + r.step * 0x9E3779B1u + (uint32_t)(t.number + i) * 0x1F83D9ABu);
+        // Whole blocks of 32 threads take part: past the end they hold zeros.
+        for (int64_t at = from + V * (int64_t)threadIdx.x; at < from + t.chunk; at += V * kThreads) {
+            const int64_t block = at / kStateBlock;
+            if (block * kStateBlock >= to) break;
+            const int n = (int)max((int64_t)0, min((int64_t)V, to - at));
+            float p[V], g[V], m[V], v[V];
+            uint32_t cm[V], cv[V];
+            load_any<V>(read, read_type, at, n, p);
+            load_any<V>(t.grad[i], grad_type, at, n, g);
+            load8(mc + at, n, cm);
+            load8(vc + at, n, cv);
+            const uint32_t old_m = t.m_scales[i][block], old_v = t.v_scales[i][block];
+            uint32_t top_m = 0, top_v = 0;
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+                m[q] = scaled_value(code_value<true>(cm[q]), old_m);
+                v[q] = scaled_value(code_value<false>(cv[q]), old_v);
+                if (q >= n) m[q] = v[q] = 0.0f;
+                r.apply(p[q], g[q], m[q], v[q]);
+                top_m = max(top_m, __float_as_uint(m[q]) & 0x7FFFFFFF);
+                top_v = max(top_v, __float_as_uint(v[q]) & 0x7FFFFFFF);
+            }
+            const uint32_t new_m = block_scale(half_wave_max(top_m)), new_v = block_scale(half_wave_max(top_v));
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+                const uint64_t e = (uint64_t)(at + q);
+                const uint32_t random = mix((uint32_t)e * 0x9E3779B1u + (uint32_t)(e >> 32) * 0xA54FF53Bu + key);
+                cm[q] = encode<true>(m[q], new_m, random & 0xFFFF);
+                cv[q] = encode<false>(v[q], new_v, random >> 16);
+            }
+            store8(mc + at, n, cm);
+            store8(vc + at, n, cv);
+            if (threadIdx.x % 32 == 0) t.m_scales[i][block] = (uint8_t)new_m, t.v_scales[i][block] = (uint8_t)new_v;
+            if (master) store<V>(master + at, n, p);
+            store_any<V>(t.param[i], type, at, n, p);
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void k_adamw_values(const AdamwTable t)
+{
+    constexpr int V = 4;
+    const int chunk = blockIdx.x, i = tensor_of(t, chunk);
+    const int64_t from = (int64_t)(chunk - t.first[i]) * t.chunk, to = min(t.size[i], from + t.chunk);
+    const uint8_t *mc = static_cast<const uint8_t *>(t.m[i]), *vc = static_cast<const uint8_t *>(t.v[i]);
+    float *om = static_cast<float *>(t.param[i]), *ov = t.master[i];
+#pragma unroll 2
+    for (int64_t at = from + V * (int64_t)threadIdx.x; at < to; at += V * kThreads) {
+        const int n = (int)min((int64_t)V, to - at);
+        const uint32_t sm = t.m_scales[i][at / kStateBlock], sv = t.v_scales[i][at / kStateBlock];
+        typedef uint32_t any __attribute__((aligned(1)));
+        uint32_t cm = 0, cv = 0;
+        if (n == V) {
+            cm = *reinterpret_cast<const any *>(mc + at);
+            cv = *reinterpret_cast<const any *>(vc + at);
+        } else {
+            for (int q = 0; q < n; ++q) cm |= (uint32_t)mc[at + q] << (8 * q), cv |= (uint32_t)vc[at + q] << (8 * q);
+        }
+        float m[V], v[V];
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            m[q] = scaled_value(code_value<true>(cm >> (8 * q) & 255), sm);
+            v[q] = scaled_value(code_value<false>(cv >> (8 * q) & 255), sv);
+        }
+        store<V>(om + at, n, m);
+        store<V>(ov + at, n, v);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const AdamwTable &t, bool bits8, const AdamwArgs &a, hipStream_t st)
+{
+    if (t.first[t.count] == 0) return hipSuccess;
+    const dim3 grid((unsigned)t.first[t.count]);
+    if (bits8) hipLaunchKernelGGL(k_adamw<true>, grid, dim3(kThreads), 0, st, t, a);
+    else hipLaunchKernelGGL(k_adamw<false>, grid, dim3(kThreads), 0, st, t, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_adamw_values(const AdamwTable &t, hipStream_t st)
+{
+    if (t.first[t.count] == 0) return hipSuccess;
+    hipLaunchKernelGGL(k_adamw_values, dim3((unsigned)t.first[t.count]), dim3(kThreads), 0, st, t);
+    return hipGetLastError();
+}
+
+}  // namespace som

@@ -1,0 +1,147 @@
+// som_layer.h -- shared between the host layer of layer norm, AdamW and the 4-bit operators
+// (include/som_dense.h) and their kernels.
+#pragma once
+
+#include <math.h>
+
+#include "som_dense.h"
+
+namespace som {
+
+// ---------------------------------------------------------------- layer norm
+
+struct NormArgs {
+    const void *x;
+    int64_t ldx;
+    const void *weight, *bias;  // null: ones, zeros
+    bool weights_f32;           // else of y's type
+    double eps;
+    void *y;                    // the gradient: dy
+    int64_t ldy;
+    double *stats;              // [N][2] mean, 1 / std; or null
+    int64_t N;
+    int32_t D;
+    // the gradient
+    const void *add;            // or null
+    int64_t lda;
+    void *dx;                   // or null
+    int64_t lddx;
+    float *parts;               // [n_parts][2][D]: dweight, dbias; or null
+    int64_t n_parts, part_rows; // parts of part_rows rows each
+    float *means;               // [N][2], of rows too long for registers
+};
+
+// Workgroups of the gradient, one part each: two a CU from 3,584 rows on, fewer for fewer rows (their
+// parts cost as much as eight rows each), and so many that a part's fp32 sums run over 256 rows at
+// most before they are joined.
+inline int64_t norm_parts(int64_t N)
+{
+    int64_t n = 64 + N / 8;
+    if (n > 512) n = 512;
+    if (n < (N + 255) / 256) n = (N + 255) / 256;
+    return n < N ? n : N < 1 ? 1 : N;
+}
+
+hipError_t launch_norm_rows(int x_type, int y_type, const NormArgs &a, hipStream_t st);
+hipError_t launch_norm_grad(int x_type, int y_type, const NormArgs &a, hipStream_t st);
+// out[j][d] = the sum of the parts' [j][d], j = 0, 1; an out that is null is left out.
+hipError_t launch_norm_sums(const float *parts, int64_t n_parts, int32_t D, void *dweight, void *dbias, int type,
+                            hipStream_t st);
+
+// ---------------------------------------------------------------- AdamW
+
+constexpr int kStateBlock = 256;   // 8-bit states: values of a block
+constexpr int kAdamwTensors = 44;  // tensors of one launch: their table fits a kernel's arguments
+
+// Elements of a workgroup: 4,096 workgroups where the tensors hold that many, 32K elements at most.
+inline int64_t adamw_chunk(int64_t total)
+{
+    const int64_t n = (total / 4096 + 2047) / 2048 * 2048;
+    return n < 2048 ? 2048 : n > 32768 ? 32768 : n;
+}
+
+struct AdamwTable {
+    void *param[kAdamwTensors];
+    const void *grad[kAdamwTensors];
+    void *m[kAdamwTensors], *v[kAdamwTensors];
+    uint8_t *m_scales[kAdamwTensors], *v_scales[kAdamwTensors];
+    float *master[kAdamwTensors];
+    int64_t size[kAdamwTensors];
+    int32_t first[kAdamwTensors + 1];  // chunks before each tensor
+    int8_t type[kAdamwTensors], grad_type[kAdamwTensors];
+    int32_t count;
+    int32_t number;  // of the first tensor in the call
+    int64_t chunk;
+};
+
+// What a step multiplies by, in fp32 from fp64: the same bits on the host and on the device.
+struct AdamwRates {
+    float b1, c1, b2, c2, keep, rate, root, eps, grad;
+    uint32_t step;
+
+    __host__ __device__ static double power(double b, uint32_t t)  // by squaring
+    {
+        double r = 1.0;
+        for (; t; t >>= 1, b *= b)
+            if (t & 1) r *= b;
+        return r;
+    }
+    __host__ __device__ void set(double lr, double beta1, double beta2, double weight_decay, uint32_t t)
+    {
+        step = t;
+        b1 = (float)beta1, c1 = (float)(1.0 - beta1);
+        b2 = (float)beta2, c2 = (float)(1.0 - beta2);
+        keep = (float)(1.0 - lr * weight_decay);
+        rate = (float)(lr / (1.0 - power(beta1, t)));
+        root = (float)(1.0 / sqrt(1.0 - power(beta2, t)));
+    }
+};
+
+struct AdamwArgs {
+    AdamwRates rates;
+    double lr, beta1, beta2, weight_decay;
+    uint32_t seed;
+    const float *lr_at;      // device, or null: lr
+    const int32_t *step_at;  // device, or null: the rates' step
+    const float *norm;       // device, or null: where it is not finite nothing is written
+};
+
+hipError_t launch_adamw(const AdamwTable &t, bool bits8, const AdamwArgs &a, hipStream_t st);
+// m and v of 8-bit states as fp32, to param and master (both fp32 here).
+hipError_t launch_adamw_values(const AdamwTable &t, hipStream_t st);
+
+// ---------------------------------------------------------------- 4-bit values
+
+constexpr int kFourBlock = 32;  // values that share a power of two: 16 bytes of codes, one of scale
+__host__ __device__ inline int64_t four_blocks(int64_t K) { return (K + kFourBlock - 1) / kFourBlock; }
+
+struct FourArgs {
+    const void *x;           // rows [N][K], or columns: [K][N]; the values' y is written instead
+    int64_t ldx;
+    uint8_t *codes, *scales; // [N][blocks * 16], [N][blocks]
+    int64_t N, K;
+};
+
+hipError_t launch_mx4_quantise(int type, bool columns, const FourArgs &a, hipStream_t st);
+hipError_t launch_mx4_values(int type, bool columns, const FourArgs &a, void *y, int64_t ldy, hipStream_t st);
+
+// Y = residual + act(X W + bias), W in 4 bits by columns, X in 16 bits or in 4 bits by rows.
+struct FourProduct {
+    const void *x;            // [N][K] of the type, or codes
+    int64_t ldx;              // elements; not read for codes
+    const uint8_t *x_scales;  // null: x is of the type
+    const uint8_t *w, *w_scales;
+    const void *bias;
+    bool bias_f32;
+    int32_t act;
+    const void *res;
+    int64_t ldr;
+    void *y;
+    int64_t ldy;
+    bool y_f32;
+    int64_t N, K, M;
+};
+
+hipError_t launch_mx4_few(bool bf16, const FourProduct &p, hipStream_t st);
+
+}  // namespace som

@@ -1,0 +1,286 @@
+// som_layer_api.cpp -- host side of layer norm, AdamW and the 4-bit operators (include/som_dense.h):
+// argument checks, workspace carving, launches on the caller's stream.
+
+#include <hip/hip_runtime.h>
+
+#include <cfloat>
+#include <cmath>
+
+#include "som_layer.h"
+
+namespace {
+
+som_status ok() { return som::set_error(SOM_OK, "%s", ""); }
+
+som_status bad(const char *who, const char *what) { return som::set_error(SOM_ERR_INVALID_ARG, "%s: %s", who, what); }
+
+som_status done(hipError_t e, const char *who)
+{
+    return e == hipSuccess ? ok() : som::set_error(SOM_ERR_HIP, "%s: %s (%d)", who, hipGetErrorString(e), (int)e);
+}
+
+bool half_type(int32_t t) { return t == SOM_F16 || t == SOM_BF16; }
+bool any_type(int32_t t) { return t == SOM_F32 || half_type(t); }
+int64_t size_of(int32_t t) { return t == SOM_F32 ? 4 : 2; }
+bool off(const void *p, int64_t align) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(align - 1)) != 0; }
+bool odd(const void *p, int32_t t) { return off(p, size_of(t)); }
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+constexpr int64_t kMostDim = (int64_t)1 << 30;
+bool dim_ok(int64_t v) { return v >= 1 && v < kMostDim; }
+bool width_ok(int64_t v) { return v >= 1 && v < ((int64_t)1 << 20); }  // of normalised rows
+bool rows_ok(int64_t v) { return v >= 0 && v < kMostDim; }
+
+som_status check_workspace(const char *who, const void *ws, size_t bytes, size_t need)
+{
+    if (need == 0) return SOM_OK;
+    if (!ws) return som::set_error(SOM_ERR_WORKSPACE, "%s: workspace is NULL", who);
+    if (off(ws, 256)) return som::set_error(SOM_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned", who);
+    if (bytes < need)
+        return som::set_error(SOM_ERR_WORKSPACE, "%s: workspace holds %zu bytes, the call needs %zu", who, bytes, need);
+    return SOM_OK;
+}
+
+const char *const kNotAligned = "a pointer is not aligned to its elements";
+const char *const kStride = "a row stride is smaller than its row";
+const char *const kNull = "null pointer";
+
+// What layer norm's two directions have in common.
+const char *norm_types(int32_t type, int32_t y_type, int32_t weight_type)
+{
+    if (!any_type(type)) return "type must be SOM_F32, SOM_F16 or SOM_BF16";
+    if (!any_type(y_type) || (y_type != type && type != SOM_F32)) return "y_type must be type, or any where that is SOM_F32";
+    if (weight_type != SOM_F32 && weight_type != y_type) return "weight_type must be SOM_F32 or y_type";
+    return nullptr;
+}
+
+som_status steps_ok(const char *who, const som_adamw_tensor *t, int64_t count, bool bits8, bool params)
+{
+    if (count < 0 || count > INT32_MAX) return bad(who, "count is out of range");
+    if (count > 0 && !t) return bad(who, kNull);
+    int64_t total = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        const som_adamw_tensor &x = t[i];
+        if (x.size < 0 || x.size > ((int64_t)1 << 38) || total > ((int64_t)1 << 43)) return bad(who, "a size is out of range");
+        total += x.size;
+        if (params && (!any_type(x.type) || !any_type(x.grad_type))) return bad(who, "unknown type");
+        if (x.size == 0) continue;
+        if (!x.m || !x.v || (params && (!x.param || !x.grad)) || (bits8 && (!x.m_scales || !x.v_scales))) return bad(who, kNull);
+        if (!bits8 && (odd(x.m, SOM_F32) || odd(x.v, SOM_F32))) return bad(who, kNotAligned);
+        if (params && (odd(x.param, x.type) || odd(x.grad, x.grad_type) || odd(x.master, SOM_F32))) return bad(who, kNotAligned);
+    }
+    return SOM_OK;
+}
+
+// Tables of the tensors, as many as a launch takes at a time; f(table).
+template <typename F> hipError_t over_tables(const som_adamw_tensor *tensors, int64_t count, F f)
+{
+    int64_t total = 0;
+    for (int64_t i = 0; i < count; ++i) total += tensors[i].size;
+    const int64_t chunk = som::adamw_chunk(total);
+    for (int64_t i = 0; i < count;) {
+        som::AdamwTable t;
+        t.count = 0;
+        t.number = (int32_t)i;
+        t.chunk = chunk;
+        t.first[0] = 0;
+        for (; i < count && t.count < som::kAdamwTensors; ++i) {
+            const som_adamw_tensor &x = tensors[i];
+            const int64_t chunks = (x.size + chunk - 1) / chunk;
+            // a launch has fewer than 2^32 threads, and 2^38 elements (a tensor's most) 2^23 chunks
+            if (t.count > 0 && t.first[t.count] + chunks > (1 << 23)) break;
+            const int j = t.count++;
+            t.param[j] = x.param, t.grad[j] = x.grad, t.m[j] = x.m, t.v[j] = x.v;
+            t.m_scales[j] = x.m_scales, t.v_scales[j] = x.v_scales, t.master[j] = x.master;
+            t.size[j] = x.size, t.type[j] = (int8_t)x.type, t.grad_type[j] = (int8_t)x.grad_type;
+            t.first[j + 1] = t.first[j] + (int32_t)chunks;
+        }
+        const hipError_t e = f(t, i);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+const char *product_sizes(int64_t N, int64_t K, int64_t M)
+{
+    return rows_ok(N) && dim_ok(K) && dim_ok(M) ? nullptr : "need 0 <= N, 1 <= K, M, all below 2^30";
+}
+
+}  // namespace
+
+extern "C" {
+
+som_status som_layer_norm(int32_t type, const void *X, int64_t ldx, const void *weight, const void *bias,
+                          int32_t weight_type, double eps, void *Y, int64_t ldy, int32_t y_type, double *stats,
+                          int64_t N, int64_t D, void *stream)
+{
+    const char *who = "som_layer_norm";
+    if (const char *what = norm_types(type, y_type, weight_type)) return bad(who, what);
+    if (!rows_ok(N) || !width_ok(D)) return bad(who, "need 0 <= N < 2^30, 1 <= D < 2^20");
+    if (!(eps >= (double)FLT_MIN) || std::isinf(eps)) return bad(who, "eps must be at least 2^-126 and finite");
+    if (N == 0) return ok();
+    if (!X || !Y) return bad(who, kNull);
+    if (ldx < D || ldy < D) return bad(who, kStride);
+    if (odd(X, type) || odd(Y, y_type) || odd(weight, weight_type) || odd(bias, weight_type) || off(stats, 8))
+        return bad(who, kNotAligned);
+    som::NormArgs a{};
+    a.x = X, a.ldx = ldx, a.weight = weight, a.bias = bias, a.weights_f32 = weight_type == SOM_F32;
+    a.eps = eps, a.y = Y, a.ldy = ldy, a.stats = stats, a.N = N, a.D = (int32_t)D;
+    return done(som::launch_norm_rows(type, y_type, a, static_cast<hipStream_t>(stream)), who);
+}
+
+size_t som_layer_norm_bwd_workspace_bytes(int64_t N, int64_t D)
+{
+    if (!rows_ok(N) || !width_ok(D)) return 0;
+    return align256((size_t)som::norm_parts(N) * 2 * (size_t)D * 4) + align256((size_t)N * 8);
+}
+
+som_status som_layer_norm_bwd(int32_t type, const void *X, int64_t ldx, const void *weight, int32_t weight_type,
+                              const void *dY, int64_t lddy, int32_t y_type, const double *stats, const void *add,
+                              int64_t ldadd, void *dX, int64_t lddx, void *dweight, void *dbias, int64_t N, int64_t D,
+                              void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "som_layer_norm_bwd";
+    if (const char *what = norm_types(type, y_type, weight_type)) return bad(who, what);
+    if (!rows_ok(N) || !width_ok(D)) return bad(who, "need 0 <= N < 2^30, 1 <= D < 2^20");
+    if (N > 0 && (!X || !dY || !stats)) return bad(who, kNull);
+    if (ldx < D || lddy < D || (add && ldadd < D) || (dX && lddx < D)) return bad(who, kStride);
+    if (odd(X, type) || odd(dY, y_type) || odd(weight, weight_type) || off(stats, 8) || odd(add, type) || odd(dX, type) ||
+        odd(dweight, weight_type) || odd(dbias, weight_type))
+        return bad(who, kNotAligned);
+    const som_status st = check_workspace(who, workspace, workspace_bytes, som_layer_norm_bwd_workspace_bytes(N, D));
+    if (st != SOM_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool sums = dweight || dbias;
+    som::NormArgs a{};
+    a.x = X, a.ldx = ldx, a.weight = weight, a.weights_f32 = weight_type == SOM_F32;
+    a.y = const_cast<void *>(dY), a.ldy = lddy, a.stats = const_cast<double *>(stats), a.N = N, a.D = (int32_t)D;
+    a.add = add, a.lda = ldadd, a.dx = dX, a.lddx = lddx;
+    a.n_parts = som::norm_parts(N);
+    a.part_rows = (N + a.n_parts - 1) / a.n_parts;
+    a.parts = sums ? static_cast<float *>(workspace) : nullptr;
+    a.means = reinterpret_cast<float *>(static_cast<char *>(workspace) + align256((size_t)a.n_parts * 2 * (size_t)D * 4));
+    if (N > 0 && (dX || sums)) {
+        const hipError_t e = som::launch_norm_grad(type, y_type, a, s);
+        if (e != hipSuccess) return done(e, who);
+    }
+    if (!sums) return ok();
+    return done(som::launch_norm_sums(a.parts, N > 0 ? a.n_parts : 0, a.D, dweight, dbias, weight_type, s), who);
+}
+
+som_status som_adamw(const som_adamw_tensor *tensors, int64_t count, const som_adamw_config *config, void *stream)
+{
+    const char *who = "som_adamw";
+    if (!config) return bad(who, kNull);
+    const som_adamw_config &c = *config;
+    if (c.bits != 32 && c.bits != 8) return bad(who, "bits must be 32 or 8");
+    if (!(c.lr >= 0) || std::isinf(c.lr) || !(c.weight_decay >= 0) || std::isinf(c.weight_decay))
+        return bad(who, "lr and weight_decay must be finite and not negative");
+    if (!(c.beta1 >= 0 && c.beta1 < 1) || !(c.beta2 >= 0 && c.beta2 < 1)) return bad(who, "beta1 and beta2 must be in [0, 1)");
+    if (!(c.eps >= (double)FLT_MIN) || c.eps > (double)FLT_MAX) return bad(who, "eps must be at least 2^-126 and finite");
+    if (!(std::fabs(c.grad_scale) <= (double)FLT_MAX)) return bad(who, "grad_scale must be finite");
+    if (c.step < 1 || c.step > INT32_MAX) return bad(who, "step must be 1 ... 2^31 - 1");
+    if (c.reserved[0] || c.reserved[1] || c.reserved[2] || c.reserved[3]) return bad(who, "reserved fields must be zero");
+    if (off(c.lr_at, 4) || off(c.step_at, 4) || off(c.norm, 4)) return bad(who, kNotAligned);
+    const bool bits8 = c.bits == 8;
+    const som_status st = steps_ok(who, tensors, count, bits8, true);
+    if (st != SOM_OK) return st;
+    som::AdamwArgs a{};
+    a.lr = c.lr, a.beta1 = c.beta1, a.beta2 = c.beta2, a.weight_decay = c.weight_decay;
+    a.rates.set(c.lr, c.beta1, c.beta2, c.weight_decay, (uint32_t)c.step);
+    a.rates.eps = (float)c.eps, a.rates.grad = (float)c.grad_scale;
+    a.seed = c.seed, a.lr_at = c.lr_at, a.step_at = c.step_at, a.norm = c.norm;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return done(over_tables(tensors, count, [&](som::AdamwTable &t, int64_t) { return som::launch_adamw(t, bits8, a, s); }), who);
+}
+
+som_status som_adamw_values(const som_adamw_tensor *tensors, int64_t count, float *const *m_out, float *const *v_out,
+                            void *stream)
+{
+    const char *who = "som_adamw_values";
+    const som_status st = steps_ok(who, tensors, count, true, false);
+    if (st != SOM_OK) return st;
+    if (count > 0 && (!m_out || !v_out)) return bad(who, kNull);
+    for (int64_t i = 0; i < count; ++i) {
+        if (tensors[i].size > 0 && (!m_out[i] || !v_out[i])) return bad(who, kNull);
+        if (odd(m_out[i], SOM_F32) || odd(v_out[i], SOM_F32)) return bad(who, kNotAligned);
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const auto launch = [&](som::AdamwTable &t, int64_t end) {
+        for (int j = 0; j < t.count; ++j) {
+            const int64_t i = end - t.count + j;
+            t.param[j] = m_out[i], t.master[j] = v_out[i];
+        }
+        return som::launch_adamw_values(t, s);
+    };
+    return done(over_tables(tensors, count, launch), who);
+}
+
+static const char *mx4_arguments(int32_t type, const void *x, int64_t ldx, int32_t columns, const void *codes,
+                                 const void *scales, int64_t n, int64_t K)
+{
+    if (!any_type(type)) return "type must be SOM_F32, SOM_F16 or SOM_BF16";
+    if (columns != 0 && columns != 1) return "columns must be 0 or 1";
+    if (!rows_ok(n) || !dim_ok(K)) return "need 0 <= n, 1 <= K, both below 2^30";
+    if (n == 0) return nullptr;
+    if (!x || !codes || !scales) return kNull;
+    if (ldx < (columns ? n : K)) return kStride;
+    if (odd(x, type)) return kNotAligned;
+    if (off(codes, 16)) return "codes must be 16-byte aligned";
+    return nullptr;
+}
+
+som_status som_mx4_quantise(int32_t type, const void *X, int64_t ldx, int32_t columns, uint8_t *codes, uint8_t *scales,
+                            int64_t n, int64_t K, void *stream)
+{
+    const char *who = "som_mx4_quantise";
+    if (const char *what = mx4_arguments(type, X, ldx, columns, codes, scales, n, K)) return bad(who, what);
+    if (n == 0) return ok();
+    som::FourArgs a{X, ldx, codes, scales, n, K};
+    return done(som::launch_mx4_quantise(type, columns != 0, a, static_cast<hipStream_t>(stream)), who);
+}
+
+som_status som_mx4_values(int32_t type, const uint8_t *codes, const uint8_t *scales, int32_t columns, void *Y,
+                          int64_t ldy, int64_t n, int64_t K, void *stream)
+{
+    const char *who = "som_mx4_values";
+    if (const char *what = mx4_arguments(type, Y, ldy, columns, codes, scales, n, K)) return bad(who, what);
+    if (n == 0) return ok();
+    som::FourArgs a{nullptr, 0, const_cast<uint8_t *>(codes), const_cast<uint8_t *>(scales), n, K};
+    return done(som::launch_mx4_values(type, columns != 0, a, Y, ldy, static_cast<hipStream_t>(stream)), who);
+}
+
+size_t som_mx4_linear_workspace_bytes(int64_t N, int64_t K, int64_t M, int32_t packed)
+{
+    (void)N, (void)K, (void)M, (void)packed;
+    return 0;
+}
+
+som_status som_mx4_linear(int32_t type, const void *X, int64_t ldx, const uint8_t *x_scales, const uint8_t *w_codes,
+                          const uint8_t *w_scales, const void *bias, int32_t bias_type, int32_t act,
+                          const void *residual, int64_t ldr, void *Y, int64_t ldy, int32_t y_type, int64_t N, int64_t K,
+                          int64_t M, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "som_mx4_linear";
+    if (!half_type(type)) return bad(who, "type must be SOM_F16 or SOM_BF16");
+    if (const char *what = product_sizes(N, K, M)) return bad(who, what);
+    if (act < SOM_ACT_NONE || act > SOM_ACT_SILU) return bad(who, "unknown activation");
+    if (y_type != SOM_F32 && y_type != type) return bad(who, "y_type must be SOM_F32 or type");
+    if (bias && bias_type != SOM_F32 && bias_type != type) return bad(who, "bias_type must be SOM_F32 or type");
+    if (N == 0) return ok();
+    if (!X || !w_codes || !w_scales || !Y) return bad(who, kNull);
+    if ((!x_scales && ldx < K) || ldy < M || (residual && ldr < M)) return bad(who, kStride);
+    if (off(w_codes, 16) || (x_scales && off(X, 16))) return bad(who, "codes must be 16-byte aligned");
+    if ((!x_scales && odd(X, type)) || odd(Y, y_type) || odd(residual, type) || (bias && odd(bias, bias_type)))
+        return bad(who, kNotAligned);
+    const som_status st = check_workspace(who, workspace, workspace_bytes,
+                                          som_mx4_linear_workspace_bytes(N, K, M, x_scales ? 1 : 0));
+    if (st != SOM_OK) return st;
+    som::FourProduct p{};
+    p.x = X, p.ldx = ldx, p.x_scales = x_scales, p.w = w_codes, p.w_scales = w_scales;
+    p.bias = bias, p.bias_f32 = bias_type == SOM_F32, p.act = act, p.res = residual, p.ldr = ldr;
+    p.y = Y, p.ldy = ldy, p.y_f32 = y_type == SOM_F32, p.N = N, p.K = K, p.M = M;
+    return done(som::launch_mx4_few(type == SOM_BF16, p, static_cast<hipStream_t>(stream)), who);
+}
+
+}  // extern "C"

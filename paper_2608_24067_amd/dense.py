@@ -1,7 +1,8 @@
 """Dense rows on a map: ctypes binding of include/som_dense.h. Argument marshalling only.
 
 Products of dense rows with a feature-major matrix (a codebook's scores, a layer), routing of rows to their best
-units, the units' experts, and clipping of all gradients to a norm. As in ``som``, every function checks its tensors
+units, the units' experts, clipping of all gradients to a norm; layer norm, AdamW's step, and rows and matrices in 4
+bits with their products. As in ``som``, every function checks its tensors
 and passes pointers and the current torch stream of the tensors' device to the C entry point of the same name.
 Matrices and rows may have any row stride; the elements of a row must be adjacent.
 
@@ -13,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -344,3 +346,301 @@ def clip(tensors, max_norm: float, out=None, norm=None, workspace=None):
     _check(lib.som_clip(ins, tos, sizes, types, n, float(max_norm), _vec(norm, "norm", (1,), torch.float32, dev),
                         *_pointer(ws), _stream(norm)), "som_clip")
     return outs, norm
+
+
+# ------------------------------------------------------------------ layer norm
+
+def _on(device, call, *args):
+    """A call with `device` as the current one, which a launch on one of its streams needs."""
+    if device.index == torch.cuda.current_device():
+        return call(*args)
+    with torch.cuda.device(device):
+        return call(*args)
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None, out_dtype=None, stats=None):
+    """(x - mean) / sqrt(var + eps) * weight + bias over each row of x [N, D].
+
+    x is float32, float16 or bfloat16; the result (``out``, or a new tensor of ``out_dtype``) is of x's type, or of any
+    of the three for float32 rows. weight and bias [D], or None, are both float32 or both of the result's type.
+    ``stats`` float64 [N, 2] takes each row's mean and 1 / sqrt(var + eps), which layer_norm_bwd needs. ``out`` may be x.
+    """
+    kind, dev = _type(x, "x", halves=False), x.device
+    N, D = _two(x, "x")
+    if out is None:
+        out = torch.empty(N, D, dtype=out_dtype or x.dtype, device=dev)
+    to = _type(out, "out", halves=False)
+    xp, ldx = _mat(x, "x", (N, D), x.dtype, dev)
+    yp, ldy = _mat(out, "out", (N, D), out.dtype, dev)
+    some = weight if weight is not None else bias
+    wdt = some.dtype if isinstance(some, torch.Tensor) and some.dtype == out.dtype else torch.float32
+    wp = _vec(weight, "weight", (D,), wdt, dev) if weight is not None else None
+    bp = _vec(bias, "bias", (D,), wdt, dev) if bias is not None else None
+    sp = _vec(stats, "stats", (N, 2), torch.float64, dev) if stats is not None else None
+    _check(_on(dev, load().som_layer_norm, kind, xp, ldx, wp, bp, _TYPES[wdt], float(eps), yp, ldy, to, sp, N, D,
+               _stream(x)), "som_layer_norm")
+    return out
+
+
+def layer_norm_bwd(x, dy, stats, weight=None, add=None, out=None, weight_dtype=None, workspace=None):
+    """(dx, dweight, dbias) of layer_norm, from dy [N, D] of its result's type and the ``stats`` it wrote.
+
+    ``add`` [N, D] of x's type is added to dx: the gradient that reaches x by another way, as round a layer. ``out``
+    may pass the three tensors; one that is None is not computed. dweight and dbias are of the weight's type
+    (``weight_dtype`` where there is none: float32, the default, or dy's type). ``out``'s dx may be ``add`` or dy.
+    """
+    kind, dev = _type(x, "x", halves=False), x.device
+    N, D = _two(x, "x")
+    g = _type(dy, "dy", halves=False)
+    wdt = weight.dtype if isinstance(weight, torch.Tensor) else weight_dtype
+    if out is None:
+        wdt = wdt or torch.float32
+        out = (torch.empty(N, D, dtype=x.dtype, device=dev), torch.empty(D, dtype=wdt, device=dev),
+               torch.empty(D, dtype=wdt, device=dev))
+    dx, dw, db = out
+    wdt = wdt or next((t.dtype for t in (dw, db) if isinstance(t, torch.Tensor)), torch.float32)
+    if wdt not in (torch.float32, dy.dtype):
+        raise TypeError(f"weight, dweight and dbias must be float32 or {dy.dtype} (got {wdt})")
+    lib = load()
+    ws = _work(workspace, lib.som_layer_norm_bwd_workspace_bytes(N, D), dev)
+    xp, ldx = _mat(x, "x", (N, D), x.dtype, dev)
+    gp, ldg = _mat(dy, "dy", (N, D), dy.dtype, dev)
+    ap, lda = _mat(add, "add", (N, D), x.dtype, dev) if add is not None else (None, 0)
+    dxp, lddx = _mat(dx, "dx", (N, D), x.dtype, dev) if dx is not None else (None, 0)
+    wp = _vec(weight, "weight", (D,), wdt, dev) if weight is not None else None
+    dwp = _vec(dw, "dweight", (D,), wdt, dev) if dw is not None else None
+    dbp = _vec(db, "dbias", (D,), wdt, dev) if db is not None else None
+    _check(_on(dev, lib.som_layer_norm_bwd, kind, xp, ldx, wp, _TYPES[wdt], gp, ldg, g,
+               _vec(stats, "stats", (N, 2), torch.float64, dev), ap, lda, dxp, lddx, dwp, dbp, N, D, *_pointer(ws),
+               _stream(x)), "som_layer_norm_bwd")
+    return tuple(out)
+
+
+# ------------------------------------------------------------------ AdamW
+
+class AdamwState(NamedTuple):
+    """A tensor's running means: float32 like the tensor, or, with scales, in 8 bits (uint8 codes and blocks' scales);
+    and its float32 copy, or None."""
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scales: Optional[torch.Tensor] = None
+    v_scales: Optional[torch.Tensor] = None
+    master: Optional[torch.Tensor] = None
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scales", "v_scales", "master")] + [
+        ("size", ctypes.c_int64), ("type", ctypes.c_int32), ("grad_type", ctypes.c_int32)]
+
+
+class _AdamwConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + [
+        ("step", ctypes.c_int64), ("bits", ctypes.c_int32), ("seed", ctypes.c_uint32), ("lr_at", ctypes.c_void_p),
+        ("step_at", ctypes.c_void_p), ("norm", ctypes.c_void_p), ("reserved", ctypes.c_int64 * 4)]
+
+
+STATE_BLOCK = 256  # values of a block of 8-bit states
+
+
+def adamw_state(param, bits: int = 32, master: bool = False) -> AdamwState:
+    """The state of a parameter before its first step: zeros, in 32 bits or 8, and with ``master`` a float32 copy."""
+    _type(param, "param", halves=False)
+    copy = param.detach().float().clone().contiguous() if master else None
+    if bits == 32:
+        m, v = (torch.zeros(param.shape, dtype=torch.float32, device=param.device) for _ in range(2))
+        return AdamwState(m, v, None, None, copy)
+    if bits != 8:
+        raise ValueError(f"bits must be 32 or 8 (got {bits})")
+    blocks = (param.numel() + STATE_BLOCK - 1) // STATE_BLOCK
+    m, v = (torch.zeros(param.shape, dtype=torch.uint8, device=param.device) for _ in range(2))
+    ms, vs = (torch.zeros(blocks, dtype=torch.uint8, device=param.device) for _ in range(2))
+    return AdamwState(m, v, ms, vs, copy)
+
+
+def _held(t, name, n, dtype, at):
+    """The pointer of a contiguous tensor of n elements on device number `at`."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.numel() != n or t.get_device() != at or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on the parameters' GPU")
+    return t.data_ptr()
+
+
+def _state_into(x, state, n, eight, at):
+    """Checks a state and puts its pointers into the C structure."""
+    m, v, ms, vs, master = state
+    kind = torch.uint8 if eight else torch.float32
+    x.m, x.v, x.size = _held(m, "m", n, kind, at), _held(v, "v", n, kind, at), n
+    if eight:
+        blocks = (n + STATE_BLOCK - 1) // STATE_BLOCK
+        x.m_scales = _held(ms, "m_scales", blocks, torch.uint8, at)
+        x.v_scales = _held(vs, "v_scales", blocks, torch.uint8, at)
+    elif ms is not None or vs is not None:
+        raise ValueError("the states must all be in 32 bits, or all in 8")
+    if master is not None:
+        x.master = _held(master, "master", n, torch.float32, at)
+
+
+def _scalar_at(t, name, dtype, dev):
+    return _vec(t, name, (1,), dtype, dev)
+
+
+def adamw(params, grads, states, step, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+          grad_scale: float = 1.0, seed: int = 0, norm=None):
+    """One step of AdamW over all parameters, in place.
+
+    The parameters and their gradients are contiguous, each float32, float16 or bfloat16, on one device; states are
+    AdamwState (adamw_state), all in 32 bits or all in 8. A state's master, where it has one, is what the step reads and
+    updates; the parameter takes its rounded value. ``step`` is this step's number from 1 on, ``lr`` the rate; either
+    may be a tensor of one element on the device (int32, float32), so that a captured step goes on when replayed.
+    Gradients are multiplied by ``grad_scale``. ``norm``, float32 [1], as clip returns it: where it is infinite or NaN
+    the step is left out. ``seed`` (0 ... 2^32 - 1) decides the rounding of 8-bit states, together with the step.
+    No tensor may hold elements of another.
+    """
+    params, grads, states = list(params), list(grads), list(states)
+    n = len(params)
+    if len(grads) != n or len(states) != n:
+        raise ValueError(f"grads and states must hold {n} entries each")
+    if not n:
+        return
+    if not isinstance(params[0], torch.Tensor) or not params[0].is_cuda:
+        raise ValueError("the parameters must be on the GPU")
+    dev = params[0].device
+    at, eight = dev.index, states[0][2] is not None
+    table = (_AdamwTensor * n)()
+    for x, p, g, state in zip(table, params, grads, states):
+        for t, name in ((p, "params"), (g, "grads")):
+            if not isinstance(t, torch.Tensor) or t.dtype not in _TYPES:
+                _type(t, name, halves=False)
+        m = p.numel()
+        x.param, x.grad = _held(p, "params", m, p.dtype, at), _held(g, "grads", m, g.dtype, at)
+        x.type, x.grad_type = _TYPES[p.dtype], _TYPES[g.dtype]
+        if (state[2] is not None) != eight:
+            raise ValueError("the states must all be in 32 bits, or all in 8")
+        _state_into(x, state, m, eight, at)
+    if len({x.param for x in table if x.size}) < sum(1 for x in table if x.size):
+        raise ValueError("params holds a tensor twice")
+    c = _AdamwConfig()
+    if isinstance(lr, torch.Tensor):
+        c.lr_at, lr = _scalar_at(lr, "lr", torch.float32, dev), 0.0
+    if isinstance(step, torch.Tensor):
+        c.step_at, step = _scalar_at(step, "step", torch.int32, dev), 1
+    if not 0 <= int(seed) < 1 << 32:
+        raise ValueError("seed must be 0 ... 2^32 - 1")
+    c.lr, c.beta1, c.beta2, c.eps, c.weight_decay = float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay)
+    c.grad_scale, c.step, c.bits, c.seed = float(grad_scale), int(step), 8 if eight else 32, int(seed)
+    if norm is not None:
+        c.norm = _scalar_at(norm, "norm", torch.float32, dev)
+    _check(_on(dev, load().som_adamw, table, n, ctypes.byref(c), _stream(params[0])), "som_adamw")
+
+
+def adamw_values(states, out=None):
+    """(m, v) of 8-bit states as lists of float32 tensors; ``out`` may pass both lists."""
+    states = list(states)
+    n = len(states)
+    if out is None:
+        out = tuple([torch.empty(s[0].shape, dtype=torch.float32, device=s[0].device) for s in states] for _ in range(2))
+    if len(out[0]) != n or len(out[1]) != n:
+        raise ValueError(f"out must hold two lists of {n} tensors")
+    if not n:
+        return out
+    if not isinstance(states[0][0], torch.Tensor) or not states[0][0].is_cuda:
+        raise ValueError("the states must be on the GPU")
+    dev = states[0][0].device
+    table = (_AdamwTensor * n)()
+    for x, state in zip(table, states):
+        _state_into(x, AdamwState(*state[:4]), state[0].numel(), True, dev.index)
+    tos = [(ctypes.c_void_p * n)(*[_held(t, name, x.size, torch.float32, dev.index) for t, x in zip(ts, table)])
+           for ts, name in zip(out, ("m", "v"))]
+    _check(_on(dev, load().som_adamw_values, table, n, tos[0], tos[1], _stream(states[0][0])), "som_adamw_values")
+    return out
+
+
+# ------------------------------------------------------------------ 4 bits
+
+class Mx4(NamedTuple):
+    """Rows (or a matrix's columns) in 4 bits: codes uint8 [n, 16 ceil(width / 32)], scales uint8 [n, ceil(width / 32)]
+    (som_dense.h says what they stand for), and how many features they hold."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    width: int
+
+
+def _four(q, name, width, dev):
+    """Pointers and the number of rows of an Mx4."""
+    codes, scales, K = q
+    if K != width or width < 1:
+        raise ValueError(f"{name} must hold {width} features (got {K})")
+    blocks = (width + 31) // 32
+    n = codes.shape[0] if isinstance(codes, torch.Tensor) and codes.dim() == 2 else -1
+    return _vec(codes, name + ".codes", (n, 16 * blocks), torch.uint8, dev), _vec(scales, name + ".scales", (n, blocks),
+                                                                                  torch.uint8, dev), n
+
+
+def mx4_quantise(x, columns: bool = False, out=None) -> Mx4:
+    """x in 4 bits: its rows [n, K], or with ``columns`` those of a feature-major matrix [K, n], as linear's W.
+
+    x is float32, float16 or bfloat16. Blocks of 32 features share a power of two, the exponent of the largest less 2;
+    values are rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times it, ties to the even code. A block with an
+    infinity or a NaN stands for NaN. ``out`` may pass (codes, scales).
+    """
+    kind, dev = _type(x, "x", halves=False), x.device
+    rows, width = _two(x, "x")
+    xp, ldx = _mat(x, "x", (rows, width), x.dtype, dev)
+    n, K = (width, rows) if columns else (rows, width)
+    blocks = (K + 31) // 32
+    if out is None:
+        out = (torch.empty(n, 16 * blocks, dtype=torch.uint8, device=dev), torch.empty(n, blocks, dtype=torch.uint8, device=dev))
+    q = Mx4(out[0], out[1], K)
+    cp = _vec(q.codes, "codes", (n, 16 * blocks), torch.uint8, dev)
+    sp = _vec(q.scales, "scales", (n, blocks), torch.uint8, dev)
+    _check(_on(dev, load().som_mx4_quantise, kind, xp, ldx, 1 if columns else 0, cp, sp, n, K, _stream(x)), "som_mx4_quantise")
+    return q
+
+
+def mx4_values(q: Mx4, columns: bool = False, dtype=None, out=None):
+    """What q stands for, rounded to ``dtype`` (float32, float16 or bfloat16, the default, which holds it exactly but for
+    the smallest scales): rows [n, width], or with ``columns`` a feature-major matrix [width, n]."""
+    dev = q[0].device
+    cp, sp, n = _four(q, "q", q[2], dev)
+    shape = (q[2], n) if columns else (n, q[2])
+    if out is None:
+        out = torch.empty(shape, dtype=dtype or torch.bfloat16, device=dev)
+    kind = _type(out, "out", halves=False)
+    yp, ldy = _mat(out, "out", shape, out.dtype, dev)
+    _check(_on(dev, load().som_mx4_values, kind, cp, sp, 1 if columns else 0, yp, ldy, n, q[2], _stream(out)), "som_mx4_values")
+    return out
+
+
+def mx4_linear(x, W: Mx4, bias=None, residual=None, act: str = "none", out=None, out_dtype=None, dtype=None,
+               workspace=None):
+    """residual + act(x W + bias), as linear, with W in 4 bits (mx4_quantise(W, columns=True)).
+
+    x is rows [N, K] in float16 or bfloat16, or in 4 bits (an Mx4; the result's type is then ``dtype``, that of out,
+    residual or a 16-bit bias, or bfloat16). bias, residual and the result are as in linear.
+    """
+    packed = isinstance(x, tuple)
+    if packed:
+        dev, K = x[0].device, x[2]
+        xp, xs, N = _four(x, "x", K, dev)
+        ldx, at = 0, x[0]
+        if dtype is None:
+            dtype = next((t.dtype for t in (out, residual, bias) if isinstance(t, torch.Tensor) and t.dtype != torch.float32),
+                         torch.bfloat16)
+    else:
+        _type(x, "x")
+        dev, at, dtype, xs = x.device, x, x.dtype, None
+        N, K = _two(x, "x")
+        xp, ldx = _mat(x, "x", (N, K), dtype, dev)
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"dtype must be float16 or bfloat16 (got {dtype})")
+    wp, ws, M = _four(W, "W", K, dev)
+    if out is None:
+        out = torch.empty(N, M, dtype=out_dtype or dtype, device=dev)
+    yp, ldy = _mat(out, "out", (N, M), out.dtype if out.dtype in (torch.float32, dtype) else dtype, dev)
+    bp = _vec(bias, "bias", (M,), (torch.float32, dtype), dev) if bias is not None else None
+    rp, ldr = _mat(residual, "residual", (N, M), dtype, dev) if residual is not None else (None, 0)
+    lib = load()
+    work = _work(workspace, lib.som_mx4_linear_workspace_bytes(N, K, M, 1 if packed else 0), dev)
+    _check(_on(dev, lib.som_mx4_linear, _TYPES[dtype], xp, ldx, xs, wp, ws, bp,
+               _TYPES[bias.dtype] if bias is not None else F32, _named(_ACTS, act, "act"), rp, ldr, yp, ldy,
+               _TYPES[out.dtype], N, K, M, *_pointer(work), _stream(at)), "som_mx4_linear")
+    return out

@@ -33,6 +33,8 @@ EXPORTS = (
     "som_validate_csr_host", "som_last_error",
     "som_linear", "som_linear_bwd_workspace_bytes", "som_linear_bwd", "som_route", "som_route_bwd",
     "som_experts_workspace_bytes", "som_experts", "som_experts_bwd", "som_clip_workspace_bytes", "som_clip",
+    "som_layer_norm", "som_layer_norm_bwd_workspace_bytes", "som_layer_norm_bwd", "som_adamw", "som_adamw_values",
+    "som_mx4_quantise", "som_mx4_values", "som_mx4_linear_workspace_bytes", "som_mx4_linear",
 )
 
 
@@ -124,10 +126,24 @@ def load():
                                     i32, i64, i64, i64, vp, sz, vp]
     lib.som_clip_workspace_bytes.argtypes = [vp, i64]
     lib.som_clip.argtypes = [vp, vp, vp, vp, i64, f32, vp, vp, sz, vp]
-    for name in ("som_linear_bwd_workspace_bytes", "som_experts_workspace_bytes", "som_clip_workspace_bytes"):
+    f64 = ctypes.c_double
+    lib.som_layer_norm.argtypes = [i32, vp, i64, vp, vp, i32, f64, vp, i64, i32, vp, i64, i64, vp]
+    lib.som_layer_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+    lib.som_layer_norm_bwd.argtypes = [i32, vp, i64, vp, i32, vp, i64, i32, vp, vp, i64, vp, i64, vp, vp, i64, i64, vp,
+                                       sz, vp]
+    lib.som_adamw.argtypes = [vp, i64, vp, vp]
+    lib.som_adamw_values.argtypes = [vp, i64, vp, vp, vp]
+    lib.som_mx4_quantise.argtypes = [i32, vp, i64, i32, vp, vp, i64, i64, vp]
+    lib.som_mx4_values.argtypes = [i32, vp, vp, i32, vp, i64, i64, i64, vp]
+    lib.som_mx4_linear_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.som_mx4_linear.argtypes = [i32, vp, i64, vp, vp, vp, vp, i32, i32, vp, i64, vp, i64, i32, i64, i64, i64, vp, sz,
+                                   vp]
+    for name in ("som_linear_bwd_workspace_bytes", "som_experts_workspace_bytes", "som_clip_workspace_bytes",
+                 "som_layer_norm_bwd_workspace_bytes", "som_mx4_linear_workspace_bytes"):
         getattr(lib, name).restype = sz
     for name in ("som_linear", "som_linear_bwd", "som_route", "som_route_bwd", "som_experts", "som_experts_bwd",
-                 "som_clip"):
+                 "som_clip", "som_layer_norm", "som_layer_norm_bwd", "som_adamw", "som_adamw_values",
+                 "som_mx4_quantise", "som_mx4_values", "som_mx4_linear"):
         getattr(lib, name).restype = ctypes.c_int
     lib.som_last_error.argtypes = []
     lib.som_last_error.restype = ctypes.c_char_p

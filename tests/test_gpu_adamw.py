@@ -1,0 +1,268 @@
+"""som_adamw and som_adamw_values against 64 bits, and 8-bit states bit for bit, on the GPU."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import layer_ref as ref
+import paper_2608_24067_amd.dense as dense
+from dense_ref import check, wide
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+HOW = dict(lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01)
+
+
+def tensors(seed, sizes, dtype, grad, dev, size=1e-2, offset=0):
+    g = torch.Generator().manual_seed(seed)
+    params, grads = [], []
+    for n in sizes:
+        for to, t, scale in ((params, dtype, 1.0), (grads, grad, size)):
+            v = torch.empty(n + offset, dtype=t, device=dev)[offset:]
+            to.append(v.copy_((torch.randn(n, generator=g) * scale).to(t)))
+    return params, grads
+
+
+def copies(states):
+    return [dense.AdamwState(*[t.clone() if t is not None else None for t in s]) for s in states]
+
+
+def fp32_states(seed, params, dev, master=False, offset=0):
+    g = torch.Generator().manual_seed(seed)
+    out = []
+    for p in params:
+        n = p.numel()
+        m, v = (torch.empty(n + offset, device=dev)[offset:] for _ in range(2))
+        m.copy_(torch.randn(n, generator=g) * 1e-3)
+        v.copy_(torch.rand(n, generator=g) * 1e-6)
+        copy = None
+        if master:
+            copy = torch.empty(n + offset, device=dev)[offset:]
+            copy.copy_(wide(p).float() + torch.randn(n, generator=g) * 1e-5)
+        out.append(dense.AdamwState(m, v, None, None, copy))
+    return out
+
+
+@pytest.mark.parametrize("dtype,grad", [(F32, F32), (BF16, BF16), (F16, F16), (BF16, F32), (F32, F16)])
+@pytest.mark.parametrize("master", [False, True])
+@pytest.mark.parametrize("sizes,offset", [([1], 0), ([3, 0, 2048, 2049], 0), ([5] * 100, 0), ([70001, 8, 300], 1),
+                                          ([1 << 20], 0)])
+def test_step(dev, dtype, grad, master, sizes, offset):
+    params, grads = tensors(1, sizes, dtype, grad, dev, offset=offset)
+    states = fp32_states(2, params, dev, master, offset)
+    before, old = [p.clone() for p in params], copies(states)
+    dense.adamw(params, grads, states, 7, **HOW)
+    for p, g, s, b, o in zip(params, grads, states, before, old):
+        source = o.master if master else b
+        (want, off), (m, off_m), (v, off_v) = ref.adamw(source, g, o.m, o.v, 7, **HOW)
+        check(s.m, m, off_m, "m")
+        check(s.v, v, off_v, "v")
+        check(p, want, off + ref.E * (want.abs() + off), "p")
+        if master:
+            check(s.master, want, off, "master")
+            assert torch.equal(p, s.master.to(dtype))
+
+
+@pytest.mark.parametrize("how", [dict(lr=0.0), dict(weight_decay=0.0), dict(betas=(0.0, 0.0)), dict(eps=1.0),
+                                 dict(grad_scale=1 / 1024), dict(lr=0.5, weight_decay=2.0)])
+@pytest.mark.parametrize("step", [1, 2, 100, 2 ** 31 - 1])
+def test_settings(dev, how, step):
+    how = {**HOW, **how}
+    params, grads = tensors(3, [1000, 77], F32, F32, dev)
+    states = [dense.adamw_state(p) for p in params] if step == 1 else fp32_states(4, params, dev)
+    before, old = [p.clone() for p in params], copies(states)
+    dense.adamw(params, grads, states, step, **how)
+    for p, g, s, b, o in zip(params, grads, states, before, old):
+        (want, off), (m, off_m), (v, off_v) = ref.adamw(b, g, o.m, o.v, step, **how)
+        check(p, want, off, "p")
+        check(s.m, m, off_m, "m")
+        check(s.v, v, off_v, "v")
+
+
+def eight(seed, params, dev):
+    """States in 8 bits with values over many sizes, some blocks empty, some of one value, some of NaN."""
+    rng = np.random.default_rng(seed)
+    out = []
+    for j, p in enumerate(params):
+        n = p.numel()
+        size = np.exp(rng.normal(size=n) * 3 - 12)
+        m, v = rng.normal(size=n) * size, rng.random(n) * size * size
+        m[rng.random(n) < 0.05] = 0.0
+        v[rng.random(n) < 0.05] = 0.0
+        if n > 2000:
+            m[256:512] = 0.0
+            v[512:768] = 0.0
+            m[800], v[800] = 1e3, 1.0
+            v[1100] = 1e-38
+        state = dense.adamw_state(p, bits=8)
+        for x, codes, scales, signed in ((m, state.m, state.m_scales, True), (v, state.v, state.v_scales, False)):
+            c, s = ref.codes8(x.astype(np.float32), signed, rng.integers(0, 65536, n))
+            codes.copy_(torch.from_numpy(c).reshape(codes.shape))
+            scales.copy_(torch.from_numpy(s))
+        out.append(state)
+    return out
+
+
+def next_states(state, g, number, seed, step, betas, grad_scale=1.0):
+    """The codes and scales after a step, by its fp32 operations in their order."""
+    f = np.float32
+    m = ref.values8(state.m.cpu().numpy().reshape(-1), state.m_scales.cpu().numpy(), True).astype(f)
+    v = ref.values8(state.v.cpu().numpy().reshape(-1), state.v_scales.cpu().numpy(), False).astype(f)
+    g = wide(g).reshape(-1).numpy().astype(f) * f(grad_scale)
+    with np.errstate(invalid="ignore", over="ignore"):
+        m = m * f(betas[0]) + g * f(1 - betas[0])
+        v = v * f(betas[1]) + (g * g) * f(1 - betas[1])
+    r = ref.random_bits(m.size, number, seed, step).astype(np.int64)
+    return ref.codes8(m, True, r & 0xFFFF), ref.codes8(v, False, r >> 16), m, v
+
+
+@pytest.mark.parametrize("dtype,grad", [(F32, F32), (BF16, BF16), (F16, F32)])
+@pytest.mark.parametrize("sizes,offset", [([1], 0), ([255, 256, 257, 0, 8], 0), ([9] * 60, 0), ([70001, 300], 1)])
+def test_eight_bit_states(dev, dtype, grad, sizes, offset):
+    params, grads = tensors(5, sizes, dtype, grad, dev, offset=offset)
+    states = eight(6, params, dev)
+    for step in (1, 2, 3):
+        before, old = [p.clone() for p in params], copies(states)
+        dense.adamw(params, grads, states, step, seed=12345, **HOW)
+        for j, (p, g, s, b, o) in enumerate(zip(params, grads, states, before, old)):
+            (mc, ms), (vc, vs), m, v = next_states(o, g, j, 12345, step, HOW["betas"])
+            assert np.array_equal(s.m_scales.cpu().numpy(), ms) and np.array_equal(s.v_scales.cpu().numpy(), vs)
+            assert np.array_equal(s.m.cpu().numpy().reshape(-1), mc) and np.array_equal(s.v.cpu().numpy().reshape(-1), vc)
+            om = torch.from_numpy(ref.values8(o.m.cpu().numpy().reshape(-1), o.m_scales.cpu().numpy(), True))
+            ov = torch.from_numpy(ref.values8(o.v.cpu().numpy().reshape(-1), o.v_scales.cpu().numpy(), False))
+            (want, off), *_ = ref.adamw(b, g, om, ov, step, **HOW)
+            check(p, want, off + ref.E * (want.abs() + off), "p")
+    got = dense.adamw_values(states)
+    for s, m, v in zip(states, *got):
+        for x, codes, scales, signed in ((m, s.m, s.m_scales, True), (v, s.v, s.v_scales, False)):
+            want = ref.values8(codes.cpu().numpy().reshape(-1), scales.cpu().numpy(), signed)
+            assert np.array_equal(wide(x).numpy().reshape(-1), want)
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan, 3.4e38])
+def test_gradient_that_is_no_number(dev, bad):
+    # its element in 32 bits; the whole block's states in 8 (3.4e38: its square is infinite)
+    for bits in (32, 8):
+        params, grads = tensors(7, [1000], F32, F32, dev)
+        states = [dense.adamw_state(params[0], bits)]
+        grads[0][300] = bad
+        dense.adamw(params, grads, states, 1, **HOW)
+        spoiled = torch.zeros(1000, dtype=torch.bool)
+        spoiled[300] = True
+        if math.isfinite(bad):
+            assert params[0].isfinite().all()  # m / infinity moves nothing
+        else:
+            assert torch.equal(~params[0].isfinite().cpu(), spoiled)
+        if bits == 8:
+            v = dense.adamw_values(states)[1][0].cpu()
+            assert v[256:512].isnan().all() and v[:256].isfinite().all() and v[512:].isfinite().all()
+        else:
+            assert torch.equal(~states[0].v.isfinite().cpu(), spoiled)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("value", [math.inf, math.nan, -math.inf, 1.0])
+def test_norm_that_is_no_number_leaves_the_step_out(dev, bits, value):
+    params, grads = tensors(8, [3000, 10], BF16, BF16, dev)
+    states = [dense.adamw_state(p, bits, master=True) for p in params]
+    before, old = [p.clone() for p in params], copies(states)
+    dense.adamw(params, grads, states, 1, norm=torch.full((1,), value, device=dev), **HOW)
+    same = all(torch.equal(a, b) for a, b in zip(params, before)) and all(
+        torch.equal(x, y) for s, o in zip(states, old) for x, y in zip(s, o) if x is not None)
+    assert same == (value != 1.0)
+
+
+def test_values_keep_their_mean(dev):
+    # one state, held by every element but the block's largest: the mean over 2^18 draws is off from it by less than
+    # 6 standard deviations of a rounding, half a code's distance at most each
+    n = 1 << 18
+    p, g = torch.zeros(n, device=dev), torch.zeros(n, device=dev)
+    g[::256] = 1.0
+    for value in (0.013, 0.77, 3e-4):
+        state = dense.adamw_state(p, bits=8)
+        g.fill_(value)
+        g[::256] = 1.0
+        dense.adamw([p], [g], [state], 1, lr=0.0, betas=(0.0, 0.0), seed=99)
+        (m,), (v,) = dense.adamw_values([state])
+        rest = torch.ones(n, dtype=torch.bool, device=dev)
+        rest[::256] = False
+        for x, want in ((m, float(np.float32(value))), (v, float(np.float32(value) * np.float32(value)))):
+            x = wide(x[rest])
+            assert (x - want).abs().max() <= want / 8 + 2.0 ** -17
+            distance = x.max() - x.min()
+            assert abs(float(x.mean()) - want) <= 6 * 0.5 * float(distance) / math.sqrt(x.numel()) + want * 2.0 ** -16
+
+
+def test_small_squares_stay_above_zero(dev):
+    g = torch.full((256,), 1e-7, device=dev)
+    g[0] = 1.0
+    p, state = torch.zeros(256, device=dev), dense.adamw_state(torch.zeros(256, device=dev), bits=8)
+    dense.adamw([p], [g], [state], 1, **HOW)
+    assert (dense.adamw_values([state])[1][0] > 0).all()
+
+
+def test_a_step_moves_along_the_mean_gradient(dev):
+    # 8-bit states against 32-bit ones over steps of a constant gradient: m and v keep their means
+    n = 4096
+    g = torch.randn(n, generator=torch.Generator().manual_seed(3)).to(dev) * 1e-3
+    a, b = torch.zeros(n, device=dev), torch.zeros(n, device=dev)
+    s32, s8 = dense.adamw_state(a), dense.adamw_state(b, bits=8)
+    for t in range(1, 41):
+        dense.adamw([a], [g], [s32], t, **HOW)
+        dense.adamw([b], [g], [s8], t, seed=t, **HOW)
+    # each of m's 40 roundings, of at most an eighth, weighs less than the next: a step is off by an eighth at most
+    # on either state's account, and 40 of them by far less than half of their length together
+    assert ((a - b).abs().sum() <= 0.5 * a.abs().sum()) and (torch.sign(a) == torch.sign(b)).float().mean() > 0.99
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_captured_step_goes_on(dev, bits):
+    params, grads = tensors(9, [5000, 33], BF16, BF16, dev)
+    states = [dense.adamw_state(p, bits, master=True) for p in params]
+    eager_p, eager_s = [p.clone() for p in params], copies(states)
+    step, lr = torch.ones(1, dtype=torch.int32, device=dev), torch.full((1,), 1e-3, device=dev)
+    how = {**HOW, "lr": lr}
+    spare = [p.clone() for p in params], copies(states)
+    dense.adamw(spare[0], grads, spare[1], step, seed=5, **how)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dense.adamw(params, grads, states, step, seed=5, **how)
+    for t in (1, 2, 3, 4):
+        step.fill_(t)
+        lr.fill_(1e-3 / t)
+        for g in grads:
+            g.copy_(torch.randn(g.shape, generator=torch.Generator().manual_seed(t)).to(BF16))
+        torch.cuda.synchronize()
+        graph.replay()
+        dense.adamw(eager_p, grads, eager_s, t, seed=5, **{**HOW, "lr": float(lr)})
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(params, eager_p))
+        assert all(torch.equal(x, y) for s, o in zip(states, eager_s) for x, y in zip(s, o) if x is not None)
+
+
+def test_same_bits_on_repeats_and_nothing_past_the_end(dev):
+    params, grads = tensors(10, [777, 4099], F32, BF16, dev, offset=3)
+    for bits in (32, 8):
+        runs = []
+        for _ in range(2):
+            p = [torch.full((q.numel() + 300,), 5.0, device=dev)[:q.numel()].copy_(q) for q in params]
+            states = [dense.adamw_state(q, bits) for q in p]
+            for t in (1, 2):
+                dense.adamw(p, grads, states, t, seed=t, **HOW)
+            runs.append((p, states))
+            for q in p:
+                tail = torch.empty(0, device=dev).set_(q.untyped_storage())[q.numel():]
+                assert (tail == 5.0).all()
+        for a, b in zip(runs[0][0], runs[1][0]):
+            assert torch.equal(a, b)
+        for s, o in zip(runs[0][1], runs[1][1]):
+            assert all(torch.equal(x, y) for x, y in zip(s, o) if x is not None)
+
+
+def test_nothing_to_do(dev):
+    dense.adamw([], [], [], 1)
+    assert dense.adamw_values([]) == ([], [])
+    p = torch.empty(0, device=dev)
+    dense.adamw([p], [p], [dense.adamw_state(p, 8)], 1)

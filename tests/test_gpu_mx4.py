@@ -1,0 +1,227 @@
+"""The 4-bit operators against 64 bits, on the GPU."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import layer_ref as ref
+import paper_2608_24067_amd.dense as dense
+from dense_ref import act, check, sums, wide, LIP
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+def spread(seed, N, K, dtype):
+    """Values over many sizes, with ties, zeros, and blocks of one value, of none, of subnormals and of the largest."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(N, K, generator=g) * torch.exp(2 * torch.randn(N, 1, generator=g))
+    tie = torch.rand(N, K, generator=g) < 0.2
+    x = torch.where(tie, torch.round(x * 4) / 4, x)
+    x[torch.rand(N, K, generator=g) < 0.05] = 0.0
+    x[torch.rand(N, K, generator=g) < 0.02] *= -0.0
+    if N > 4:
+        x[1, :32] = 0.0
+        x[2, :32] = 2.0 ** -24 if dtype == F16 else 1e-40
+        x[3, :32] = torch.finfo(dtype).max
+        x[4] = 1.0
+    return x.to(dtype)
+
+
+def codes_equal(q, x):
+    codes, scales = ref.codes4(wide(x))
+    assert np.array_equal(q.scales.cpu().numpy(), scales)
+    assert np.array_equal(q.codes.cpu().numpy(), codes)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("N,K,extra", [(1, 1, 0), (5, 31, 0), (7, 32, 0), (33, 33, 1), (64, 100, 4), (130, 1003, 0),
+                                       (17, 2048, 8), (300, 64, 3)])
+def test_quantise_and_values(dev, dtype, N, K, extra):
+    x = spread(N + K, N, K, dtype)
+    rows = torch.full((N, K + extra), float("nan"), dtype=dtype, device=dev)[:, :K].copy_(x)
+    q = dense.mx4_quantise(rows)
+    codes_equal(q, x)
+    columns = torch.full((K, N + extra), float("nan"), dtype=dtype, device=dev)[:, :N].copy_(x.t())
+    c = dense.mx4_quantise(columns, columns=True)
+    assert torch.equal(c.codes, q.codes) and torch.equal(c.scales, q.scales)
+    want = ref.values4(q.codes, q.scales, K)
+    for t in (F32, BF16, F16):
+        to = torch.full((N, K + extra), 7.0, dtype=t, device=dev)
+        dense.mx4_values(q, out=to[:, :K])
+        assert torch.equal(to[:, :K].cpu(), want.to(t)) and (to[:, K:] == 7.0).all()
+        to = torch.full((K, N + extra), 7.0, dtype=t, device=dev)
+        dense.mx4_values(q, columns=True, out=to[:, :N])
+        assert torch.equal(to[:, :N].cpu(), want.t().to(t)) and (to[:, N:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_blocks_with_no_number(dev, dtype, bad):
+    x = spread(3, 6, 100, dtype)
+    x[2, 40] = bad
+    x[5, 99] = bad
+    for columns in (False, True):
+        q = dense.mx4_quantise((x.t().contiguous() if columns else x).to(dev), columns=columns)
+        v = dense.mx4_values(q, dtype=F32).cpu()
+        spoiled = torch.zeros(6, 100, dtype=torch.bool)
+        spoiled[2, 32:64] = spoiled[5, 96:] = True
+        assert torch.equal(v.isnan(), spoiled)
+        y = dense.mx4_quantise(torch.where(spoiled, torch.zeros_like(x), x).to(dev))
+        keep = ~torch.tensor([[False] * 4, [False] * 4, [False, True, False, False], [False] * 4, [False] * 4,
+                              [False] * 3 + [True]])
+        assert torch.equal(q.scales.cpu()[keep], y.scales.cpu()[keep])
+
+
+def matrix(seed, K, M, dev):
+    g = torch.Generator().manual_seed(seed)
+    return dense.mx4_quantise((torch.randn(K, M, generator=g) * torch.exp(torch.randn(1, M, generator=g)) * K ** -0.5).to(dev),
+                              columns=True)
+
+
+def product(dev, dtype, N, K, M, packed, a="none", res=False, bias=None, out=None, extra=0):
+    g = torch.Generator().manual_seed(N + 7 * K + M)
+    x = torch.full((N, K + extra), float("nan"), dtype=dtype, device=dev)[:, :K].copy_(torch.randn(N, K, generator=g))
+    W = matrix(K + M, K, M, dev)
+    rows = dense.mx4_quantise(x) if packed else x
+    xv = ref.values4(rows.codes, rows.scales, K) if packed else wide(x)
+    wv = ref.values4(W.codes, W.scales, K)
+    b = torch.randn(M, generator=g).to(bias).to(dev) if bias is not None else None
+    r = torch.full((N, M + extra), float("nan"), dtype=dtype, device=dev)[:, :M].copy_(torch.randn(N, M, generator=g)) if res else None
+    z = xv @ wv.t() + (wide(b) if b is not None else 0)
+    size = xv.abs() @ wv.abs().t() + (wide(b).abs() if b is not None else 0)
+    # fp16 rows meet the matrix as two values each: twice the terms
+    off = LIP * sums(2 * K + 4, size) + (2.0 ** -20 * z.abs().clamp_min(1) if a != "none" else 0)
+    want = act(a, z)
+    if r is not None:
+        want, off = want + wide(r), off + 2.0 ** -24 * (want.abs() + wide(r).abs())
+    to = torch.full((N, M + extra), 7.0, dtype=out or dtype, device=dev)
+    y = dense.mx4_linear(rows, W, b, residual=r, act=a, out=to[:, :M], dtype=dtype if packed else None)
+    check(y, want, off, "y")
+    assert (to[:, M:] == 7.0).all()
+    return y
+
+
+SIZES = [(1, 1, 1), (1, 64, 64), (1, 1024, 4096), (2, 33, 17), (15, 100, 130), (16, 256, 257), (17, 1003, 70), (33, 2048, 300),
+         (64, 96, 129), (65, 4096, 40), (100, 1000, 1000), (129, 160, 256), (257, 513, 515), (500, 257, 130), (1000, 640, 384)]
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("N,K,M", SIZES)
+def test_product(dev, dtype, packed, N, K, M):
+    product(dev, dtype, N, K, M, packed, bias=dtype, out=F32)
+    product(dev, dtype, N, K, M, packed, bias=F32)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("a", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("dtype,out", [(F16, None), (BF16, None), (BF16, F32)])
+@pytest.mark.parametrize("N", [3, 40, 300])
+def test_epilogue_and_strides(dev, dtype, out, packed, a, N):
+    product(dev, dtype, N, 200, 203, packed, a=a, res=True, bias=F32, out=out, extra=3)
+    product(dev, dtype, N, 256, 256, packed, a=a, res=True, out=out, extra=8)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("N", [1, 20, 200])
+def test_no_number_stays_in_its_row_and_column(dev, packed, N):
+    K, M = 300, 150
+    g = torch.Generator().manual_seed(9)
+    x, w = torch.randn(N, K, generator=g).to(BF16).to(dev), torch.randn(K, M, generator=g).to(dev)
+    clean = dense.mx4_linear(dense.mx4_quantise(x) if packed else x, dense.mx4_quantise(w, columns=True))
+    x[N - 1, 299] = math.inf
+    w[40, 5] = math.nan
+    W = dense.mx4_quantise(w, columns=True)
+    y = dense.mx4_linear(dense.mx4_quantise(x) if packed else x, W)
+    spoiled = torch.zeros(N, M, dtype=torch.bool)
+    spoiled[N - 1] = spoiled[:, 5] = True
+    assert not y.isfinite().cpu()[spoiled].any()
+    assert y[:, 5].isnan().all()
+    assert torch.equal(y.cpu()[~spoiled], clean.cpu()[~spoiled])
+
+
+@pytest.mark.parametrize("N", [2, 70, 300])
+def test_fp16_rows_of_all_sizes(dev, N):
+    # subnormal and largest fp16 values, and a matrix whose scales fp16 does not hold
+    K, M = 128, 40
+    g = torch.Generator().manual_seed(21)
+    x = (torch.randn(N, K, generator=g) * torch.exp2(torch.randint(-24, 13, (N, K), generator=g).float())).clamp(-65504, 65504).half()
+    w = torch.randn(K, M, generator=g) * torch.exp2(torch.randint(-60, 20, (K, M), generator=g).float())
+    W = dense.mx4_quantise(w.to(dev), columns=True)
+    wv = ref.values4(W.codes, W.scales, K)
+    y = dense.mx4_linear(x.to(dev), W, out_dtype=F32)
+    check(y, wide(x) @ wv.t(), sums(2 * K, wide(x).abs() @ wv.abs().t()), "y")
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_scales_at_the_ends(dev, packed):
+    # products of the smallest and of large blocks; sums stay within fp32
+    K, M = 64, 33
+    x = torch.full((3, K), 2.0 ** -100, device=dev)
+    x[1] = 2.0 ** 100
+    x[2, 32:] = 0.0
+    w = torch.full((K, M), 2.0 ** -20, device=dev)
+    w[:, 1] = 2.0 ** 20
+    w[:, 2] = 2.0 ** -126
+    W = dense.mx4_quantise(w, columns=True)
+    rows = dense.mx4_quantise(x) if packed else x.to(BF16)
+    y = dense.mx4_linear(rows, W, out_dtype=F32, dtype=BF16 if packed else None)
+    want = wide(x) @ wide(w)
+    assert ((wide(y) - want).abs() <= 2.0 ** -149 * 2 + 2.0 ** -22 * want.abs()).all()
+
+
+def test_same_bits_on_repeats_and_on_another_stream(dev):
+    x = torch.randn(300, 700, generator=torch.Generator().manual_seed(1)).to(BF16).to(dev)
+    W = matrix(4, 700, 500, dev)
+    for n in (1, 20, 300):
+        for packed in (False, True):
+            rows = dense.mx4_quantise(x[:n]) if packed else x[:n]
+            first = dense.mx4_linear(rows, W)
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                again = dense.mx4_linear(rows, W)
+            torch.cuda.current_stream().wait_stream(side)
+            assert torch.equal(first, again)
+
+
+@pytest.mark.parametrize("N", [1, 40, 400])
+def test_captured_and_replayed(dev, N):
+    W = matrix(5, 512, 768, dev)
+    x = torch.zeros(N, 512, dtype=BF16, device=dev)
+    codes, scales = torch.empty(N, 256, dtype=torch.uint8, device=dev), torch.empty(N, 16, dtype=torch.uint8, device=dev)
+    y, y4 = torch.empty(N, 768, dtype=BF16, device=dev), torch.empty(N, 768, dtype=BF16, device=dev)
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device=dev)
+
+    def step(a, b):
+        dense.mx4_linear(x, W, act="silu", out=a, workspace=ws)
+        dense.mx4_linear(dense.mx4_quantise(x, out=(codes, scales)), W, residual=a, out=b, workspace=ws)
+
+    step(y, y4)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(y, y4)
+    for k in range(3):
+        x.copy_(torch.randn(N, 512, generator=torch.Generator().manual_seed(k)).to(BF16))
+        a, b = torch.empty_like(y), torch.empty_like(y)
+        step(a, b)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a, y) and torch.equal(b, y4)
+
+
+def test_residual_in_place_and_no_rows(dev):
+    W = matrix(6, 100, 90, dev)
+    x = torch.randn(50, 100, generator=torch.Generator().manual_seed(2)).to(BF16).to(dev)
+    r = torch.randn(50, 90, generator=torch.Generator().manual_seed(3)).to(BF16).to(dev)
+    want = dense.mx4_linear(x, W, residual=r, act="gelu")
+    dense.mx4_linear(x, W, residual=r, act="gelu", out=r)
+    assert torch.equal(r, want)
+    assert dense.mx4_linear(x[:0], W).shape == (0, 90)
+    q = dense.mx4_quantise(x[:0])
+    assert q.codes.shape == (0, 64) and dense.mx4_values(q).shape == (0, 100)
+    assert dense.mx4_linear(q, W).shape == (0, 90)
