@@ -19,6 +19,7 @@ SOURCES = [os.path.join(CSRC, "som_sweep.hip"), os.path.join(CSRC, "som_rows.hip
            os.path.join(CSRC, "som_dense_api.cpp"), os.path.join(CSRC, "som_norm_rows.hip"),
            os.path.join(CSRC, "som_norm_grad.hip"), os.path.join(CSRC, "som_adamw.hip"),
            os.path.join(CSRC, "som_mx4.hip"), os.path.join(CSRC, "som_mx4_few.hip"),
+           os.path.join(CSRC, "som_mx4_half.hip"), os.path.join(CSRC, "som_mx4_packed.hip"),
            os.path.join(CSRC, "som_layer_api.cpp")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -131,6 +131,7 @@ struct FourProduct {
     int64_t ldx;              // elements; not read for codes
     const uint8_t *x_scales;  // null: x is of the type
     const uint8_t *w, *w_scales;
+    int64_t x_pitch, w_pitch;  // bytes of a row's scales
     const void *bias;
     bool bias_f32;
     int32_t act;
@@ -143,5 +144,16 @@ struct FourProduct {
 };
 
 hipError_t launch_mx4_few(bool bf16, const FourProduct &p, hipStream_t st);
+
+// The same for many rows, by tiles of 128 x 128 or 256 x 256. Rows in 16 bits must be whole 16-byte
+// chunks, rows of scales whole 16-byte pieces (four_pitch).
+enum FourTile { kFourMid, kFourLarge };
+hipError_t launch_mx4_half(bool bf16, FourTile t, const FourProduct &p, hipStream_t st);
+hipError_t launch_mx4_packed(bool bf16, FourTile t, const FourProduct &p, hipStream_t st);
+
+__host__ __device__ inline int64_t four_pitch(int64_t K) { return (four_blocks(K) + 15) / 16 * 16; }
+// Rows' scales to rows of four_pitch bytes, and rows of K values to rows of whole blocks, zeros behind them.
+hipError_t launch_pad_scales(const uint8_t *scales, int64_t rows, int64_t K, uint8_t *to, hipStream_t st);
+hipError_t launch_pad_rows(const void *x, int64_t ldx, int64_t rows, int64_t K, void *to, hipStream_t st);
 
 }  // namespace som

@@ -106,6 +106,45 @@ const char *product_sizes(int64_t N, int64_t K, int64_t M)
     return rows_ok(N) && dim_ok(K) && dim_ok(M) ? nullptr : "need 0 <= N, 1 <= K, M, all below 2^30";
 }
 
+// ---------------------------------------------------------------- products with a 4-bit matrix
+
+// How a product is computed, and what of its workspace holds what.
+struct FourLayout {
+    bool few;
+    som::FourTile tile;
+    int64_t strip;            // rows in 16 bits that are copied and multiplied at a time
+    size_t x, xs, ws, total;  // their copy, and padded rows of scales
+};
+
+// Rows up to which the kernel for few rows reads the matrix straight into registers.
+constexpr int64_t kFourFew = 64;
+
+// Bytes of the copied rows at most: strips of them stay in the cache.
+constexpr int64_t kFourStrip = (int64_t)32 << 20;
+
+FourLayout four_layout(int64_t N, int64_t K, int64_t M, bool packed)
+{
+    FourLayout L{};
+    const int64_t row = som::four_blocks(K) * 64, most = kFourStrip / row / 256 * 256;
+    L.strip = packed || N < most ? N : most;
+    L.few = N <= kFourFew || L.strip == 0;
+    if (L.few) return L;
+    const int64_t tiles = (N + 255) / 256 * ((M + 255) / 256);
+    L.tile = tiles >= 128 ? som::kFourLarge : som::kFourMid;
+    const bool ragged = som::four_blocks(K) % 16 != 0;
+    size_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t p = at;
+        at += align256((size_t)bytes);
+        return p;
+    };
+    L.ws = take(ragged ? M * som::four_pitch(K) : 0);
+    L.xs = take(ragged && packed ? N * som::four_pitch(K) : 0);
+    L.x = take(packed ? 0 : L.strip * row);
+    L.total = at;
+    return L;
+}
+
 }  // namespace
 
 extern "C" {
@@ -252,8 +291,8 @@ som_status som_mx4_values(int32_t type, const uint8_t *codes, const uint8_t *sca
 
 size_t som_mx4_linear_workspace_bytes(int64_t N, int64_t K, int64_t M, int32_t packed)
 {
-    (void)N, (void)K, (void)M, (void)packed;
-    return 0;
+    if (product_sizes(N, K, M) || (packed != 0 && packed != 1)) return 0;
+    return four_layout(N, K, M, packed == 1).total;
 }
 
 som_status som_mx4_linear(int32_t type, const void *X, int64_t ldx, const uint8_t *x_scales, const uint8_t *w_codes,
@@ -280,7 +319,35 @@ som_status som_mx4_linear(int32_t type, const void *X, int64_t ldx, const uint8_
     p.x = X, p.ldx = ldx, p.x_scales = x_scales, p.w = w_codes, p.w_scales = w_scales;
     p.bias = bias, p.bias_f32 = bias_type == SOM_F32, p.act = act, p.res = residual, p.ldr = ldr;
     p.y = Y, p.ldy = ldy, p.y_f32 = y_type == SOM_F32, p.N = N, p.K = K, p.M = M;
-    return done(som::launch_mx4_few(type == SOM_BF16, p, static_cast<hipStream_t>(stream)), who);
+    const bool bf16 = type == SOM_BF16, packed = x_scales != nullptr;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const FourLayout L = four_layout(N, K, M, packed);
+    const bool ragged = som::four_blocks(K) % 16 != 0;
+    if (L.few || (!ragged && (off(w_scales, 16) || off(x_scales, 16)))) return done(som::launch_mx4_few(bf16, p, s), who);
+    char *b = static_cast<char *>(workspace);
+    p.x_pitch = p.w_pitch = som::four_pitch(K);
+    if (ragged) {
+        uint8_t *ws = reinterpret_cast<uint8_t *>(b + L.ws), *xs = reinterpret_cast<uint8_t *>(b + L.xs);
+        hipError_t e = som::launch_pad_scales(w_scales, M, K, ws, s);
+        if (e == hipSuccess && packed) e = som::launch_pad_scales(x_scales, N, K, xs, s);
+        if (e != hipSuccess) return done(e, who);
+        p.w_scales = ws;
+        if (packed) p.x_scales = xs;
+    }
+    if (packed) return done(som::launch_mx4_packed(bf16, L.tile, p, s), who);
+    if (!off(X, 16) && ldx % 8 == 0 && K % 8 == 0) return done(som::launch_mx4_half(bf16, L.tile, p, s), who);
+    const int64_t width = som::four_blocks(K) * 32;
+    for (int64_t n = 0; n < N; n += L.strip) {
+        som::FourProduct q = p;
+        q.N = N - n < L.strip ? N - n : L.strip;
+        q.x = b + L.x, q.ldx = width, q.K = width;
+        q.res = residual ? static_cast<const char *>(residual) + n * ldr * 2 : nullptr;
+        q.y = static_cast<char *>(Y) + n * ldy * size_of(y_type);
+        hipError_t e = som::launch_pad_rows(static_cast<const char *>(X) + n * ldx * 2, ldx, q.N, K, b + L.x, s);
+        if (e == hipSuccess) e = som::launch_mx4_half(bf16, L.tile, q, s);
+        if (e != hipSuccess) return done(e, who);
+    }
+    return ok();
 }
 
 }  // extern "C"

@@ -25,8 +25,8 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 8, kUnit = 128;
 
-// 2^(s - 127) for the conversion; NaN for 255.
-__device__ inline float scale_value(uint32_t s) { return __uint_as_float(s == 255 ? 0x7FC00000u : s ? s << 23 : 0x00400000u); }
+// 2^(s - 127), a subnormal for 0 and NaN for 255.
+__device__ inline float scale_value(uint32_t s) { return __uint_as_float(max(s << 23, 0x00400000u) | (s + 1) >> 8 << 22); }
 
 // Eight codes as bf16 values.
 __device__ inline bf16x8 widen(uint32_t c, float scale)
