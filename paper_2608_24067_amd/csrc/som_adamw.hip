@@ -58,12 +58,17 @@ struct Rates : AdamwRates {
             set(lr, a.beta1, a.beta2, a.weight_decay, a.step_at ? (uint32_t)max(*a.step_at, 1) : step);
         }
     }
-    __device__ void apply(float &p, float g, float &m, float &v) const
+    // by1, by2: b1 and b2, or what stands for them (an 8-bit block's). The products of m and v are
+    // rounded one by one, as documented; the parameter's part takes the hardware's root and reciprocal,
+    // good to a unit in the last place, for a third of an 8-bit step's instructions. The hardware takes a
+    // subnormal root's argument as zero, so it is kept at the smallest normal value.
+    __device__ void apply(float &p, float g, float &m, float &v, float by1, float by2) const
     {
         g *= grad;
-        m = m * b1 + g * c1;
-        v = v * b2 + g * g * c2;
-        p = p * keep - rate * (m / (sqrtf(v) * root + eps));
+        m = m * by1 + g * c1;
+        v = v * by2 + g * g * c2;
+        const float den = fmaf(__builtin_amdgcn_sqrtf(v < 0x1p-126f ? 0x1p-126f : v), root, eps);
+        p = fmaf(-rate, m * __builtin_amdgcn_rcpf(den), p * keep);
     }
 };
 
@@ -81,43 +86,33 @@ template <int V> __device__ inline void store_any(void *p, int type, int64_t at,
     else store<V>(static_cast<__bf16 *>(p) + at, n, v);
 }
 
-__device__ inline float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 ... 127
-
-// x 2^e for -254 <= e <= 254 and x not near the ends of fp32's range on the way.
-__device__ inline float times_power(float x, int e)
+// What codes stand for under a block's byte s: a code's bits (its sign at the front) are those of an
+// fp32 value whose exponent is 127 - s + 112 (m) or 96 (v) too small; codes below the first exponent
+// are subnormal there. `word` holds the code in its byte B.
+template <bool SIGNED, int B> __device__ inline float decode(uint32_t word, int s)
 {
-    const int half = e >> 1;
-    return x * power_of_two(half) * power_of_two(e - half);
+    const uint32_t bits = SIGNED ? (uint32_t)((int32_t)(word << (24 - 8 * B)) >> 4) & 0x87F00000u : (word >> (8 * B) & 255) << 20;
+    return ldexpf(__uint_as_float(bits), s - (SIGNED ? 15 : 31));
 }
 
-// What a code stands for, before the block's power: its bits are those of an fp32 value whose exponent
-// is 112 (m) or 96 (v) too small; codes below the first exponent are subnormal there.
-template <bool SIGNED> __device__ inline float code_value(uint32_t c)
-{
-    const float size = __uint_as_float((SIGNED ? c & 127 : c) << 20) * (SIGNED ? 0x1p112f : 0x1p96f);
-    return SIGNED && c & 128 ? -size : size;
-}
+// What a block's old values are multiplied by: nothing where it is held as zeros, NaN where it holds none.
+__device__ inline float block_factor(uint32_t s, float b) { return s == 255 ? __builtin_nanf("") : s ? b : 0.0f; }
 
 // The exponent e of a block's power from the bits of its largest magnitude, as its byte.
 __device__ inline uint32_t block_scale(uint32_t bits)
 {
-    const uint32_t f = (bits + 0xFFFFF) >> 23;  // a NaN may carry past 255
+    const uint32_t f = ((bits & 0x7FFFFFFF) + 0xFFFFF) >> 23;  // a NaN may carry past 255
     return f < 27 ? 0 : min(f, 255u);
 }
 
-// The code of x under the block's byte, by 16 random bits. A block of NaN gets codes of no meaning.
-template <bool SIGNED> __device__ inline uint32_t encode(float x, uint32_t scale, uint32_t random)
+// The code of x by 16 random bits, `random` in their place above the four that are dropped; `some`: the
+// block's byte is not 0. A block of NaN gets codes of no meaning.
+template <bool SIGNED> __device__ inline uint32_t encode(float x, int s, bool some, uint32_t random)
 {
-    const float y = times_power(fabsf(x), 127 - (int)scale) * (SIGNED ? 0x1p-112f : 0x1p-96f);
-    uint32_t c = (__float_as_uint(y) + (random << 4)) >> 20;
-    if (SIGNED) c = min(c, 127u) | (x < 0.0f ? 128u : 0u);
-    else c = x > 0.0f ? max(min(c, 255u), 1u) : 0u;
-    return scale ? c : 0u;
-}
-
-__device__ inline float scaled_value(float v, uint32_t scale)
-{
-    return scale == 255 ? __builtin_nanf("") : scale ? times_power(v, (int)scale - 127) : 0.0f;
+    const uint32_t c = (__float_as_uint(ldexpf(fabsf(x), (SIGNED ? 15 : 31) - s)) + random) >> 20;
+    if (SIGNED) return min(c, some ? 127u : 0u) | (x < 0.0f && some ? 128u : 0u);
+    const uint32_t least = x > 0.0f && some ? 1u : 0u;  // and 0 for 0, whose bits the random ones do not carry
+    return min(max(c, least), some ? 255u : 0u);
 }
 
 // The largest over the 32 lanes of a block's half wave.
@@ -130,34 +125,43 @@ __device__ inline uint32_t half_wave_max(uint32_t v)
     return max(v, (uint32_t)__shfl_xor((int)v, 16));
 }
 
-// n codes (up to 8) as bytes.
-__device__ inline void load8(const uint8_t *p, int n, uint32_t *c)
+// n codes (up to V, 4 or 8) as the bytes of words.
+template <int V> __device__ inline void load_codes(const uint8_t *p, int n, uint32_t *w)
 {
-    if (n >= 8) {
-        typedef VecOf<uint32_t, 2>::type two;
-        typedef two any __attribute__((aligned(1)));
-        const two t = *reinterpret_cast<const any *>(p);
+    typedef typename VecOf<uint32_t, V / 4>::type words;
+    typedef words any __attribute__((aligned(1)));
+    if (n >= V) {
+        const words t = *reinterpret_cast<const any *>(p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = t[i / 4] >> (8 * (i % 4)) & 255;
+        for (int i = 0; i < V / 4; ++i) w[i] = t[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = i < n ? p[i] : 0;
+        for (int i = 0; i < V / 4; ++i) w[i] = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) w[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
     }
 }
-__device__ inline void store8(uint8_t *p, int n, const uint32_t *c)
+template <int V> __device__ inline void store_codes(uint8_t *p, int n, const uint32_t *w)
 {
-    if (n >= 8) {
-        typedef VecOf<uint32_t, 2>::type two;
-        typedef two any __attribute__((aligned(1)));
-        two t;
+    typedef typename VecOf<uint32_t, V / 4>::type words;
+    typedef words any __attribute__((aligned(1)));
+    if (n >= V) {
+        words t;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) t[h] = c[4 * h] | c[4 * h + 1] << 8 | c[4 * h + 2] << 16 | c[4 * h + 3] << 24;
+        for (int i = 0; i < V / 4; ++i) t[i] = w[i];
         *reinterpret_cast<any *>(p) = t;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) p[i] = (uint8_t)c[i];
+        for (int i = 0; i < V; ++i)
+            if (i < n) p[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
     }
+}
+
+template <bool SIGNED> __device__ inline void decode4(uint32_t word, int s, float *v)
+{
+    v[0] = decode<SIGNED, 0>(word, s), v[1] = decode<SIGNED, 1>(word, s);
+    v[2] = decode<SIGNED, 2>(word, s), v[3] = decode<SIGNED, 3>(word, s);
 }
 
 template <bool BITS8> __global__ __launch_bounds__(kThreads) void k_adamw(const AdamwTable t, const AdamwArgs a)
@@ -182,7 +186,7 @@ template <bool BITS8> __global__ __launch_bounds__(kThreads) void k_adamw(const 
             load<V>(ms + at, n, m);
             load<V>(vs + at, n, v);
 #pragma unroll
-            for (int q = 0; q < V; ++q) r.apply(p[q], g[q], m[q], v[q]);
+            for (int q = 0; q < V; ++q) r.apply(p[q], g[q], m[q], v[q], r.b1, r.b2);
             store<V>(ms + at, n, m);
             store<V>(vs + at, n, v);
             if (master) store<V>(master + at, n, p);
@@ -198,32 +202,42 @@ template <bool BITS8> __global__ __launch_bounds__(kThreads) void k_adamw(const 
             if (block * kStateBlock >= to) break;
             const int n = (int)max((int64_t)0, min((int64_t)V, to - at));
             float p[V], g[V], m[V], v[V];
-            uint32_t cm[V], cv[V];
+            uint32_t cm[V / 4], cv[V / 4];
             load_any<V>(read, read_type, at, n, p);
             load_any<V>(t.grad[i], grad_type, at, n, g);
-            load8(mc + at, n, cm);
-            load8(vc + at, n, cv);
+            load_codes<V>(mc + at, n, cm);
+            load_codes<V>(vc + at, n, cv);
             const uint32_t old_m = t.m_scales[i][block], old_v = t.v_scales[i][block];
+            const float by1 = block_factor(old_m, r.b1), by2 = block_factor(old_v, r.b2);
             uint32_t top_m = 0, top_v = 0;
 #pragma unroll
-            for (int q = 0; q < V; ++q) {
-                m[q] = scaled_value(code_value<true>(cm[q]), old_m);
-                v[q] = scaled_value(code_value<false>(cv[q]), old_v);
-                if (q >= n) m[q] = v[q] = 0.0f;
-                r.apply(p[q], g[q], m[q], v[q]);
-                top_m = max(top_m, __float_as_uint(m[q]) & 0x7FFFFFFF);
-                top_v = max(top_v, __float_as_uint(v[q]) & 0x7FFFFFFF);
-            }
-            const uint32_t new_m = block_scale(half_wave_max(top_m)), new_v = block_scale(half_wave_max(top_v));
+            for (int h = 0; h < V / 4; ++h) decode4<true>(cm[h], (int)old_m, m + 4 * h), decode4<false>(cv[h], (int)old_v, v + 4 * h);
 #pragma unroll
             for (int q = 0; q < V; ++q) {
-                const uint64_t e = (uint64_t)(at + q);
-                const uint32_t random = mix((uint32_t)e * 0x9E3779B1u + (uint32_t)(e >> 32) * 0xA54FF53Bu + key);
-                cm[q] = encode<true>(m[q], new_m, random & 0xFFFF);
-                cv[q] = encode<false>(v[q], new_v, random >> 16);
+                r.apply(p[q], g[q], m[q], v[q], by1, by2);
             }
-            store8(mc + at, n, cm);
-            store8(vc + at, n, cv);
+            if (n < V) {  // past the end, also in a block of NaN
+#pragma unroll
+                for (int q = 0; q < V; ++q)
+                    if (q >= n) m[q] = v[q] = 0.0f;
+            }
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+                top_m = max(top_m, __float_as_uint(m[q]) & 0x7FFFFFFF);
+                top_v = max(top_v, __float_as_uint(v[q]));  // not negative, but for a NaN
+            }
+            const uint32_t new_m = block_scale(half_wave_max(top_m)), new_v = block_scale(half_wave_max(top_v));
+            const uint32_t first = (uint32_t)at * 0x9E3779B1u + (uint32_t)((uint64_t)at >> 32) * 0xA54FF53Bu + key;
+#pragma unroll
+            for (int h = 0; h < V / 4; ++h) cm[h] = cv[h] = 0;
+#pragma unroll
+            for (int q = 0; q < V; ++q) {  // a thread's eight numbers share their upper half
+                const uint32_t random = mix(first + (uint32_t)q * 0x9E3779B1u);
+                cm[q / 4] |= encode<true>(m[q], (int)new_m, new_m != 0, (random & 0xFFFF) << 4) << (8 * (q % 4));
+                cv[q / 4] |= encode<false>(v[q], (int)new_v, new_v != 0, random >> 16 << 4) << (8 * (q % 4));
+            }
+            store_codes<V>(mc + at, n, cm);
+            store_codes<V>(vc + at, n, cv);
             if (threadIdx.x % 32 == 0) t.m_scales[i][block] = (uint8_t)new_m, t.v_scales[i][block] = (uint8_t)new_v;
             if (master) store<V>(master + at, n, p);
             store_any<V>(t.param[i], type, at, n, p);
@@ -242,20 +256,15 @@ __global__ __launch_bounds__(kThreads) void k_adamw_values(const AdamwTable t)
     for (int64_t at = from + V * (int64_t)threadIdx.x; at < to; at += V * kThreads) {
         const int n = (int)min((int64_t)V, to - at);
         const uint32_t sm = t.m_scales[i][at / kStateBlock], sv = t.v_scales[i][at / kStateBlock];
-        typedef uint32_t any __attribute__((aligned(1)));
-        uint32_t cm = 0, cv = 0;
-        if (n == V) {
-            cm = *reinterpret_cast<const any *>(mc + at);
-            cv = *reinterpret_cast<const any *>(vc + at);
-        } else {
-            for (int q = 0; q < n; ++q) cm |= (uint32_t)mc[at + q] << (8 * q), cv |= (uint32_t)vc[at + q] << (8 * q);
-        }
+        const float by_m = block_factor(sm, 1.0f), by_v = block_factor(sv, 1.0f);
+        uint32_t cm, cv;
+        load_codes<V>(mc + at, n, &cm);
+        load_codes<V>(vc + at, n, &cv);
         float m[V], v[V];
+        decode4<true>(cm, (int)sm, m);
+        decode4<false>(cv, (int)sv, v);
 #pragma unroll
-        for (int q = 0; q < V; ++q) {
-            m[q] = scaled_value(code_value<true>(cm >> (8 * q) & 255), sm);
-            v[q] = scaled_value(code_value<false>(cv >> (8 * q) & 255), sv);
-        }
+        for (int q = 0; q < V; ++q) m[q] *= by_m, v[q] *= by_v;
         store<V>(om + at, n, m);
         store<V>(ov + at, n, v);
     }

@@ -152,24 +152,27 @@ __device__ inline void values_columns(const FourArgs &a, int32_t row_blocks, T *
     }
 }
 
-// A workgroup takes 16 vectors of columns by 16 blocks at a time; f(first column, block).
+// A wave takes 16 vectors of columns by four blocks at a time; f(first column, block). Workgroups are single
+// waves, which spread over the CUs (1,003 x 5,625 fp32 is 704 of them).
+constexpr int kColumnBlocks = 4;
+
 template <int V, typename F> __device__ inline void over_columns(const FourArgs &a, int32_t row_blocks, F f)
 {
-    const int64_t across = (a.N + 16 * V - 1) / (16 * V), total = across * ((row_blocks + 15) / 16);
+    const int64_t across = (a.N + 16 * V - 1) / (16 * V), total = across * ((row_blocks + kColumnBlocks - 1) / kColumnBlocks);
     for (int64_t i = blockIdx.x; i < total; i += gridDim.x) {
         const int64_t col = (i % across * 16 + threadIdx.x % 16) * V;
-        const int block = (int)(i / across) * 16 + (int)threadIdx.x / 16;
+        const int block = (int)(i / across) * kColumnBlocks + (int)threadIdx.x / 16;
         if (col < a.N && block < row_blocks) f(col, block);
     }
 }
 
-template <typename T> __global__ __launch_bounds__(kThreads) void k_quantise_columns(const FourArgs a, int32_t row_blocks)
+template <typename T> __global__ __launch_bounds__(64) void k_quantise_columns(const FourArgs a, int32_t row_blocks)
 {
     over_columns<16 / sizeof(T)>(a, row_blocks, [&](int64_t col, int block) { quantise_columns<T>(a, row_blocks, col, block); });
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_values_columns(const FourArgs a, int32_t row_blocks, T *y, int64_t ldy)
+__global__ __launch_bounds__(64) void k_values_columns(const FourArgs a, int32_t row_blocks, T *y, int64_t ldy)
 {
     over_columns<16 / sizeof(T)>(a, row_blocks, [&](int64_t col, int block) { values_columns<T>(a, row_blocks, y, ldy, col, block); });
 }
@@ -179,7 +182,7 @@ constexpr int64_t kGroups = 1 << 20;  // workgroups of a launch, which go on fro
 template <typename T> dim3 column_grid(const FourArgs &a, int64_t row_blocks)
 {
     constexpr int V = 16 / sizeof(T);
-    const int64_t n = (a.N + 16 * V - 1) / (16 * V) * ((row_blocks + 15) / 16);
+    const int64_t n = (a.N + 16 * V - 1) / (16 * V) * ((row_blocks + kColumnBlocks - 1) / kColumnBlocks);
     return dim3((unsigned)(n < kGroups ? n : kGroups));
 }
 
@@ -187,7 +190,7 @@ template <typename T> hipError_t quantise(bool columns, const FourArgs &a, hipSt
 {
     const int64_t row_blocks = four_blocks(a.K), blocks = a.N * row_blocks;
     if (columns) {
-        hipLaunchKernelGGL(k_quantise_columns<T>, column_grid<T>(a, row_blocks), dim3(kThreads), 0, st, a, (int32_t)row_blocks);
+        hipLaunchKernelGGL(k_quantise_columns<T>, column_grid<T>(a, row_blocks), dim3(64), 0, st, a, (int32_t)row_blocks);
     } else {
         const int64_t n = (blocks + kThreads / 4 - 1) / (kThreads / 4);
         hipLaunchKernelGGL(k_quantise_rows<T>, dim3((unsigned)(n < kGroups ? n : kGroups)), dim3(kThreads), 0, st, a, blocks,
@@ -200,7 +203,7 @@ template <typename T> hipError_t values(bool columns, const FourArgs &a, void *y
 {
     const int64_t row_blocks = four_blocks(a.K), blocks = a.N * row_blocks;
     if (columns) {
-        hipLaunchKernelGGL(k_values_columns<T>, column_grid<T>(a, row_blocks), dim3(kThreads), 0, st, a, (int32_t)row_blocks, static_cast<T *>(y), ldy);
+        hipLaunchKernelGGL(k_values_columns<T>, column_grid<T>(a, row_blocks), dim3(64), 0, st, a, (int32_t)row_blocks, static_cast<T *>(y), ldy);
     } else {
         const int64_t n = (blocks + kThreads / 4 - 1) / (kThreads / 4);
         hipLaunchKernelGGL(k_values_rows<T>, dim3((unsigned)(n < kGroups ? n : kGroups)), dim3(kThreads), 0, st, a, blocks,

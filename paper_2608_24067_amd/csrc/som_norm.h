@@ -46,19 +46,20 @@ __device__ inline void moments(double s, double q, double from, int D, double ep
 }
 
 // (x - mean) / std in fp32: the mean in two parts, so that a mean much larger than the spread costs
-// nothing. Where fp32's range does not hold the differences they are formed in fp64.
+// nothing. Rows that come near the end of fp32's range are scaled down first, which is exact and, in the
+// fused product, free.
 struct Centre {
-    float hi, lo, inv;
-    double mean, inv64;
-    bool wide;
-    __device__ Centre(double m, double i) : hi((float)m), lo((float)(m - (double)(float)m)), inv((float)i), mean(m), inv64(i)
+    float scale, hi, lo, inv, inv_std;
+    __device__ Centre(double mean, double i) : inv_std((float)i)
     {
-        wide = !(fabs(m) < 0x1p125 && i > 0x1p-120);
+        const bool far = !(fabs(mean) < 0x1p125 && i > 0x1p-120);
+        const double s = far ? 0x1p-32 : 1.0;
+        scale = (float)s;
+        hi = (float)(mean * s);
+        lo = (float)(mean * s - (double)hi);
+        inv = (float)(i * (far ? 0x1p32 : 1.0));
     }
-    __device__ float of(float x) const
-    {
-        return wide ? (float)(((double)x - mean) * inv64) : ((x - hi) - lo) * inv;
-    }
+    __device__ float of(float x) const { return (fmaf(x, scale, -hi) - lo) * inv; }
 };
 
 template <typename Y, int V> __device__ inline void load_weight(const void *p, bool f32, int at, int n, float *v, float none)
@@ -199,7 +200,8 @@ template <typename X, typename Y> __global__ __launch_bounds__(1024) void k_norm
 //   dx = add + (t - mean(t) - h mean(t h)) / std,   dweight = sum over rows of dy h,   dbias = of dy.
 // A workgroup takes part_rows rows and holds its sums of dweight and dbias in registers; they are
 // joined over its waves in LDS and written as one part, and k_norm_sums adds the parts in order.
-template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT) void k_norm_grad(const NormArgs a)
+// Two workgroups a CU, whose loads hide each other's exchanges, where a thread has two vectors at most.
+template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT, S::C <= 2 ? 4 : 2) void k_norm_grad(const NormArgs a)
 {
     typedef typename S::X X;
     typedef typename S::Y Y;
@@ -262,7 +264,7 @@ template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT) void k_norm_g
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const float h = centre.of((float)xn.v[c][i]), u = (float)gn.v[c][i] * w[c][i];
-                        v[i] = (u - s - h * q) * centre.inv;
+                        v[i] = (u - s - h * q) * centre.inv_std;
                         if (a.add) v[i] += more[i];
                     }
                     store<V>(static_cast<X *>(a.dx) + row * a.lddx + at, WHOLE ? V : D - at, v);
@@ -352,7 +354,7 @@ template <typename X, typename Y> __global__ __launch_bounds__(256) void k_norm_
             const float h = centre.of(v[i]);
             dw[i] = fmaf(g[i], h, dw[i]);
             db[i] += g[i];
-            v[i] = (g[i] * w[i] - s - h * q) * centre.inv;
+            v[i] = (g[i] * w[i] - s - h * q) * centre.inv_std;
             if (a.add) v[i] += more[i];
         }
         if (a.dx) store<V>(static_cast<X *>(a.dx) + row * a.lddx + at, n, v);

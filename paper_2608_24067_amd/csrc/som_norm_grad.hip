@@ -24,7 +24,7 @@ template <typename X, typename Y> hipError_t by_width(const NormArgs &a, hipStre
     if (vectors <= 32) return grad<NormShape<X, Y, 32, 1, 512>>(a, st);
     if (vectors <= 64) return grad<NormShape<X, Y, 64, 1, 512>>(a, st);
     if (vectors <= 128) return grad<NormShape<X, Y, 64, 2, 512>>(a, st);
-    if (vectors <= 256) return grad<NormShape<X, Y, 64, 4, 512>>(a, st);
+    if (vectors <= 256) return grad<NormShape<X, Y, 128, 2, 512>>(a, st);
     if (vectors <= 512) return grad<NormShape<X, Y, 256, 2, 512>>(a, st);
     if (vectors <= 1024) return grad<NormShape<X, Y, 512, 2, 512>>(a, st);
     if (vectors <= 2048) return grad<NormShape<X, Y, 512, 4, 512>>(a, st);

@@ -27,6 +27,7 @@ template <typename X, typename Y> hipError_t by_width(const NormArgs &a, hipStre
     if (vectors <= 16) return rows<NormShape<X, Y, 16, 1, 256>>(a, st);
     if (vectors <= 32) return rows<NormShape<X, Y, 32, 1, 256>>(a, st);
     if (vectors <= 64) return rows<NormShape<X, Y, 64, 1, 256>>(a, st);
+    if (a.N <= 256 && vectors <= 512) return rows<NormShape<X, Y, 256, 2, 256>>(a, st);  // a row a CU: latency counts
     if (vectors <= 128) return rows<NormShape<X, Y, 64, 2, 256>>(a, st);
     if (vectors <= 256) return rows<NormShape<X, Y, 64, 4, 256>>(a, st);
     if (vectors <= 512) return rows<NormShape<X, Y, 256, 2, 256>>(a, st);

@@ -14,6 +14,8 @@ from __future__ import annotations
 
 import ctypes
 import functools
+from array import array
+from itertools import chain
 from typing import NamedTuple, Optional
 
 import torch
@@ -350,9 +352,15 @@ def clip(tensors, max_norm: float, out=None, norm=None, workspace=None):
 
 # ------------------------------------------------------------------ layer norm
 
+try:  # the current device's number, without the wait for its initialisation that torch's own function checks for
+    _device = torch._C._cuda_getDevice
+except AttributeError:
+    _device = torch.cuda.current_device
+
+
 def _on(device, call, *args):
     """A call with `device` as the current one, which a launch on one of its streams needs."""
-    if device.index == torch.cuda.current_device():
+    if device.index == _device():
         return call(*args)
     with torch.cuda.device(device):
         return call(*args)
@@ -428,9 +436,8 @@ class AdamwState(NamedTuple):
     master: Optional[torch.Tensor] = None
 
 
-class _AdamwTensor(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scales", "v_scales", "master")] + [
-        ("size", ctypes.c_int64), ("type", ctypes.c_int32), ("grad_type", ctypes.c_int32)]
+# A tensor of a step as the C structure holds it: nine words of 64 bits, seven pointers, the size and the two types.
+_ADAMW_WORDS = 9
 
 
 class _AdamwConfig(ctypes.Structure):
@@ -457,26 +464,49 @@ def adamw_state(param, bits: int = 32, master: bool = False) -> AdamwState:
     return AdamwState(m, v, ms, vs, copy)
 
 
+def _refuse_held(t, name, n, dtype):
+    raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on the parameters' GPU"
+                     + (f" (got {t.dtype}, {t.numel()} elements on {t.device})" if isinstance(t, torch.Tensor) else ""))
+
+
 def _held(t, name, n, dtype, at):
     """The pointer of a contiguous tensor of n elements on device number `at`."""
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.numel() != n or t.get_device() != at or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on the parameters' GPU")
+        _refuse_held(t, name, n, dtype)
     return t.data_ptr()
 
 
-def _state_into(x, state, n, eight, at):
-    """Checks a state and puts its pointers into the C structure."""
-    m, v, ms, vs, master = state
-    kind = torch.uint8 if eight else torch.float32
-    x.m, x.v, x.size = _held(m, "m", n, kind, at), _held(v, "v", n, kind, at), n
-    if eight:
-        blocks = (n + STATE_BLOCK - 1) // STATE_BLOCK
-        x.m_scales = _held(ms, "m_scales", blocks, torch.uint8, at)
-        x.v_scales = _held(vs, "v_scales", blocks, torch.uint8, at)
-    elif ms is not None or vs is not None:
+def _held_all(ts, name, dtype, sizes, at):
+    """The pointers of such tensors; dtype None: of any type."""
+    try:
+        if ([t.numel() for t in ts] == sizes and {t.get_device() for t in ts} == {at}
+                and (dtype is None or {t.dtype for t in ts} == {dtype}) and all([t.is_contiguous() for t in ts])):
+            return [t.data_ptr() for t in ts]
+    except AttributeError:  # something that is no tensor
+        pass
+    return [_held(t, name, n, t.dtype if dtype is None else dtype, at) for t, n in zip(ts, sizes)]
+
+
+def _state_pointers(states, sizes, eight, at):
+    """Checks the states and returns their pointers, in the C structure's order: m, v, their scales, the masters."""
+    ms, vs, m_scales, v_scales, masters = zip(*states)
+    none, kind = [0] * len(sizes), torch.uint8 if eight else torch.float32
+    if any([(x is not None) != eight for x in m_scales]) or any([(x is not None) != eight for x in v_scales]):
         raise ValueError("the states must all be in 32 bits, or all in 8")
-    if master is not None:
-        x.master = _held(master, "master", n, torch.float32, at)
+    scales = (none, none)
+    if eight:
+        blocks = [(n + STATE_BLOCK - 1) // STATE_BLOCK for n in sizes]
+        scales = (_held_all(m_scales, "m_scales", kind, blocks, at), _held_all(v_scales, "v_scales", kind, blocks, at))
+    copies = none
+    if masters.count(None) < len(sizes):
+        copies = [0 if t is None else _held(t, "master", n, torch.float32, at) for t, n in zip(masters, sizes)]
+    return (_held_all(ms, "m", kind, sizes, at), _held_all(vs, "v", kind, sizes, at), *scales, copies)
+
+
+def _table(*columns):
+    """The C structures, one after the other, and their address."""
+    words = array("q", list(chain.from_iterable(zip(*columns))))
+    return words, words.buffer_info()[0]
 
 
 def _scalar_at(t, name, dtype, dev):
@@ -505,18 +535,15 @@ def adamw(params, grads, states, step, lr=1e-3, betas=(0.9, 0.999), eps: float =
         raise ValueError("the parameters must be on the GPU")
     dev = params[0].device
     at, eight = dev.index, states[0][2] is not None
-    table = (_AdamwTensor * n)()
-    for x, p, g, state in zip(table, params, grads, states):
-        for t, name in ((p, "params"), (g, "grads")):
-            if not isinstance(t, torch.Tensor) or t.dtype not in _TYPES:
-                _type(t, name, halves=False)
-        m = p.numel()
-        x.param, x.grad = _held(p, "params", m, p.dtype, at), _held(g, "grads", m, g.dtype, at)
-        x.type, x.grad_type = _TYPES[p.dtype], _TYPES[g.dtype]
-        if (state[2] is not None) != eight:
-            raise ValueError("the states must all be in 32 bits, or all in 8")
-        _state_into(x, state, m, eight, at)
-    if len({x.param for x in table if x.size}) < sum(1 for x in table if x.size):
+    kinds, grad_kinds = ([_TYPES.get(getattr(t, "dtype", None)) for t in ts] for ts in (params, grads))
+    if None in kinds or None in grad_kinds:
+        for t in params + grads:
+            _type(t, "params and grads", halves=False)
+    sizes = [t.numel() for t in params]
+    pointers = _held_all(params, "params", None, sizes, at)
+    table, address = _table(pointers, _held_all(grads, "grads", None, sizes, at), *_state_pointers(states, sizes, eight, at),
+                            sizes, [k | g << 32 for k, g in zip(kinds, grad_kinds)])
+    if len(set(pointers)) < n and len({p for p, m in zip(pointers, sizes) if m}) < sum([m > 0 for m in sizes]):
         raise ValueError("params holds a tensor twice")
     c = _AdamwConfig()
     if isinstance(lr, torch.Tensor):
@@ -529,7 +556,7 @@ def adamw(params, grads, states, step, lr=1e-3, betas=(0.9, 0.999), eps: float =
     c.grad_scale, c.step, c.bits, c.seed = float(grad_scale), int(step), 8 if eight else 32, int(seed)
     if norm is not None:
         c.norm = _scalar_at(norm, "norm", torch.float32, dev)
-    _check(_on(dev, load().som_adamw, table, n, ctypes.byref(c), _stream(params[0])), "som_adamw")
+    _check(_on(dev, load().som_adamw, address, n, ctypes.byref(c), _stream(params[0])), "som_adamw")
 
 
 def adamw_values(states, out=None):
@@ -545,12 +572,11 @@ def adamw_values(states, out=None):
     if not isinstance(states[0][0], torch.Tensor) or not states[0][0].is_cuda:
         raise ValueError("the states must be on the GPU")
     dev = states[0][0].device
-    table = (_AdamwTensor * n)()
-    for x, state in zip(table, states):
-        _state_into(x, AdamwState(*state[:4]), state[0].numel(), True, dev.index)
-    tos = [(ctypes.c_void_p * n)(*[_held(t, name, x.size, torch.float32, dev.index) for t, x in zip(ts, table)])
-           for ts, name in zip(out, ("m", "v"))]
-    _check(_on(dev, load().som_adamw_values, table, n, tos[0], tos[1], _stream(states[0][0])), "som_adamw_values")
+    sizes, none = [s[0].numel() for s in states], [0] * n
+    held = _state_pointers([(*s[:4], None) for s in states], sizes, True, dev.index)
+    table, address = _table(none, none, *held, sizes, none)  # read during the call
+    tos = [array("q", _held_all(ts, name, torch.float32, sizes, dev.index)) for ts, name in zip(out, ("m", "v"))]
+    _check(_on(dev, load().som_adamw_values, address, n, tos[0].buffer_info()[0], tos[1].buffer_info()[0], _stream(states[0][0])), "som_adamw_values")
     return out
 
 

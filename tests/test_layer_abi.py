@@ -58,8 +58,14 @@ def test_layer_norm_refusals():
         assert lib.som_layer_norm_bwd_workspace_bytes(*bad) == 0
 
 
+class Tensor(ctypes.Structure):
+    """som_adamw_tensor"""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scales", "v_scales", "master")] + [
+        ("size", ctypes.c_int64), ("type", ctypes.c_int32), ("grad_type", ctypes.c_int32)]
+
+
 def adamw(tensor=None, count=1, **k):
-    t = dense._AdamwTensor()
+    t = Tensor()
     for n in ("param", "grad", "m", "v", "m_scales", "v_scales", "master"):
         setattr(t, n, 1 << 20)
     t.size, t.type, t.grad_type = 1000, 2, 0
@@ -71,7 +77,7 @@ def adamw(tensor=None, count=1, **k):
             c.reserved[3] = v
         else:
             setattr(c, n, v)
-    return som.load().som_adamw((dense._AdamwTensor * 1)(t), count, ctypes.byref(c), None)
+    return som.load().som_adamw((Tensor * 1)(t), count, ctypes.byref(c), None)
 
 
 def test_adamw_refusals():
@@ -92,9 +98,9 @@ def test_adamw_refusals():
     assert lib.som_adamw(None, 1, None, None) == INVALID
     assert adamw(count=0) == som.SOM_OK
     assert adamw(dict(size=0, param=None, grad=None, m=None, v=None)) == som.SOM_OK
-    t = dense._AdamwTensor(m=1 << 20, v=1 << 20, m_scales=1 << 20, v_scales=1 << 20, size=10)
+    t = Tensor(m=1 << 20, v=1 << 20, m_scales=1 << 20, v_scales=1 << 20, size=10)
     one, none, off = ((ctypes.c_void_p * 1)(p) for p in (1 << 20, None, (1 << 20) + 2))
-    table = (dense._AdamwTensor * 1)(t)
+    table = (Tensor * 1)(t)
     for m, v in ((none, one), (one, none), (off, one), (None, one), (one, None)):
         assert lib.som_adamw_values(table, 1, m, v, None) == INVALID
     assert lib.som_adamw_values(None, 0, None, None, None) == som.SOM_OK
@@ -231,4 +237,4 @@ int main(void)
                         "-o", exe, f"-L{PKG}", "-lsom", f"-Wl,-rpath,{PKG}"], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
     assert subprocess.run([exe], timeout=120).returncode == 0
-    assert ctypes.sizeof(dense._AdamwTensor) == 72 and ctypes.sizeof(dense._AdamwConfig) == 120
+    assert ctypes.sizeof(Tensor) == 72 == 8 * dense._ADAMW_WORDS and ctypes.sizeof(dense._AdamwConfig) == 120
