@@ -141,18 +141,21 @@ struct FourProduct {
     int64_t ldy;
     bool y_f32;
     int64_t N, K, M;
+    int64_t width;  // features of x's rows, K or more (zeros behind K)
 };
 
-hipError_t launch_mx4_few(bool bf16, const FourProduct &p, hipStream_t st);
+// The tile of a workgroup; the first four are those of the kernel for few rows.
+enum FourTile { kFour16x16, kFour16x32, kFour32x32, kFour32x64, kFour64, kFour128, kFour256 };
+hipError_t launch_mx4_few(bool bf16, FourTile t, const FourProduct &p, hipStream_t st);
 
-// The same for many rows, by tiles of 128 x 128 or 256 x 256. Rows in 16 bits must be whole 16-byte
-// chunks, rows of scales whole 16-byte pieces (four_pitch).
-enum FourTile { kFourMid, kFourLarge };
+// The same for many rows. Rows in 16 bits must be whole lines of 128 bytes (four_width), rows of scales
+// whole 16-byte pieces (four_pitch).
 hipError_t launch_mx4_half(bool bf16, FourTile t, const FourProduct &p, hipStream_t st);
 hipError_t launch_mx4_packed(bool bf16, FourTile t, const FourProduct &p, hipStream_t st);
 
+inline int64_t four_width(int64_t K) { return (K + 63) / 64 * 64; }
 __host__ __device__ inline int64_t four_pitch(int64_t K) { return (four_blocks(K) + 15) / 16 * 16; }
-// Rows' scales to rows of four_pitch bytes, and rows of K values to rows of whole blocks, zeros behind them.
+// Rows' scales to rows of four_pitch bytes, and rows of K values to rows of four_width; zeros behind them.
 hipError_t launch_pad_scales(const uint8_t *scales, int64_t rows, int64_t K, uint8_t *to, hipStream_t st);
 hipError_t launch_pad_rows(const void *x, int64_t ldx, int64_t rows, int64_t K, void *to, hipStream_t st);
 

@@ -110,27 +110,49 @@ const char *product_sizes(int64_t N, int64_t K, int64_t M)
 
 // How a product is computed, and what of its workspace holds what.
 struct FourLayout {
-    bool few;
     som::FourTile tile;
     int64_t strip;            // rows in 16 bits that are copied and multiplied at a time
     size_t x, xs, ws, total;  // their copy, and padded rows of scales
 };
 
-// Rows up to which the kernel for few rows reads the matrix straight into registers.
-constexpr int64_t kFourFew = 64;
-
 // Bytes of the copied rows at most: strips of them stay in the cache.
 constexpr int64_t kFourStrip = (int64_t)32 << 20;
+// Features up to which the rows of a tile lie within the 32-bit offsets that its loads use.
+constexpr int64_t kFourMostWidth = (int64_t)1 << 22;
 
-FourLayout four_layout(int64_t N, int64_t K, int64_t M, bool packed)
+int64_t four_tiles(int64_t N, int64_t M, int64_t rows, int64_t cols) { return (N + rows - 1) / rows * ((M + cols - 1) / cols); }
+
+// The tile of a product. The kernel for few rows reads the operands straight into registers and is bound
+// by a CU's reads, about 28 KB a us: the smallest of its tiles whose workgroups are one a CU at most. In
+// us, bf16 rows, by 16 x 16, 16 x 32, 32 x 32, 32 x 64 and by tiles of 64 through LDS:
+//    64 x 4096 x 1024   8.4  10.2  14.4  18.3  21.5      128 x 4096 x 4096   45  32  27  19.0  22.2
+//    64 x 4096 x 4096   25   17.6  14.7  18.5  21.9      128 x 2048 x 8192   46  33  29  20.9  13.8
+// Of fp16 rows 32 x 64 does not fit the registers; up to 16 rows take 16 x 32 at any number of columns
+// (1 x 1024 x 32768: 8.5, by 64 10.9). Rows in 4 bits go through LDS once 16 x 32 is too small (64 x
+// 4096 x 4096: 17.5, 13.9, 10.9 by the first three, 8.7 by 64; 1 x 1024 x 32768 7.3, 7.6, 8.2, 6.0).
+// Through LDS a tile is 64 while two a CU hold all (by 64, 128, 256 in bf16: 512 x 4096 x 4096 36, 42, 85;
+// 1024 x 4096 x 4096 51, 46, 85; in 4 bits 12.8, 14.6, 28.7 and 22.1, 17.8, 30.8), and 256 where that
+// fills three CUs in four (2048 x 2048 x 8192 104, 70, 60; 42.6, 31.9, 27.0).
+som::FourTile four_tile(int64_t N, int64_t K, int64_t M, bool packed, bool bf16)
+{
+    if (K > kFourMostWidth) return N <= 16 ? som::kFour16x32 : som::kFour32x32;
+    if (four_tiles(N, M, 16, 16) <= 256) return som::kFour16x16;
+    if (four_tiles(N, M, 16, 32) <= 256 || (!packed && N <= 16)) return som::kFour16x32;
+    if (!packed && four_tiles(N, M, 32, 32) <= 256) return som::kFour32x32;
+    if (!packed && bf16 && four_tiles(N, M, 32, 64) <= 256) return som::kFour32x64;
+    if (four_tiles(N, M, 256, 256) >= 192) return som::kFour256;
+    return four_tiles(N, M, 64, 64) <= 512 ? som::kFour64 : som::kFour128;
+}
+
+bool few_rows(som::FourTile t) { return t <= som::kFour32x64; }
+
+FourLayout four_layout(int64_t N, int64_t K, int64_t M, bool packed, bool bf16)
 {
     FourLayout L{};
-    const int64_t row = som::four_blocks(K) * 64, most = kFourStrip / row / 256 * 256;
-    L.strip = packed || N < most ? N : most;
-    L.few = N <= kFourFew || L.strip == 0;
-    if (L.few) return L;
-    const int64_t tiles = (N + 255) / 256 * ((M + 255) / 256);
-    L.tile = tiles >= 128 ? som::kFourLarge : som::kFourMid;
+    L.tile = four_tile(N, K, M, packed, bf16);
+    if (few_rows(L.tile)) return L;
+    const int64_t row = som::four_width(K) * 2, most = kFourStrip / row / 256 * 256;
+    L.strip = packed || N < most ? N : most;  // 0: rows that long are not copied
     const bool ragged = som::four_blocks(K) % 16 != 0;
     size_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -292,7 +314,8 @@ som_status som_mx4_values(int32_t type, const uint8_t *codes, const uint8_t *sca
 size_t som_mx4_linear_workspace_bytes(int64_t N, int64_t K, int64_t M, int32_t packed)
 {
     if (product_sizes(N, K, M) || (packed != 0 && packed != 1)) return 0;
-    return four_layout(N, K, M, packed == 1).total;
+    const size_t a = four_layout(N, K, M, packed == 1, true).total, b = four_layout(N, K, M, packed == 1, false).total;
+    return a > b ? a : b;  // of either type
 }
 
 som_status som_mx4_linear(int32_t type, const void *X, int64_t ldx, const uint8_t *x_scales, const uint8_t *w_codes,
@@ -318,12 +341,15 @@ som_status som_mx4_linear(int32_t type, const void *X, int64_t ldx, const uint8_
     som::FourProduct p{};
     p.x = X, p.ldx = ldx, p.x_scales = x_scales, p.w = w_codes, p.w_scales = w_scales;
     p.bias = bias, p.bias_f32 = bias_type == SOM_F32, p.act = act, p.res = residual, p.ldr = ldr;
-    p.y = Y, p.ldy = ldy, p.y_f32 = y_type == SOM_F32, p.N = N, p.K = K, p.M = M;
+    p.y = Y, p.ldy = ldy, p.y_f32 = y_type == SOM_F32, p.N = N, p.K = p.width = K, p.M = M;
     const bool bf16 = type == SOM_BF16, packed = x_scales != nullptr;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const FourLayout L = four_layout(N, K, M, packed);
+    const FourLayout L = four_layout(N, K, M, packed, bf16);
     const bool ragged = som::four_blocks(K) % 16 != 0;
-    if (L.few || (!ragged && (off(w_scales, 16) || off(x_scales, 16)))) return done(som::launch_mx4_few(bf16, p, s), who);
+    const bool whole = packed || (!off(X, 16) && ldx % 8 == 0 && ldx <= kFourMostWidth && K % 64 == 0);
+    // Tiles take rows of scales that start on 16 bytes, and whole lines of the rows, or a copy of them.
+    if (few_rows(L.tile) || (!ragged && (off(w_scales, 16) || off(x_scales, 16))) || (!whole && L.strip == 0))
+        return done(som::launch_mx4_few(bf16, few_rows(L.tile) ? L.tile : som::kFour32x32, p, s), who);
     char *b = static_cast<char *>(workspace);
     p.x_pitch = p.w_pitch = som::four_pitch(K);
     if (ragged) {
@@ -335,12 +361,12 @@ som_status som_mx4_linear(int32_t type, const void *X, int64_t ldx, const uint8_
         if (packed) p.x_scales = xs;
     }
     if (packed) return done(som::launch_mx4_packed(bf16, L.tile, p, s), who);
-    if (!off(X, 16) && ldx % 8 == 0 && K % 8 == 0) return done(som::launch_mx4_half(bf16, L.tile, p, s), who);
-    const int64_t width = som::four_blocks(K) * 32;
+    if (whole) return done(som::launch_mx4_half(bf16, L.tile, p, s), who);
+    const int64_t width = som::four_width(K);
     for (int64_t n = 0; n < N; n += L.strip) {
         som::FourProduct q = p;
         q.N = N - n < L.strip ? N - n : L.strip;
-        q.x = b + L.x, q.ldx = width, q.K = width;
+        q.x = b + L.x, q.ldx = width, q.width = width;
         q.res = residual ? static_cast<const char *>(residual) + n * ldr * 2 : nullptr;
         q.y = static_cast<char *>(Y) + n * ldy * size_of(y_type);
         hipError_t e = som::launch_pad_rows(static_cast<const char *>(X) + n * ldx * 2, ldx, q.N, K, b + L.x, s);

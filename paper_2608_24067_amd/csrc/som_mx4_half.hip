@@ -20,11 +20,12 @@ template <typename T, class S> hipError_t launch(const FourProduct &p, hipStream
 
 template <typename T> hipError_t by_tile(FourTile t, const FourProduct &p, hipStream_t st)
 {
-    if (t == kFourMid) return launch<T, Tile<128, 128, 2, 2, 2>>(p, st);
+    if (t == kFour64) return launch<T, Tile<64, 64, 2, 2, 2>>(p, st);
+    if (t == kFour128) return launch<T, Tile<128, 128, 2, 2, 2>>(p, st);
     return launch<T, Tile<256, 256, 2, 4, 1>>(p, st);
 }
 
-// 16-byte chunks of whole blocks of a row, from rows of any alignment.
+// 16-byte chunks of whole lines of a row, from rows of any alignment.
 __global__ __launch_bounds__(256) void k_pad_rows(const uint16_t *x, int64_t ldx, int64_t rows, int32_t K, int32_t chunks, uint4 *to)
 {
     typedef uint16_t eight __attribute__((ext_vector_type(8)));
@@ -55,7 +56,7 @@ hipError_t launch_mx4_half(bool bf16, FourTile t, const FourProduct &p, hipStrea
 
 hipError_t launch_pad_rows(const void *x, int64_t ldx, int64_t rows, int64_t K, void *to, hipStream_t st)
 {
-    const int64_t chunks = four_blocks(K) * 4, groups = (rows * chunks + 255) / 256;
+    const int64_t chunks = four_width(K) / 8, groups = (rows * chunks + 255) / 256;
     hipLaunchKernelGGL(k_pad_rows, dim3((unsigned)(groups < 1 << 20 ? groups : 1 << 20)), dim3(256), 0, st,
                        static_cast<const uint16_t *>(x), ldx, rows, (int32_t)K, (int32_t)chunks, static_cast<uint4 *>(to));
     return hipGetLastError();

@@ -20,11 +20,13 @@ template <typename T, class S> hipError_t launch(const FourProduct &p, hipStream
 
 template <typename T> hipError_t by_tile(FourTile t, const FourProduct &p, hipStream_t st)
 {
-    if (t == kFourMid) return launch<T, Tile<128, 128, 2, 2, 2>>(p, st);
+    if (t == kFour64) return launch<T, Tile<64, 64, 2, 2, 2>>(p, st);
+    if (t == kFour128) return launch<T, Tile<128, 128, 2, 2, 2>>(p, st);
     return launch<T, Tile<256, 256, 2, 4, 1>>(p, st);
 }
 
-// A scale that no block has stands past the last one: its codes are zeros.
+// Past the last block stands the smallest scale: what a product of two of them meets is nothing in fp32
+// (2^-254), and with zeros it makes zeros.
 __global__ __launch_bounds__(256) void k_pad_scales(const uint8_t *scales, int64_t rows, int32_t blocks, int32_t pitch, uint8_t *to)
 {
     const int64_t total = rows * (pitch / 16), step = (int64_t)gridDim.x * 256;
@@ -32,10 +34,10 @@ __global__ __launch_bounds__(256) void k_pad_scales(const uint8_t *scales, int64
         const int64_t row = at / (pitch / 16);
         const int b = (int)(at - row * (pitch / 16)) * 16;
         const uint8_t *from = scales + row * blocks + b;
-        uint32_t v[4] = {0x7F7F7F7F, 0x7F7F7F7F, 0x7F7F7F7F, 0x7F7F7F7F};
+        uint32_t v[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            if (b + i < blocks) v[i / 4] = (v[i / 4] & ~(255u << (8 * (i % 4)))) | (uint32_t)from[i] << (8 * (i % 4));
+            if (b + i < blocks) v[i / 4] |= (uint32_t)from[i] << (8 * (i % 4));
         reinterpret_cast<uint4 *>(to)[at] = uint4{v[0], v[1], v[2], v[3]};
     }
 }

@@ -225,3 +225,60 @@ def test_residual_in_place_and_no_rows(dev):
     q = dense.mx4_quantise(x[:0])
     assert q.codes.shape == (0, 64) and dense.mx4_values(q).shape == (0, 100)
     assert dense.mx4_linear(q, W).shape == (0, 90)
+
+
+# Every tile, and its edges: sizes on both sides of the rules' bounds.
+TILES = [(16, 70, 4096), (16, 70, 4100), (16, 70, 8192), (16, 70, 8200), (33, 200, 3000), (128, 100, 1025), (60, 96, 5000),
+         (31, 64, 16000), (300, 320, 2000), (1000, 33, 2000), (1500, 577, 2000), (2500, 96, 5000), (3300, 513, 3700)]
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("N,K,M", TILES)
+def test_tiles(dev, dtype, packed, N, K, M):
+    product(dev, dtype, N, K, M, packed, a="silu", bias=dtype, res=True, extra=1)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_rows_copied_in_strips(dev, dtype):
+    # 36 MB of padded rows, so two strips; the last one is short
+    product(dev, dtype, 8200, 2113, 130, False, res=True, bias=F32, extra=1)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("K", [160, 544, 600, 1000])
+@pytest.mark.parametrize("N,M", [(300, 1500), (2100, 2100), (4000, 3400)])
+def test_no_number_in_the_last_block(dev, dtype, packed, K, N, M):
+    # what stands behind the last block meets neither its infinities nor its scale for NaN
+    g = torch.Generator().manual_seed(K)
+    x, w = torch.randn(N, K, generator=g).to(dtype).to(dev), torch.randn(K, M, generator=g).to(dev)
+    clean = dense.mx4_linear(dense.mx4_quantise(x) if packed else x, dense.mx4_quantise(w, columns=True))
+    x[N - 2, K - 1] = math.inf
+    w[K - 1, M - 3] = math.nan
+    y = dense.mx4_linear(dense.mx4_quantise(x) if packed else x, dense.mx4_quantise(w, columns=True))
+    spoiled = torch.zeros(N, M, dtype=torch.bool, device=dev)
+    spoiled[N - 2] = spoiled[:, M - 3] = True
+    assert not y[spoiled].isfinite().any()
+    assert torch.equal(y[~spoiled], clean[~spoiled])
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_operands_off_their_alignment(dev, packed):
+    # scales that start on any byte and rows that start on any element have the same product
+    K, N, M = 512, 700, 900
+    W = matrix(8, K, M, dev)
+    x = torch.randn(N, K, generator=torch.Generator().manual_seed(8)).to(BF16).to(dev)
+    rows = dense.mx4_quantise(x) if packed else x
+
+    def moved(s):
+        return torch.empty(s.numel() + 5, dtype=torch.uint8, device=dev)[5:].view(s.shape).copy_(s)
+
+    at = torch.empty(N * (K + 2) + 1, dtype=BF16, device=dev)[1:].view(N, K + 2)[:, :K].copy_(x)
+    other = dense.Mx4(rows.codes, moved(rows.scales), K) if packed else at
+    want = ref.values4(rows.codes, rows.scales, K) if packed else wide(x)
+    wv = ref.values4(W.codes, W.scales, K)
+    bound = sums(K, want.abs() @ wv.abs().t())
+    for r, w in ((rows, W), (other, W), (rows, dense.Mx4(W.codes, moved(W.scales), K)), (other, dense.Mx4(W.codes, moved(W.scales), K))):
+        y = dense.mx4_linear(r, w, out_dtype=F32, dtype=BF16 if packed else None)
+        check(y, want @ wv.t(), bound, "y")
