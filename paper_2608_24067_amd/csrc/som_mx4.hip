@@ -6,9 +6,7 @@
 // with an infinity or a NaN gets s = 255, and all of it stands for NaN. Block b of a row holds
 // features 32 b to 32 b + 31, two to a byte, the first in the low half; past the last feature are zeros.
 //
-// Bound by the bytes read and written. Rows: four threads a block, eight values each. Feature-major
-// matrices: a thread takes one 16-byte vector of columns over a block's 32 features, 32 loads in
-// flight, and needs no exchange.
+// Bound by the bytes read and written. Rows: four threads a block, eight values each.
 
 #include "som_layer_device.h"
 
@@ -25,9 +23,6 @@ __device__ inline uint32_t scale_byte(uint32_t top)
     const uint32_t e = top >> 23;
     return e == 255 ? 255 : e > 2 ? e - 2 : 0;
 }
-
-// 2^(s - 127) as the conversions take it: 0 stands for 2^-127, a subnormal.
-__device__ inline float scale_value(uint32_t s) { return __uint_as_float(s ? s << 23 : 0x00400000u); }
 
 // Eight values over the scale as codes.
 __device__ inline uint32_t encode8(const float *v, float scale)
@@ -73,40 +68,63 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_quantise_row
     }
 }
 
-// A thread: V columns by one block of features.
-template <typename T> __device__ inline void quantise_columns(const FourArgs &a, int32_t row_blocks, int64_t col, int block)
+// Feature-major matrices: a workgroup takes 128 features by 64 columns through LDS, rows by 16-byte
+// vectors on the side of the matrix, one block of a column a thread on the side of the codes. 1003 x 5625
+// fp32 takes 9.0 us and 8.1 back (22.6 MB); a thread for eight columns' blocks, without LDS, took as
+// long there, but 12.6 us for a matrix in bf16 of any small size, its code being fetched (now 3.4).
+constexpr int kCols = 64, kFeatures = kThreads / 64 * kFourBlock;
+
+template <typename T> struct Vectors {
+    static constexpr int V = 16 / sizeof(T), kAcross = kCols / V, kStep = kThreads / kAcross, kTurns = kFeatures / kStep;
+};
+
+__host__ __device__ inline int64_t column_tiles(int64_t N, int64_t row_blocks)
 {
-    constexpr int V = 16 / sizeof(T);
-    const int n = (int)min((int64_t)V, a.N - col), k = block * kFourBlock, left = (int)min((int64_t)kFourBlock, a.K - k);
-    const T *x = static_cast<const T *>(a.x) + (int64_t)k * a.ldx + col;
-    typename VecOf<T, V>::type v[kFourBlock];
+    return (N + kCols - 1) / kCols * ((row_blocks + kFeatures / kFourBlock - 1) / (kFeatures / kFourBlock));
+}
+
+template <typename T> __global__ __launch_bounds__(kThreads) void k_quantise_columns(const FourArgs a, int32_t row_blocks)
+{
+    typedef Vectors<T> S;
+    typedef typename VecOf<T, S::V>::type vec;
+    __shared__ __align__(16) T tile[kFeatures][kCols];
+    const int64_t across = (a.N + kCols - 1) / kCols, total = column_tiles(a.N, row_blocks);
+    const int c = (int)threadIdx.x % 64, own = (int)threadIdx.x / 64, v = (int)threadIdx.x % S::kAcross * S::V, r0 = (int)threadIdx.x / S::kAcross;
+    for (int64_t i = blockIdx.x; i < total; i += gridDim.x) {
+        const int64_t col = i % across * kCols, k = i / across * kFeatures;
+        const T *x = static_cast<const T *>(a.x) + k * a.ldx + col;
+        const int rows = (int)min((int64_t)kFeatures, a.K - k), cols = (int)min((int64_t)kCols, a.N - col);
+        vec in[S::kTurns];
+        if (cols == kCols) {
 #pragma unroll
-    for (int i = 0; i < kFourBlock; ++i) {
-        if (i < left && n == V) {
-            v[i] = *reinterpret_cast<const typename VecOf<T, V>::any *>(x + i * a.ldx);
+            for (int t = 0; t < S::kTurns; ++t)
+                in[t] = *reinterpret_cast<const typename VecOf<T, S::V>::any *>(x + min(r0 + t * S::kStep, rows - 1) * a.ldx + v);
         } else {
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[i][j] = i < left && j < n ? x[i * a.ldx + j] : (T)0.0f;
+            for (int t = 0; t < S::kTurns; ++t)
+#pragma unroll
+                for (int j = 0; j < S::V; ++j) in[t][j] = x[min(r0 + t * S::kStep, rows - 1) * a.ldx + min(v + j, cols - 1)];
         }
-    }
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        if (j >= n) break;
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < kFourBlock; ++i) top = max(top, magnitude((float)v[i][j]));
-        const uint32_t s = scale_byte(top);
-        uint32_t c[4];
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            float f[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = (float)v[8 * h + i][j];
-            c[h] = encode8(f, scale_value(s));
+        for (int t = 0; t < S::kTurns; ++t) {
+            const int r = r0 + t * S::kStep;
+            *reinterpret_cast<vec *>(&tile[r][v]) = r < rows ? in[t] : vec(0);
         }
-        const int64_t at = (col + j) * row_blocks + block;
-        reinterpret_cast<uint4 *>(a.codes)[at] = uint4{c[0], c[1], c[2], c[3]};
-        a.scales[at] = (uint8_t)s;
+        __syncthreads();
+        const int64_t block = k / kFourBlock + own;
+        if (c < cols && block < row_blocks) {
+            float f[kFourBlock];
+            uint32_t top = 0, q[4];
+#pragma unroll
+            for (int e = 0; e < kFourBlock; ++e) f[e] = (float)tile[own * kFourBlock + e][c], top = max(top, magnitude(f[e]));
+            const uint32_t s = scale_byte(top);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) q[h] = encode8(f + 8 * h, scale_value(s));
+            const int64_t at = (col + c) * row_blocks + block;
+            reinterpret_cast<uint4 *>(a.codes)[at] = uint4{q[0], q[1], q[2], q[3]};
+            a.scales[at] = (uint8_t)s;
+        }
+        __syncthreads();
     }
 }
 
@@ -123,66 +141,50 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_values_rows(
 }
 
 template <typename T>
-__device__ inline void values_columns(const FourArgs &a, int32_t row_blocks, T *y, int64_t ldy, int64_t col, int block)
+__global__ __launch_bounds__(kThreads) void k_values_columns(const FourArgs a, int32_t row_blocks, T *y, int64_t ldy)
 {
-    constexpr int V = 16 / sizeof(T);
-    const int n = (int)min((int64_t)V, a.N - col), k = block * kFourBlock, left = (int)min((int64_t)kFourBlock, a.K - k);
-    uint4 c[V];
-    uint32_t s[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int64_t at = (min(col + j, a.N - 1)) * row_blocks + block;
-        c[j] = reinterpret_cast<const uint4 *>(a.codes)[at];
-        s[j] = a.scales[at];
-    }
-    T *out = y + (int64_t)k * ldy + col;
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        float v[V][8];
-#pragma unroll
-        for (int j = 0; j < V; ++j) decode8(h == 0 ? c[j].x : h == 1 ? c[j].y : h == 2 ? c[j].z : c[j].w, s[j], v[j]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (8 * h + i >= left) continue;
-            float r[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) r[j] = v[j][i];
-            store<V>(out + (int64_t)(8 * h + i) * ldy, n, r);
-        }
-    }
-}
-
-// A wave takes 16 vectors of columns by four blocks at a time; f(first column, block). Workgroups are single
-// waves, which spread over the CUs (1,003 x 5,625 fp32 is 704 of them).
-constexpr int kColumnBlocks = 4;
-
-template <int V, typename F> __device__ inline void over_columns(const FourArgs &a, int32_t row_blocks, F f)
-{
-    const int64_t across = (a.N + 16 * V - 1) / (16 * V), total = across * ((row_blocks + kColumnBlocks - 1) / kColumnBlocks);
+    typedef Vectors<T> S;
+    typedef typename VecOf<T, S::V>::type vec;
+    __shared__ __align__(16) T tile[kFeatures][kCols];
+    const int64_t across = (a.N + kCols - 1) / kCols, total = column_tiles(a.N, row_blocks);
+    const int c = (int)threadIdx.x % 64, own = (int)threadIdx.x / 64, v = (int)threadIdx.x % S::kAcross * S::V, r0 = (int)threadIdx.x / S::kAcross;
     for (int64_t i = blockIdx.x; i < total; i += gridDim.x) {
-        const int64_t col = (i % across * 16 + threadIdx.x % 16) * V;
-        const int block = (int)(i / across) * kColumnBlocks + (int)threadIdx.x / 16;
-        if (col < a.N && block < row_blocks) f(col, block);
+        const int64_t col = i % across * kCols, k = i / across * kFeatures;
+        const int rows = (int)min((int64_t)kFeatures, a.K - k), cols = (int)min((int64_t)kCols, a.N - col);
+        const int64_t at = (col + min(c, cols - 1)) * row_blocks + min(k / kFourBlock + own, (int64_t)row_blocks - 1);
+        const uint4 q = reinterpret_cast<const uint4 *>(a.codes)[at];
+        const uint32_t s = a.scales[at], words[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            float f[8];
+            decode8(words[h], s, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) tile[own * kFourBlock + 8 * h + e][c] = (T)f[e];
+        }
+        __syncthreads();
+        T *out = y + k * ldy + col;
+#pragma unroll
+        for (int t = 0; t < S::kTurns; ++t) {
+            const int r = r0 + t * S::kStep;
+            if (r >= rows) continue;
+            const vec w = *reinterpret_cast<const vec *>(&tile[r][v]);
+            if (cols == kCols) {
+                *reinterpret_cast<typename VecOf<T, S::V>::any *>(out + r * ldy + v) = w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < S::V; ++j)
+                    if (v + j < cols) out[r * ldy + v + j] = w[j];
+            }
+        }
+        __syncthreads();
     }
-}
-
-template <typename T> __global__ __launch_bounds__(64) void k_quantise_columns(const FourArgs a, int32_t row_blocks)
-{
-    over_columns<16 / sizeof(T)>(a, row_blocks, [&](int64_t col, int block) { quantise_columns<T>(a, row_blocks, col, block); });
-}
-
-template <typename T>
-__global__ __launch_bounds__(64) void k_values_columns(const FourArgs a, int32_t row_blocks, T *y, int64_t ldy)
-{
-    over_columns<16 / sizeof(T)>(a, row_blocks, [&](int64_t col, int block) { values_columns<T>(a, row_blocks, y, ldy, col, block); });
 }
 
 constexpr int64_t kGroups = 1 << 20;  // workgroups of a launch, which go on from there
 
-template <typename T> dim3 column_grid(const FourArgs &a, int64_t row_blocks)
+dim3 column_grid(const FourArgs &a, int64_t row_blocks)
 {
-    constexpr int V = 16 / sizeof(T);
-    const int64_t n = (a.N + 16 * V - 1) / (16 * V) * ((row_blocks + kColumnBlocks - 1) / kColumnBlocks);
+    const int64_t n = column_tiles(a.N, row_blocks);
     return dim3((unsigned)(n < kGroups ? n : kGroups));
 }
 
@@ -190,7 +192,7 @@ template <typename T> hipError_t quantise(bool columns, const FourArgs &a, hipSt
 {
     const int64_t row_blocks = four_blocks(a.K), blocks = a.N * row_blocks;
     if (columns) {
-        hipLaunchKernelGGL(k_quantise_columns<T>, column_grid<T>(a, row_blocks), dim3(64), 0, st, a, (int32_t)row_blocks);
+        hipLaunchKernelGGL(k_quantise_columns<T>, column_grid(a, row_blocks), dim3(kThreads), 0, st, a, (int32_t)row_blocks);
     } else {
         const int64_t n = (blocks + kThreads / 4 - 1) / (kThreads / 4);
         hipLaunchKernelGGL(k_quantise_rows<T>, dim3((unsigned)(n < kGroups ? n : kGroups)), dim3(kThreads), 0, st, a, blocks,
@@ -203,7 +205,7 @@ template <typename T> hipError_t values(bool columns, const FourArgs &a, void *y
 {
     const int64_t row_blocks = four_blocks(a.K), blocks = a.N * row_blocks;
     if (columns) {
-        hipLaunchKernelGGL(k_values_columns<T>, column_grid<T>(a, row_blocks), dim3(64), 0, st, a, (int32_t)row_blocks, static_cast<T *>(y), ldy);
+        hipLaunchKernelGGL(k_values_columns<T>, column_grid(a, row_blocks), dim3(kThreads), 0, st, a, (int32_t)row_blocks, static_cast<T *>(y), ldy);
     } else {
         const int64_t n = (blocks + kThreads / 4 - 1) / (kThreads / 4);
         hipLaunchKernelGGL(k_values_rows<T>, dim3((unsigned)(n < kGroups ? n : kGroups)), dim3(kThreads), 0, st, a, blocks,

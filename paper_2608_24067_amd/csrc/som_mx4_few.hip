@@ -12,8 +12,9 @@
 //     all scales, and the instruction's sums over one block are then added under the scale in fp32.
 // bf16 and 4 bits: the matrix is the instruction's first operand, so that a lane owns four neighbouring
 // columns of a row; fp16: the rows are, so that it owns one column, under one scale.
-// Bound by a CU's reads and, at the smallest sizes, by the launch: 1 x 1024 x 4096 takes 3.8 us (2.2 MB; an
-// empty launch 2.5), 1 x 4096 x 4096 5.7 (8.9 MB), 64 x 4096 x 4096 in bf16 14.7 with 32 x 32 a workgroup.
+// Bound by a CU's reads and, at the smallest sizes, by what a launch and the first loads take: 1 x 1024 x 4096
+// takes 3.8 us (2.2 MB), 1 x 4096 x 4096 6.0 (8.9 MB), 64 x 4096 x 4096 in bf16 14.8 with 32 x 32 a workgroup,
+// 33 x 2048 x 8192 11.4 with 32 x 64 (12.5 before the join took all threads and bias and residual came early).
 
 #include "som_layer_device.h"
 #include "som_mm.h"
@@ -49,7 +50,7 @@ template <typename T, bool PACKED, int RT, int CT> __global__ __launch_bounds__(
 {
     typedef Operands<T, PACKED, RT, CT> Unit;
     constexpr bool kColumn = !PACKED && __is_same(T, _Float16);
-    __shared__ f32x4 joined[kWaves][CT][64];
+    __shared__ f32x4 joined[kWaves][RT * CT][64];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int q = lane >> 4, i = lane & 15;
     const int64_t across = (p.M + CT * 16 - 1) / (CT * 16), b = mm::block_number();
@@ -149,6 +150,26 @@ template <typename T, bool PACKED, int RT, int CT> __global__ __launch_bounds__(
             }
         }
     };
+    // A thread's four results after the join: four columns of a row, or (kColumn) four rows of a column.
+    // Their bias and residual are loaded first, so that nothing waits for them at the end.
+    static_assert(RT * CT <= kWaves, "four results a thread");
+    const int64_t row = row0 + 16 * (wave / CT) + (kColumn ? q * 4 : i), col = col0 + 16 * (wave % CT) + (kColumn ? i : q * 4);
+    const int n = wave < RT * CT && row < p.N && col < p.M ? (int)min((int64_t)4, kColumn ? p.N - row : p.M - col) : 0;
+    float bias[4] = {0, 0, 0, 0}, res[4] = {0, 0, 0, 0};
+    if (p.bias && n > 0) {
+        if (p.bias_f32) mm::load4(static_cast<const float *>(p.bias) + col, kColumn ? 1 : n, bias);
+        else mm::load4(static_cast<const T *>(p.bias) + col, kColumn ? 1 : n, bias);
+    }
+    if (p.res && n > 0) {
+        const T *from = static_cast<const T *>(p.res) + row * p.ldr + col;
+        if constexpr (kColumn) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < n) res[k] = (float)from[k * p.ldr];
+        } else {
+            mm::load4(from, n, res);
+        }
+    }
     // A wave's units are kWaves apart; the last unit of all may be a part of one.
     const int whole = (int)(p.K / kUnit);
     Unit even, odd;
@@ -165,53 +186,37 @@ template <typename T, bool PACKED, int RT, int CT> __global__ __launch_bounds__(
         load(u, odd, mm::Inside<false>());
         multiply(odd);
     }
-    for (int r = 0; r < RT; ++r) {
-        if (r > 0) __syncthreads();  // the last sums have been read
 #pragma unroll
-        for (int at = 0; at < RT; ++at) {
-            if (at != r) continue;
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int c = 0; c < CT; ++c) joined[wave][c][lane] = acc[at][c];
+        for (int c = 0; c < CT; ++c) joined[wave][r * CT + c][lane] = acc[r][c];
+    __syncthreads();
+    if (n <= 0) return;
+    f32x4 s = joined[0][wave][lane];
+#pragma unroll
+    for (int k = 1; k < kWaves; ++k) s += joined[k][wave][lane];
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = s[k] + bias[kColumn ? 0 : k];
+    if (p.act != SOM_ACT_NONE) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = p.y_f32 ? mm::act_fine(p.act, v[k]) : mm::act_value(p.act, v[k]);
+    }
+    if (p.res) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] += res[k];
+    }
+    if constexpr (kColumn) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k >= n) continue;
+            if (p.y_f32) static_cast<float *>(p.y)[(row + k) * p.ldy + col] = v[k];
+            else static_cast<T *>(p.y)[(row + k) * p.ldy + col] = (T)v[k];
         }
-        __syncthreads();
-        const int o = threadIdx.x;  // CT x 64 threads: four results each
-        if (o >= CT * 64) continue;
-        const int c = o / 64, l = o % 64;
-        f32x4 s = joined[0][c][l];
-#pragma unroll
-        for (int k = 1; k < kWaves; ++k) s += joined[k][c][l];
-        // four columns of a row, or four rows of a column
-        const int64_t row = row0 + 16 * r + (kColumn ? l / 16 * 4 : l % 16), col = col0 + 16 * c + (kColumn ? l % 16 : l / 16 * 4);
-        const int n = (int)min((int64_t)4, kColumn ? p.N - row : p.M - col);
-        if (n <= 0 || row >= p.N || col >= p.M) continue;
-        float v[4] = {s[0], s[1], s[2], s[3]}, t[4] = {0, 0, 0, 0};
-        if (p.bias) {
-            if (p.bias_f32) mm::load4(static_cast<const float *>(p.bias) + col, kColumn ? 1 : n, t);
-            else mm::load4(static_cast<const T *>(p.bias) + col, kColumn ? 1 : n, t);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] += t[kColumn ? 0 : k];
-        }
-        if (p.act != SOM_ACT_NONE) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = p.y_f32 ? mm::act_fine(p.act, v[k]) : mm::act_value(p.act, v[k]);
-        }
-        if constexpr (kColumn) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (k >= n) continue;
-                if (p.res) v[k] += (float)static_cast<const T *>(p.res)[(row + k) * p.ldr + col];
-                if (p.y_f32) static_cast<float *>(p.y)[(row + k) * p.ldy + col] = v[k];
-                else static_cast<T *>(p.y)[(row + k) * p.ldy + col] = (T)v[k];
-            }
-        } else {
-            if (p.res) {
-                mm::load4(static_cast<const T *>(p.res) + row * p.ldr + col, n, t);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] += t[k];
-            }
-            if (p.y_f32) mm::store4(static_cast<float *>(p.y) + row * p.ldy + col, n, v);
-            else mm::store4(static_cast<T *>(p.y) + row * p.ldy + col, n, v);
-        }
+    } else if (p.y_f32) {
+        mm::store4(static_cast<float *>(p.y) + row * p.ldy + col, n, v);
+    } else {
+        mm::store4(static_cast<T *>(p.y) + row * p.ldy + col, n, v);
     }
 }
 

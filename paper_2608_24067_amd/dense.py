@@ -497,8 +497,10 @@ def _state_pointers(states, sizes, eight, at):
     if eight:
         blocks = [(n + STATE_BLOCK - 1) // STATE_BLOCK for n in sizes]
         scales = (_held_all(m_scales, "m_scales", kind, blocks, at), _held_all(v_scales, "v_scales", kind, blocks, at))
-    copies = none
-    if masters.count(None) < len(sizes):
+    copies, missing = none, sum([t is None for t in masters])  # not masters.count(None): a tensor compares slowly
+    if missing == 0:
+        copies = _held_all(masters, "master", torch.float32, sizes, at)
+    elif missing < len(sizes):
         copies = [0 if t is None else _held(t, "master", n, torch.float32, at) for t, n in zip(masters, sizes)]
     return (_held_all(ms, "m", kind, sizes, at), _held_all(vs, "v", kind, sizes, at), *scales, copies)
 
