@@ -131,9 +131,8 @@ int64_t four_tiles(int64_t N, int64_t M, int64_t rows, int64_t cols) { return (N
 // (1 x 1024 x 32768: 8.5, by 64 10.9). Rows in 4 bits go through LDS once 16 x 32 is too small (64 x
 // 4096 x 4096: 17.5, 13.9, 10.9 by the first three, 8.7 by 64; 1 x 1024 x 32768 7.3, 7.6, 8.2, 6.0).
 // Through LDS a tile is 64 while two a CU hold all (by 64, 128, 256 in bf16: 512 x 4096 x 4096 36, 42, 85;
-// 1024 x 4096 x 4096 51, 46, 85; in 4 bits 12.8, 14.6, 28.7 and 22.1, 17.8, 30.8), or six in fp16, whose
-// larger tiles take longest (1024 x 4096 x 4096 62, 73; 2048 x 1024 x 4096 37.8, 32.0), and 256 where
-// that fills three CUs in four (2048 x 2048 x 8192 104, 70, 60; 42.6, 31.9, 27.0; fp16 131, 105, 89).
+// 1024 x 4096 x 4096 51, 46, 85; in 4 bits 12.8, 14.6, 28.7 and 22.1, 17.8, 30.8; fp16 512 x 2048 x 4096 21,
+// 26, 56), and 256 where that fills three CUs in four (2048 x 2048 x 8192 104, 70, 60; 42.6, 31.9, 27.0).
 som::FourTile four_tile(int64_t N, int64_t K, int64_t M, bool packed, bool bf16)
 {
     if (K > kFourMostWidth) return N <= 16 ? som::kFour16x32 : som::kFour32x32;
@@ -142,7 +141,7 @@ som::FourTile four_tile(int64_t N, int64_t K, int64_t M, bool packed, bool bf16)
     if (!packed && four_tiles(N, M, 32, 32) <= 256) return som::kFour32x32;
     if (!packed && bf16 && four_tiles(N, M, 32, 64) <= 256) return som::kFour32x64;
     if (four_tiles(N, M, 256, 256) >= 192) return som::kFour256;
-    return four_tiles(N, M, 64, 64) <= (packed || bf16 ? 512 : 1536) ? som::kFour64 : som::kFour128;
+    return four_tiles(N, M, 64, 64) <= 512 ? som::kFour64 : som::kFour128;
 }
 
 bool few_rows(som::FourTile t) { return t <= som::kFour32x64; }

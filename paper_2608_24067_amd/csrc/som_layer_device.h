@@ -69,22 +69,27 @@ template <int LANES, typename T> __device__ inline T lane_sum(T v)
 // 2^(s - 127), a subnormal for 0 and NaN for 255; no branch, which a choice would become.
 __device__ inline float scale_value(uint32_t s) { return __uint_as_float(max(s << 23, 0x00400000u) | (s + 1) >> 8 << 22); }
 
-// Eight codes as 16-bit values, exactly: bf16 under the scale byte s, whose place in an fp32 value's exponent
-// is all that the conversion reads (255 makes NaN), fp16 without it, since fp16 does not hold all scales.
-template <typename T> __device__ inline T __attribute__((ext_vector_type(8))) widen8(uint32_t codes, uint32_t s)
+// Eight codes times a scale as 16-bit values. Of the scale the conversion reads the exponent's place alone
+// (0 stands for 2^-127, 255 makes NaN).
+template <typename T> __device__ inline T __attribute__((ext_vector_type(8))) widen8_by(uint32_t codes, float scale)
 {
     typedef T two __attribute__((ext_vector_type(2)));
     typedef T eight __attribute__((ext_vector_type(8)));
     two a, b, c, d;
     if constexpr (__is_same(T, __bf16)) {
-        const float scale = __uint_as_float(s << 23);
         a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
         c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
     } else {
-        a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 1);
-        c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 3);
+        a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3);
     }
     return eight{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The same, exactly: bf16 under the scale byte s, fp16 without it, since fp16 does not hold all scales.
+template <typename T> __device__ inline T __attribute__((ext_vector_type(8))) widen8(uint32_t codes, uint32_t s)
+{
+    return widen8_by<T>(codes, __is_same(T, __bf16) ? __uint_as_float(s << 23) : 1.0f);
 }
 
 }  // namespace layer

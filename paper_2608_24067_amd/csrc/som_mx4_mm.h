@@ -6,12 +6,13 @@
 //   Rows in 4 bits: a step takes 128 features by v_mfma_scale_f32_16x16x128_f8f6f4, which applies
 //     both blocks' scales: lane (q, i) holds block q of row i.
 //   Rows in 16 bits: a step takes 32 features, one block of each column, by v_mfma_f32_16x16x32. The
-//     codes come for eight steps at a time and are widened in registers, where a wave's rows share them:
-//     to bf16 under their scale, which is exact; to fp16 without it, since fp16 does not hold all
-//     scales, and the instruction's sums over the block are then added under the scale in fp32.
-// Measured, us and TFLOP/s: 8192 x 4096 x 4096 rows in 4 bits 77 and 3,560, in bf16 202 and 1,360, in fp16
-// 316 and 870. In 4 bits the fragments' reads of LDS bind (a line more a row than half of one gave 2 us), in
-// fp16 the four additions for each instruction.
+//     codes come for eight steps at a time and are widened in registers, where a wave's rows share them,
+//     under their scale, which is exact: to bf16, and to fp16 relative to the tile's largest scale. A tile
+//     whose scales fp16 does not span widens without them; the instruction's sums over a block are then
+//     added under the scale in fp32, four additions for each instruction.
+// Measured, us and TFLOP/s: 8192 x 4096 x 4096 rows in 4 bits 77 and 3,560, in bf16 200 and 1,370, in fp16 212
+// and 1,300 (316 and 870 without the scales). Of 8192 x 2048 x 4096 in 4 bits, 54 us, some 30 go to the
+// first loads and the results' stores, during which the matrix units wait: there is one workgroup a CU.
 //
 // Rows must be whole lines (the host copies others to the workspace). Rows and columns past the last
 // ones repeat it; codes past the last feature meet zeros, or scales that make them nothing.
@@ -380,14 +381,75 @@ template <typename T, class S> __global__ __launch_bounds__(S::NT, S::PER_CU * S
 // LDS: two tiles of x, 64 features each, two places for the codes of 256 and two for their scales.
 template <class S> struct Half {
     static constexpr int kA = S::BM * 128, kB = S::BN * 128, kCodes = 2 * kA, kScales = kCodes + 2 * kB, kPlace = S::BN * 8;
+    // what the waves tell each other (fp16)
+    static constexpr int kMarks = kScales + 2 * kPlace, kWaves = kMarks + S::NT / 64 * 8, kAll = kWaves + S::NT / 64 * 4;
     static constexpr int kEnd = S::WM * S::WN * 16 * (S::NI * 16 + 4) * 4;
-    static constexpr int kBytes = kScales + 2 * kPlace > kEnd ? kScales + 2 * kPlace : kEnd;
+    static constexpr int kBytes = kAll > kEnd ? kAll : kEnd;
+    static_assert(kEnd <= kMarks, "the marks are read after the tiles");
 };
+
+// fp16 holds the codes of a tile under their scales, each over a power that the tile shares, where the scales
+// span 2^26 at most: with the largest at 2^13 all are normal numbers, 6 x 2^13 and 2^-1 x 2^-13 and what is between.
+// Then the sums run in the matrix instruction, as in bf16. `top`: the tile's largest byte. Two bytes count for
+// nothing: 0, which blocks of zeros have (if others do, those below 2^-124, the answer is no), and 255, whose
+// columns are marked in LDS and become NaN at the end.
+template <class S> __device__ inline bool scales_fit(const FourProduct &p, const uint8_t *scale_row, int n0, char *lds, int &top)
+{
+    typedef uint16_t pair __attribute__((ext_vector_type(2)));
+    constexpr int kParts = S::NT / S::BN;  // threads of a column
+    const int64_t blocks = four_blocks(p.K);
+    pair high = {0, 0}, low = {0xFFFF, 0xFFFF};  // of the bytes + 1: 255 becomes 0 and 0 becomes 1
+    uint32_t others = 0, nans = 0;
+    for (int64_t at = (int)threadIdx.x / S::BN; at < p.w_pitch / 16; at += kParts) {
+        const uint4 piece = reinterpret_cast<const uint4 *>(scale_row)[at];
+        const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
+        uint32_t zeros = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const pair a = (__builtin_bit_cast(pair, w[i] & 0x00FF00FF) + (pair)1) & (pair)255, b = (__builtin_bit_cast(pair, w[i] >> 8 & 0x00FF00FF) + (pair)1) & (pair)255;
+            high = __builtin_elementwise_max(high, __builtin_elementwise_max(a, b));
+            low = __builtin_elementwise_min(low, __builtin_elementwise_min(a - (pair)2, b - (pair)2));  // 0 and 1 become the largest
+            zeros |= (w[i] - 0x01010101u) & ~w[i] & 0x80808080u;
+            nans |= (~w[i] - 0x01010101u) & w[i] & 0x80808080u;
+        }
+        if (zeros == 0) continue;
+        const uint4 *codes = reinterpret_cast<const uint4 *>(p.w) + min(n0 + (int)threadIdx.x % S::BN, (int)p.M - 1) * blocks;
+#pragma unroll 1
+        for (int64_t b = at * 16; b < min(at * 16 + 16, blocks); ++b) {
+            if (scale_row[b] != 0) continue;
+            const uint4 c = codes[b];
+            others |= (c.x | c.y | c.z | c.w) & 0x77777777u;
+        }
+    }
+    uint32_t h = others ? 255 : max((uint32_t)max(high[0], high[1]), 1u) - 1, l = min((uint32_t)min(low[0], low[1]), 254u) + 1;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) h = max(h, (uint32_t)__shfl_xor((int)h, d)), l = min(l, (uint32_t)__shfl_xor((int)l, d));
+    uint64_t *marks = reinterpret_cast<uint64_t *>(lds + Half<S>::kMarks);
+    uint32_t *waves = reinterpret_cast<uint32_t *>(lds + Half<S>::kWaves);
+    const uint64_t mark = __ballot(nans != 0);
+    if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = h | l << 8, marks[threadIdx.x / 64] = mark;
+    __syncthreads();
+    h = 0, l = 255;
+#pragma unroll
+    for (int k = 0; k < S::NT / 64; ++k) h = max(h, waves[k] & 255), l = min(l, waves[k] >> 8);
+    top = __builtin_amdgcn_readfirstlane((int)h);
+    return top < 255 && top <= __builtin_amdgcn_readfirstlane((int)l) + 26;
+}
+
+// Whether scales_fit marked a column of the tile.
+template <class S> __device__ inline bool marked(const char *lds, int column)
+{
+    const uint64_t *marks = reinterpret_cast<const uint64_t *>(lds + Half<S>::kMarks);
+    uint64_t m = 0;
+#pragma unroll
+    for (int k = 0; k < S::NT / S::BN; ++k) m |= marks[k * (S::BN / 64) + column / 64];
+    return m >> (column % 64) & 1;
+}
 
 template <typename T, class S> __global__ __launch_bounds__(S::NT, S::PER_CU * S::NT / 256) void k_mx4_half(const FourProduct p)
 {
     typedef Half<S> L;
-    constexpr bool kScaled = __is_same(T, __bf16);  // the widened codes hold their scale
+    constexpr bool kBf16 = __is_same(T, __bf16);
     typedef typename mm::Vec8<T>::type Frag;
     extern __shared__ __align__(1024) char lds[];
     int m0, n0;
@@ -405,9 +467,6 @@ template <typename T, class S> __global__ __launch_bounds__(S::NT, S::PER_CU * S
     const uint8_t *scale_row = p.w_scales + (int64_t)min(n0 + (int)threadIdx.x % S::BN, (int)p.M - 1) * p.w_pitch;
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 
-    f32x4 acc[S::MI][S::NI];
-    start<T, S::MI, S::NI, !kScaled>(p, acc, n0 + wn * S::NI * 16);
-
     // As in the product of 4-bit rows, with tiles of 64 features in two steps of 32, a block of each
     // column. The codes come for four tiles at a time: when the waves meet in the last of four, those of
     // the four before are no longer read, and the ones after the next four take their place.
@@ -422,22 +481,14 @@ template <typename T, class S> __global__ __launch_bounds__(S::NT, S::PER_CU * S
     const uint32_t va = base + (at_a + li) * 128, slot[2] = {(uint32_t)(q ^ line_xor(li)) << 4, (uint32_t)((4 + q) ^ line_xor(li)) << 4};
     const uint32_t vb = base + L::kCodes + (at_b + li) * 128 + 4 * q, vx = (uint32_t)line_xor(li) << 4;
     const uint32_t vs = base + L::kScales + (at_b + li) * 4;
-    auto start_a = [&](int P, int D) { return formed(va + slot[D] + P * L::kA); };
+    auto start_a = [&](int P, int D) { return formed(va + slot[D]) + P * L::kA; };
     auto read_a = [&](uint32_t at, int i) { return __builtin_bit_cast(Frag, lds_chunk(at + i * 2048)); };
     // Block B of the eight at a place (0 or 1): the scales of four blocks are a dword of a column.
     auto read_b = [&](uint32_t place, int B, Raw (&raw)[S::NI]) {
-        const uint32_t at = formed(place * L::kB + vb + (((uint32_t)B << 4) ^ vx));
-        const uint32_t s = formed(place * L::kPlace + vs + (B / 4 * S::BN * 4 + B % 4));
+        const uint32_t at = formed(place * L::kB + vb + (((uint32_t)B << 4) ^ formed(vx)));
+        const uint32_t s = formed(place * L::kPlace + vs) + (B / 4 * S::BN * 4 + B % 4);
 #pragma unroll
         for (int j = 0; j < S::NI; ++j) raw[j] = Raw{lds_word(at + j * 2048), lds_byte(s + j * 64)};
-    };
-    auto widen = [&](const Raw &r) { return Wide{widen8<T>(r.codes, r.scale), kScaled ? 0.0f : scale_value(r.scale)}; };
-    auto multiply = [&](const Wide &b, const Frag &a, f32x4 c) {
-        if constexpr (kScaled) return mm::mma(b.v, a, c);
-        const f32x4 s = mm::mma(a, b.v, f32x4{0, 0, 0, 0});
-#pragma unroll
-        for (int k = 0; k < 4; ++k) c[k] = fmaf(s[k], b.scale, c[k]);
-        return c;
     };
     constexpr int kA = LineLoader<S::BM, S::NT>::kPer, kB = LineLoader<S::BN, S::NT>::kPer;
     // Load c of the codes of four tiles: two of scales, the others of codes.
@@ -448,80 +499,139 @@ template <typename T, class S> __global__ __launch_bounds__(S::NT, S::PER_CU * S
         else
             lb.load(c - 2, four, base + L::kCodes + at * L::kB);
     };
+    auto load_first = [&] {
 #pragma unroll
-    for (int c = 0; c < kB + 2; ++c) load_codes(c, 0);
+        for (int t = 0; t < 2; ++t) {
 #pragma unroll
-    for (int c = 0; c < kA; ++c) la.load(c, 0, base);
+            for (int c = 0; c < kB + 2; ++c) load_codes(c, t);
 #pragma unroll
-    for (int c = 0; c < kB + 2; ++c) load_codes(c, 1);
-#pragma unroll
-    for (int c = 0; c < kA; ++c) la.load(c, 1, base + L::kA);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kA + kB + 2) : "memory");
-    constexpr int kWindow = S::MI < 4 ? S::MI / 2 : 4, kMeet = S::MI - kWindow;
-    Wide even[S::NI], odd[S::NI];
-    Frag a[kWindow];
-    Raw raw[S::NI];
-    read_b(0, 0, raw);
-#pragma unroll
-    for (int j = 0; j < S::NI; ++j) even[j] = widen(raw[j]);
-    uint32_t first = start_a(0, 0);
-#pragma unroll
-    for (int i = 0; i < kWindow; ++i) a[i] = read_a(first, i);
-    // Tile t, U: t % 4. No branch stands between its instructions: past one the compiler would move them.
-    auto tile = [&](int t, auto u) {
-        constexpr int U = decltype(u)::value, P = U % 2;
-        const uint32_t codes = (uint32_t)(t / 4 % 2), next = U == 3 ? 1 - codes : codes;
-        constexpr int kFrom = S::MI / 2, kWide = (S::NI + S::MI - kFrom - 1) / (S::MI - kFrom);
-        const uint32_t second = start_a(P, 1), following = start_a(1 - P, 0);
-#pragma unroll
-        for (int i = 0; i < S::MI; ++i) {
-            if (i == 0) read_b(codes, 2 * U + 1, raw);
-#pragma unroll
-            for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply(even[j], a[i % kWindow], acc[i][j]);
-            a[i % kWindow] = i < kMeet ? read_a(first, i + kWindow) : read_a(second, i - kMeet);
-            if (i >= kFrom) {
-#pragma unroll
-                for (int j = (i - kFrom) * kWide; j < (i - kFrom + 1) * kWide && j < S::NI; ++j) odd[j] = widen(raw[j]);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+            for (int c = 0; c < kA; ++c) la.load(c, t, base + t * L::kA);
         }
-        constexpr int kLoads = kA + (U == 3 ? kB + 2 : 0), kAfter = S::MI - kMeet, kOf = (kLoads + kAfter - 1) / kAfter;
-#pragma unroll
-        for (int i = 0; i < S::MI; ++i) {
-            if (i == 0) read_b(next, (2 * U + 2) % 8, raw);
-            if (i == kMeet) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-#pragma unroll
-            for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply(odd[j], a[i % kWindow], acc[i][j]);
-            a[i % kWindow] = i < kMeet ? read_a(second, i + kWindow) : read_a(following, i - kMeet);
-            if (i >= kFrom) {
-#pragma unroll
-                for (int j = (i - kFrom) * kWide; j < (i - kFrom + 1) * kWide && j < S::NI; ++j) even[j] = widen(raw[j]);
-            }
-            if (i >= kMeet) {
-#pragma unroll
-                for (int c = (i - kMeet) * kOf; c < (i - kMeet + 1) * kOf && c < kLoads; ++c) {
-                    if (c < kA) la.load(c, t + 2, base + P * L::kA);
-                    else load_codes(c - kA, t / 4 + 2);
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        first = following;
     };
-    int t = 0;
-    for (; t + 4 <= tiles; t += 4) {
-        tile(t, Number<0>());
-        tile(t + 1, Number<1>());
-        tile(t + 2, Number<2>());
-        tile(t + 3, Number<3>());
+    // The product of the tile; scaled: the widened codes hold their scale, in fp16 over 2^(top - 13 - 127).
+    auto run = [&](auto scaled, f32x4 (&acc)[S::MI][S::NI], int top) {
+        constexpr bool kScaled = decltype(scaled)::value;
+        const int over = (140 - top) * (1 << 23);
+        auto widen = [&](const Raw &r) {
+            if constexpr (kBf16) return Wide{widen8<T>(r.codes, r.scale), 0.0f};
+            // a block of zeros may end below 0 and is taken there
+            else if constexpr (kScaled) return Wide{layer::widen8_by<T>(r.codes, __int_as_float(max((int)(r.scale << 23) + over, 0))), 0.0f};
+            else return Wide{widen8<T>(r.codes, r.scale), scale_value(r.scale)};
+        };
+        auto multiply = [&](const Wide &b, const Frag &a, f32x4 c) {
+            if constexpr (kScaled) return mm::mma(b.v, a, c);
+            const f32x4 s = mm::mma(a, b.v, f32x4{0, 0, 0, 0});
+#pragma unroll
+            for (int k = 0; k < 4; ++k) c[k] = fmaf(s[k], b.scale, c[k]);
+            return c;
+        };
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kA + kB + 2) : "memory");
+        constexpr int kWindow = S::MI < 4 ? S::MI / 2 : 4, kMeet = S::MI - kWindow;
+        Wide even[S::NI], odd[S::NI];
+        Frag a[kWindow];
+        Raw raw[S::NI];
+        read_b(0, 0, raw);
+#pragma unroll
+        for (int j = 0; j < S::NI; ++j) even[j] = widen(raw[j]);
+        uint32_t first = start_a(0, 0);
+#pragma unroll
+        for (int i = 0; i < kWindow; ++i) a[i] = read_a(first, i);
+        // Tile t, U: t % 4. No branch stands between its instructions: past one the compiler would move them.
+        auto tile = [&](int t, auto u) {
+            constexpr int U = decltype(u)::value, P = U % 2;
+            const uint32_t codes = (uint32_t)(t / 4 % 2), next = U == 3 ? 1 - codes : codes;
+            constexpr int kFrom = S::MI / 2, kWide = (S::NI + S::MI - kFrom - 1) / (S::MI - kFrom);
+            const uint32_t second = start_a(P, 1), following = start_a(1 - P, 0);
+#pragma unroll
+            for (int i = 0; i < S::MI; ++i) {
+                if (i == 0) read_b(codes, 2 * U + 1, raw);
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply(even[j], a[i % kWindow], acc[i][j]);
+                a[i % kWindow] = i < kMeet ? read_a(first, i + kWindow) : read_a(second, i - kMeet);
+                if (i >= kFrom) {
+#pragma unroll
+                    for (int j = (i - kFrom) * kWide; j < (i - kFrom + 1) * kWide && j < S::NI; ++j) odd[j] = widen(raw[j]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            constexpr int kLoads = kA + (U == 3 ? kB + 2 : 0), kAfter = S::MI - kMeet, kOf = (kLoads + kAfter - 1) / kAfter;
+#pragma unroll
+            for (int i = 0; i < S::MI; ++i) {
+                if (i == 0) read_b(next, (2 * U + 2) % 8, raw);
+                if (i == kMeet) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) acc[i][j] = multiply(odd[j], a[i % kWindow], acc[i][j]);
+                a[i % kWindow] = i < kMeet ? read_a(second, i + kWindow) : read_a(following, i - kMeet);
+                if (i >= kFrom) {
+#pragma unroll
+                    for (int j = (i - kFrom) * kWide; j < (i - kFrom + 1) * kWide && j < S::NI; ++j) even[j] = widen(raw[j]);
+                }
+                if (i >= kMeet) {
+#pragma unroll
+                    for (int c = (i - kMeet) * kOf; c < (i - kMeet + 1) * kOf && c < kLoads; ++c) {
+                        if (c < kA) la.load(c, t + 2, base + P * L::kA);
+                        else load_codes(c - kA, t / 4 + 2);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            first = following;
+        };
+        int t = 0;
+        for (; t + 4 <= tiles; t += 4) {
+            tile(t, Number<0>());
+            tile(t + 1, Number<1>());
+            tile(t + 2, Number<2>());
+            tile(t + 3, Number<3>());
+        }
+        if (t < tiles) tile(t, Number<0>());
+        if (t + 1 < tiles) tile(t + 1, Number<1>());
+        if (t + 2 < tiles) tile(t + 2, Number<2>());
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // nothing lands in LDS after the workgroup left it
+        __syncthreads();  // the tiles are no longer read
+        if constexpr (!kBf16 && kScaled) {
+            const int col0 = n0 + (int)at_b + 4 * q;
+#pragma unroll
+            for (int j = 0; j < S::NI; ++j) {
+                float bias[4] = {0, 0, 0, 0};
+                const int cnt = min(4, (int)p.M - col0 - 16 * j);
+                if (p.bias && cnt > 0) {
+                    if (p.bias_f32) mm::load4(static_cast<const float *>(p.bias) + col0 + 16 * j, cnt, bias);
+                    else mm::load4(static_cast<const T *>(p.bias) + col0 + 16 * j, cnt, bias);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (marked<S>(lds, (int)at_b + 16 * j + 4 * q + k)) bias[k] = __builtin_nanf("");
+#pragma unroll
+                for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[i][j][k] = ldexpf(acc[i][j][k], top - 140) + bias[k];
+            }
+        }
+        finish<T, S::MI, S::NI, !kScaled>(p, acc, m0 + (int)at_a, n0 + (int)at_b,
+                                          reinterpret_cast<float *>(lds) + wave * (16 * (S::NI * 16 + 4)));
+    };
+    if constexpr (kBf16) {
+        f32x4 acc[S::MI][S::NI];
+        start<T, S::MI, S::NI, false>(p, acc, n0 + wn * S::NI * 16);
+        load_first();
+        run(Number<1>(), acc, 0);
+    } else {
+        load_first();
+        int top;
+        if (scales_fit<S>(p, scale_row, n0, lds, top)) {
+            f32x4 acc[S::MI][S::NI];
+#pragma unroll
+            for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+            run(Number<1>(), acc, top);
+        } else {
+            f32x4 acc[S::MI][S::NI];
+            start<T, S::MI, S::NI, true>(p, acc, n0 + wn * S::NI * 16);
+            run(Number<0>(), acc, 0);
+        }
     }
-    if (t < tiles) tile(t, Number<0>());
-    if (t + 1 < tiles) tile(t + 1, Number<1>());
-    if (t + 2 < tiles) tile(t + 2, Number<2>());
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // nothing lands in LDS after the workgroup left it
-    __syncthreads();  // the tiles are no longer read
-    finish<T, S::MI, S::NI, !kScaled>(p, acc, m0 + (int)at_a, n0 + (int)at_b,
-                                      reinterpret_cast<float *>(lds) + wave * (16 * (S::NI * 16 + 4)));
 }
 
 template <class S> int64_t tiles(const FourProduct &p) { return (p.N + S::BM - 1) / S::BM * ((p.M + S::BN - 1) / S::BN); }

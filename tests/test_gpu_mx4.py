@@ -282,3 +282,58 @@ def test_operands_off_their_alignment(dev, packed):
     for r, w in ((rows, W), (other, W), (rows, dense.Mx4(W.codes, moved(W.scales), K)), (other, dense.Mx4(W.codes, moved(W.scales), K))):
         y = dense.mx4_linear(r, w, out_dtype=F32, dtype=BF16 if packed else None)
         check(y, want @ wv.t(), bound, "y")
+
+
+def codes_and_scales(seed, K, M, lowest, highest, dev):
+    """A 4-bit matrix of random codes whose scale bytes are lowest ... highest, both among them, by column and block."""
+    g = torch.Generator().manual_seed(seed)
+    blocks = (K + 31) // 32
+    codes = torch.randint(0, 256, (M, blocks * 16), generator=g, dtype=torch.uint8)
+    if K % 32:
+        codes[:, blocks * 16 - (32 - K % 32) // 2:] = 0
+    scales = torch.randint(lowest, highest + 1, (M, blocks), generator=g).to(torch.uint8)
+    scales[::7, 0], scales[::5, -1] = lowest, highest
+    return codes, scales
+
+
+@pytest.mark.parametrize("N,M", [(300, 1500), (700, 2100), (4000, 3400)])
+@pytest.mark.parametrize("lowest,highest", [(120, 124), (100, 126), (100, 127), (60, 140), (1, 20), (190, 215), (215, 220)])
+def test_fp16_rows_and_any_range_of_scales(dev, N, M, lowest, highest):
+    # 2^26 and less within a tile, and more
+    K = 160
+    codes, scales = codes_and_scales(lowest + highest, K, M, lowest, highest, dev)
+    W = dense.Mx4(codes.to(dev), scales.to(dev), K)
+    g = torch.Generator().manual_seed(N)
+    x = (torch.randn(N, K, generator=g) * torch.exp2(torch.randint(-22, 6, (N, K), generator=g).float())).half()
+    b = torch.randn(M, generator=g)
+    wv = ref.values4(codes, scales, K)
+    size = wide(x).abs() @ wv.abs().t() + wide(b).abs()
+    y = dense.mx4_linear(x.to(dev), W, b.to(dev), out_dtype=F32)
+    check(y, wide(x) @ wv.t() + wide(b), sums(K + 4, size) + 2.0 ** -148, "y")
+
+
+@pytest.mark.parametrize("N,M", [(300, 1500), (4000, 3400)])
+@pytest.mark.parametrize("how", ["zeros", "smallest", "nan"])
+def test_fp16_rows_and_scales_of_no_size(dev, N, M, how):
+    # blocks of zeros have the scale 0, and so have blocks of the smallest values; 255 stands for NaN
+    K = 544
+    codes, scales = codes_and_scales(5, K, M, 128, 130, dev)
+    g = torch.Generator().manual_seed(N + 1)
+    some = torch.rand(scales.shape, generator=g) < 0.1
+    scales[some] = 0
+    if how != "smallest":
+        codes.view(M, -1, 16)[some] = 0
+    if how == "nan":
+        scales[7, 3] = 255
+    x = torch.randn(N, K, generator=g).half()
+    if how == "smallest":
+        x[5] = 0
+        x.view(N, -1, 32)[5, some[9]] = 1.0  # nothing but the smallest of column 9
+    W = dense.Mx4(codes.to(dev), scales.to(dev), K)
+    y = dense.mx4_linear(x.to(dev), W, out_dtype=F32)
+    wv = ref.values4(codes, scales, K)
+    if how == "nan":
+        assert y[:, 7].isnan().all()
+        wv[7], y[:, 7] = 0, 0
+    size = wide(x).abs() @ wv.abs().t()
+    check(y, wide(x) @ wv.t(), sums(K, size) + 2.0 ** -148, "y")
