@@ -73,11 +73,11 @@ som_status steps_ok(const char *who, const som_adamw_tensor *t, int64_t count, b
 }
 
 // Tables of the tensors, as many as a launch takes at a time; f(table).
-template <typename F> hipError_t over_tables(const som_adamw_tensor *tensors, int64_t count, F f)
+template <typename F> hipError_t over_tables(const som_adamw_tensor *tensors, int64_t count, bool step8, F f)
 {
     int64_t total = 0;
     for (int64_t i = 0; i < count; ++i) total += tensors[i].size;
-    const int64_t chunk = som::adamw_chunk(total);
+    const int64_t chunk = som::adamw_chunk(total, step8);
     for (int64_t i = 0; i < count;) {
         som::AdamwTable t;
         t.count = 0;
@@ -87,7 +87,7 @@ template <typename F> hipError_t over_tables(const som_adamw_tensor *tensors, in
         for (; i < count && t.count < som::kAdamwTensors; ++i) {
             const som_adamw_tensor &x = tensors[i];
             const int64_t chunks = (x.size + chunk - 1) / chunk;
-            // a launch has fewer than 2^32 threads, and 2^38 elements (a tensor's most) 2^23 chunks
+            // a launch has fewer than 2^32 threads; a tensor has 2^22 chunks at most
             if (t.count > 0 && t.first[t.count] + chunks > (1 << 23)) break;
             const int j = t.count++;
             t.param[j] = x.param, t.grad[j] = x.grad, t.m[j] = x.m, t.v[j] = x.v;
@@ -252,7 +252,7 @@ som_status som_adamw(const som_adamw_tensor *tensors, int64_t count, const som_a
     a.rates.eps = (float)c.eps, a.rates.grad = (float)c.grad_scale;
     a.seed = c.seed, a.lr_at = c.lr_at, a.step_at = c.step_at, a.norm = c.norm;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return done(over_tables(tensors, count, [&](som::AdamwTable &t, int64_t) { return som::launch_adamw(t, bits8, a, s); }), who);
+    return done(over_tables(tensors, count, bits8, [&](som::AdamwTable &t, int64_t) { return som::launch_adamw(t, bits8, a, s); }), who);
 }
 
 som_status som_adamw_values(const som_adamw_tensor *tensors, int64_t count, float *const *m_out, float *const *v_out,
@@ -274,7 +274,7 @@ som_status som_adamw_values(const som_adamw_tensor *tensors, int64_t count, floa
         }
         return som::launch_adamw_values(t, s);
     };
-    return done(over_tables(tensors, count, launch), who);
+    return done(over_tables(tensors, count, false, launch), who);
 }
 
 static const char *mx4_arguments(int32_t type, const void *x, int64_t ldx, int32_t columns, const void *codes,
