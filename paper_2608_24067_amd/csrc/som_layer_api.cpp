@@ -193,7 +193,7 @@ som_status som_layer_norm(int32_t type, const void *X, int64_t ldx, const void *
 size_t som_layer_norm_bwd_workspace_bytes(int64_t N, int64_t D)
 {
     if (!rows_ok(N) || !width_ok(D)) return 0;
-    return align256((size_t)som::norm_parts(N) * 2 * (size_t)D * 4) + align256((size_t)N * 8);
+    return align256((size_t)som::norm_parts(N, false) * 2 * (size_t)D * 4) + align256((size_t)N * 8);
 }
 
 som_status som_layer_norm_bwd(int32_t type, const void *X, int64_t ldx, const void *weight, int32_t weight_type,
@@ -217,7 +217,7 @@ som_status som_layer_norm_bwd(int32_t type, const void *X, int64_t ldx, const vo
     a.x = X, a.ldx = ldx, a.weight = weight, a.weights_f32 = weight_type == SOM_F32;
     a.y = const_cast<void *>(dY), a.ldy = lddy, a.stats = const_cast<double *>(stats), a.N = N, a.D = (int32_t)D;
     a.add = add, a.lda = ldadd, a.dx = dX, a.lddx = lddx;
-    a.n_parts = som::norm_parts(N);
+    a.n_parts = som::norm_parts(N, D * size_of(type) > 1024 * 16);  // rows of more than 1,024 vectors
     a.part_rows = (N + a.n_parts - 1) / a.n_parts;
     a.parts = sums ? static_cast<float *>(workspace) : nullptr;
     a.means = reinterpret_cast<float *>(static_cast<char *>(workspace) + align256((size_t)a.n_parts * 2 * (size_t)D * 4));

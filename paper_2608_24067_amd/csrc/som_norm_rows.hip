@@ -7,14 +7,16 @@ namespace {
 
 using namespace layer;
 
-// Workgroups a launch has at most: enough for every CU to hold what it can of them, so that a
-// workgroup reads the weights once for all its rows.
-constexpr int64_t kGroups = 2048;
+// Workgroups a launch has at most: as many as the CUs hold at once, so that each reads the weights once for
+// all its rows and the rows in flight are neighbours (us with 256, 1024 and 2048 of them: 4000 x 8192 and
+// 2000 x 16384 fp32, a row by 1024 threads, 48, 57, 62 and 39, 50, 51; 20011 x 1003 fp32, four vectors a
+// thread, 37, 25.8, 28.1; 8192 x 4096 bf16, two, 1024 29.9, 2048 29.7).
+template <class S> constexpr int64_t kGroups = S::NT == 1024 ? 256 : S::C == 4 ? 1024 : 2048;
 
 template <class S> hipError_t rows(const NormArgs &a, hipStream_t st)
 {
     const int64_t all = (a.N + S::ROWS - 1) / S::ROWS;
-    const dim3 grid((unsigned)(all < kGroups ? all : kGroups));
+    const dim3 grid((unsigned)(all < kGroups<S> ? all : kGroups<S>));
     if (a.D % S::V == 0) hipLaunchKernelGGL((k_norm_rows<S, true>), grid, dim3(S::NT), 0, st, a);
     else hipLaunchKernelGGL((k_norm_rows<S, false>), grid, dim3(S::NT), 0, st, a);
     return hipGetLastError();
@@ -34,7 +36,7 @@ template <typename X, typename Y> hipError_t by_width(const NormArgs &a, hipStre
     if (vectors <= 1024) return rows<NormShape<X, Y, 256, 4, 256>>(a, st);
     if (vectors <= 2048) return rows<NormShape<X, Y, 1024, 2, 1024>>(a, st);
     if (vectors <= 4096) return rows<NormShape<X, Y, 1024, 4, 1024>>(a, st);
-    hipLaunchKernelGGL((k_norm_long<X, Y>), dim3((unsigned)(a.N < kGroups ? a.N : kGroups)), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((k_norm_long<X, Y>), dim3((unsigned)(a.N < 2048 ? a.N : 2048)), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 
