@@ -285,7 +285,7 @@ som_status som_adamw_values(const som_adamw_tensor *tensors, int64_t count, floa
  * block's largest magnitude, less 2, plus 127, at least 0; values are rounded to the nearest, ties to the even code,
  * and those above 6 to 6. A block with an infinity or a NaN gets 255. som_mx4_values writes what codes and scales
  * stand for, rounded to `type`, to Y, laid out as X. Scales of 253 and 254 are not made here; magnitudes beyond
- * fp32 count as infinite.
+ * fp32 are infinite in values, and in products where they do not fit.
  * 0 <= n < 2^30, 1 <= K < 2^30.
  */
 som_status som_mx4_quantise(int32_t type, const void *X, int64_t ldx, int32_t columns, uint8_t *codes, uint8_t *scales,

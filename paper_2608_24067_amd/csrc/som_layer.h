@@ -31,10 +31,10 @@ struct NormArgs {
     float *means;               // [N][2], of rows too long for registers
 };
 
-// Workgroups of the gradient, one part each: as many as the CUs hold at once, two a CU from 3,584 rows on
-// or one of more than 1,024 vectors (3000 x 16384 bf16: 78 us, with two 95), fewer for fewer rows (their
-// parts cost as much as eight rows each), and so many that a part's fp32 sums run over 256 rows at
-// most before they are joined.
+// Workgroups of the gradient, one part each: from 3,584 rows on as many as the CUs hold at once, two a CU or,
+// where rows have more than 1,024 vectors, one (3000 x 16384 bf16: 78 us, with two 95); fewer for fewer
+// rows (their parts cost as much as eight rows each), and so many that a part's fp32 sums run over 256
+// rows at most before they are joined.
 inline int64_t norm_parts(int64_t N, bool wide)
 {
     int64_t n = 64 + N / 8;

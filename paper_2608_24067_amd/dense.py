@@ -410,7 +410,7 @@ def layer_norm_bwd(x, dy, stats, weight=None, add=None, out=None, weight_dtype=N
     if wdt not in (torch.float32, dy.dtype):
         raise TypeError(f"weight, dweight and dbias must be float32 or {dy.dtype} (got {wdt})")
     lib = load()
-    ws = _work(workspace, lib.som_layer_norm_bwd_workspace_bytes(N, D), dev)
+    ws = _work(workspace, lib.som_layer_norm_bwd_workspace_bytes(N, D) if workspace is None else 0, dev)
     xp, ldx = _mat(x, "x", (N, D), x.dtype, dev)
     gp, ldg = _mat(dy, "dy", (N, D), dy.dtype, dev)
     ap, lda = _mat(add, "add", (N, D), x.dtype, dev) if add is not None else (None, 0)
@@ -667,7 +667,7 @@ def mx4_linear(x, W: Mx4, bias=None, residual=None, act: str = "none", out=None,
     bp = _vec(bias, "bias", (M,), (torch.float32, dtype), dev) if bias is not None else None
     rp, ldr = _mat(residual, "residual", (N, M), dtype, dev) if residual is not None else (None, 0)
     lib = load()
-    work = _work(workspace, lib.som_mx4_linear_workspace_bytes(N, K, M, 1 if packed else 0), dev)
+    work = _work(workspace, lib.som_mx4_linear_workspace_bytes(N, K, M, 1 if packed else 0) if workspace is None else 0, dev)
     _check(_on(dev, lib.som_mx4_linear, _TYPES[dtype], xp, ldx, xs, wp, ws, bp,
                _TYPES[bias.dtype] if bias is not None else F32, _named(_ACTS, act, "act"), rp, ldr, yp, ldy,
                _TYPES[out.dtype], N, K, M, *_pointer(work), _stream(at)), "som_mx4_linear")

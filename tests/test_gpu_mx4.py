@@ -229,7 +229,7 @@ def test_residual_in_place_and_no_rows(dev):
 
 # Every tile, and its edges: sizes on both sides of the rules' bounds.
 TILES = [(16, 70, 4096), (16, 70, 4100), (16, 70, 8192), (16, 70, 8200), (33, 200, 3000), (128, 100, 1025), (60, 96, 5000),
-         (31, 64, 16000), (300, 320, 2000), (1000, 33, 2000), (1500, 577, 2000), (2500, 96, 5000), (3300, 513, 3700)]
+         (31, 64, 16000), (20000, 70, 10), (9000, 200, 130), (40, 100, 33000), (300, 320, 2000), (1000, 33, 2000), (1500, 577, 2000), (2500, 96, 5000), (3300, 513, 3700)]
 
 
 @pytest.mark.parametrize("packed", [False, True])
@@ -337,3 +337,17 @@ def test_fp16_rows_and_scales_of_no_size(dev, N, M, how):
         wv[7], y[:, 7] = 0, 0
     size = wide(x).abs() @ wv.abs().t()
     check(y, wide(x) @ wv.t(), sums(K, size) + 2.0 ** -148, "y")
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("N,K,M", [(40, 256, 300), (700, 320, 900), (1500, 577, 2000), (3300, 512, 3700)])
+def test_residual_is_the_result(dev, dtype, packed, N, K, M):
+    W = matrix(N, K, M, dev)
+    g = torch.Generator().manual_seed(M)
+    x, r = torch.randn(N, K, generator=g).to(dtype).to(dev), torch.randn(N, M + 2, generator=g).to(dtype).to(dev)
+    rows = dense.mx4_quantise(x) if packed else x
+    want = dense.mx4_linear(rows, W, residual=r[:, 1:M + 1], act="silu")
+    sides = r[:, 0].clone(), r[:, M + 1].clone()
+    dense.mx4_linear(rows, W, residual=r[:, 1:M + 1], act="silu", out=r[:, 1:M + 1])
+    assert torch.equal(r[:, 1:M + 1], want) and torch.equal(r[:, 0], sides[0]) and torch.equal(r[:, M + 1], sides[1])
