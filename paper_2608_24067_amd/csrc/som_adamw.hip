@@ -6,7 +6,7 @@
 // One launch takes the chunks of up to 44 tensors; a thread's four or eight elements are loaded in
 // vectors. Bound by the bytes it moves: 28 an element in fp32 (168 million elements: 865 us, 5.5 TB/s), 10
 // of a 16-bit parameter with 8-bit states (350 us, 4.8 TB/s), whose arithmetic, some 65 instructions an
-// element, takes nearly as long.
+// element, takes nearly as long. A block's bytes are loaded before its codes: asked for after them, their wait came on top.
 //
 // 8-bit states. A block of 256 values shares a power of two 2^e, the least at which its largest
 // value is at most 1.875, held as e + 127 in a byte (255: the block held an infinity or NaN, and all
@@ -30,12 +30,16 @@ constexpr int kThreads = 256;
 
 // The bits of h spread over all of them: shifts, and multiplications by the fractional parts of the
 // square roots of 3 and 2.
-__device__ inline uint32_t mix(uint32_t h)
+__device__ inline uint32_t mix_product(uint32_t h)  // all but the last step
 {
     h ^= h >> 16;
     h *= 0xBB67AE85u;
     h ^= h >> 15;
-    h *= 0x6A09E667u;
+    return h * 0x6A09E667u;
+}
+__device__ inline uint32_t mix(uint32_t h)
+{
+    h = mix_product(h);
     return h ^ h >> 16;
 }
 
@@ -106,14 +110,13 @@ __device__ inline uint32_t block_scale(uint32_t bits)
     return f < 27 ? 0 : min(f, 255u);
 }
 
-// The code of x by 16 random bits, `random` in their place above the four that are dropped; `some`: the
-// block's byte is not 0. A block of NaN gets codes of no meaning.
-template <bool SIGNED> __device__ inline uint32_t encode(float x, int s, bool some, uint32_t random)
+// The code of x by 16 random bits, which are added above the four that are dropped. Codes of a block whose
+// byte is 0 are cleared afterwards; a block of NaN gets codes of no meaning.
+template <bool SIGNED> __device__ inline uint32_t encode(float x, int s, uint32_t random)
 {
-    const uint32_t c = (__float_as_uint(ldexpf(fabsf(x), (SIGNED ? 15 : 31) - s)) + random) >> 20;
-    if (SIGNED) return min(c, some ? 127u : 0u) | (x < 0.0f && some ? 128u : 0u);
-    const uint32_t least = x > 0.0f && some ? 1u : 0u;  // and 0 for 0, whose bits the random ones do not carry
-    return min(max(c, least), some ? 255u : 0u);
+    const uint32_t c = (__float_as_uint(ldexpf(fabsf(x), (SIGNED ? 15 : 31) - s)) + (random << 4)) >> 20;
+    if (SIGNED) return min(c, 127u) | (x < 0.0f ? 128u : 0u);
+    return min(max(c, x > 0.0f ? 1u : 0u), 255u);  // and 0 for 0, whose bits the random ones do not carry
 }
 
 // The largest over the 32 lanes of a block's half wave.
@@ -197,18 +200,19 @@ template <bool BITS8> __global__ __launch_bounds__(kThreads) void k_adamw(const 
         constexpr int V = 8;
         uint8_t *mc = static_cast<uint8_t *>(t.m[i]), *vc = static_cast<uint8_t *>(t.v[i]);
         const uint32_t key = mix(a.seed + r.step * 0x9E3779B1u + (uint32_t)(t.number + i) * 0x1F83D9ABu);
-        // Whole blocks of 32 threads take part: past the end they hold zeros.
+        uint8_t *m_scales = t.m_scales[i], *v_scales = t.v_scales[i];
+        // Whole blocks of 32 threads take part: past the end they hold zeros (NaN in a block of NaN).
         for (int64_t at = from + V * (int64_t)threadIdx.x; at < from + t.chunk; at += V * kThreads) {
             const int64_t block = at / kStateBlock;
             if (block * kStateBlock >= to) break;
             const int n = (int)max((int64_t)0, min((int64_t)V, to - at));
             float p[V], g[V], m[V], v[V];
             uint32_t cm[V / 4], cv[V / 4];
+            const uint32_t old_m = m_scales[block], old_v = v_scales[block];
             load_any<V>(read, read_type, at, n, p);
             load_any<V>(t.grad[i], grad_type, at, n, g);
             load_codes<V>(mc + at, n, cm);
             load_codes<V>(vc + at, n, cv);
-            const uint32_t old_m = t.m_scales[i][block], old_v = t.v_scales[i][block];
             const float by1 = block_factor(old_m, r.b1), by2 = block_factor(old_v, r.b2);
             uint32_t top_m = 0, top_v = 0;
 #pragma unroll
@@ -216,11 +220,6 @@ template <bool BITS8> __global__ __launch_bounds__(kThreads) void k_adamw(const 
 #pragma unroll
             for (int q = 0; q < V; ++q) {
                 r.apply(p[q], g[q], m[q], v[q], by1, by2);
-            }
-            if (n < V) {  // past the end, also in a block of NaN
-#pragma unroll
-                for (int q = 0; q < V; ++q)
-                    if (q >= n) m[q] = v[q] = 0.0f;
             }
 #pragma unroll
             for (int q = 0; q < V; ++q) {
@@ -233,13 +232,15 @@ template <bool BITS8> __global__ __launch_bounds__(kThreads) void k_adamw(const 
             for (int h = 0; h < V / 4; ++h) cm[h] = cv[h] = 0;
 #pragma unroll
             for (int q = 0; q < V; ++q) {  // a thread's eight numbers share their upper half
-                const uint32_t random = mix(first + (uint32_t)q * 0x9E3779B1u);
-                cm[q / 4] |= encode<true>(m[q], (int)new_m, new_m != 0, (random & 0xFFFF) << 4) << (8 * (q % 4));
-                cv[q / 4] |= encode<false>(v[q], (int)new_v, new_v != 0, random >> 16 << 4) << (8 * (q % 4));
+                const uint32_t h = mix_product(first + (uint32_t)q * 0x9E3779B1u);
+                cm[q / 4] |= encode<true>(m[q], (int)new_m, (h & 0xFFFF) ^ h >> 16) << (8 * (q % 4));
+                cv[q / 4] |= encode<false>(v[q], (int)new_v, h >> 16) << (8 * (q % 4));
             }
+#pragma unroll
+            for (int h = 0; h < V / 4; ++h) cm[h] = new_m ? cm[h] : 0, cv[h] = new_v ? cv[h] : 0;
             store_codes<V>(mc + at, n, cm);
             store_codes<V>(vc + at, n, cv);
-            if (threadIdx.x % 32 == 0) t.m_scales[i][block] = (uint8_t)new_m, t.v_scales[i][block] = (uint8_t)new_v;
+            if (threadIdx.x % 32 == 0) m_scales[block] = (uint8_t)new_m, v_scales[block] = (uint8_t)new_v;
             if (master) store<V>(master + at, n, p);
             store_any<V>(t.param[i], type, at, n, p);
         }
