@@ -151,7 +151,7 @@ struct FourProduct {
 };
 
 // The tile of a workgroup; the first four are those of the kernel for few rows.
-enum FourTile { kFour16x16, kFour16x32, kFour32x32, kFour32x64, kFour64, kFour128, kFour256 };
+enum FourTile { kFour16x16, kFour16x32, kFour32x32, kFour32x64, kFour64, kFour128, kFour192x256, kFour256 };
 hipError_t launch_mx4_few(bool bf16, FourTile t, const FourProduct &p, hipStream_t st);
 
 // The same for many rows. Rows in 16 bits must be whole lines of 128 bytes (four_width), rows of scales

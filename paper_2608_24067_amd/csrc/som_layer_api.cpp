@@ -133,6 +133,8 @@ int64_t four_tiles(int64_t N, int64_t M, int64_t rows, int64_t cols) { return (N
 // Through LDS a tile is 64 while two a CU hold all (by 64, 128, 256 in bf16: 512 x 4096 x 4096 36, 42, 85;
 // 1024 x 4096 x 4096 51, 46, 85; in 4 bits 12.8, 14.6, 28.7 and 22.1, 17.8, 30.8; fp16 512 x 2048 x 4096 21,
 // 26, 56), and 256 where that fills three CUs in four (2048 x 2048 x 8192 104, 70, 60; 42.6, 31.9, 27.0),
+// or 192 x 256 where that needs no more rounds of the CUs and fills them better (2011 x 1024 x 5625 by
+// 128, 192, 256 36.9, 33.9, 37.5; 6000 x 1024 x 4096 56, 53, 59; 12000 x 1024 x 1024 32.7, 27.7, 30.7),
 // unless a larger tile is too much padding (bf16 60000 x 1024 x 64 23, 24, 30; 100000 x 512 x 130 41, 48, 50;
 // 100000 x 512 x 300 66, 62, 83; 130 x 1024 x 32768 25, 21, 29).
 som::FourTile four_tile(int64_t N, int64_t K, int64_t M, bool packed, bool bf16)
@@ -143,6 +145,8 @@ som::FourTile four_tile(int64_t N, int64_t K, int64_t M, bool packed, bool bf16)
     if (!packed && four_tiles(N, M, 32, 32) <= 256) return som::kFour32x32;
     if (!packed && bf16 && four_tiles(N, M, 32, 64) <= 256) return som::kFour32x64;
     const int64_t by64 = four_tiles(N, M, 64, 64), by128 = four_tiles(N, M, 128, 128), by256 = four_tiles(N, M, 256, 256);
+    const int64_t by192 = four_tiles(N, M, 192, 256), rounds = (by256 + 255) / 256;
+    if (by192 <= rounds * 256 && by192 >= rounds * 218 && by192 * 3 <= by128 + by128 / 8) return som::kFour192x256;
     if (by256 >= 192 && by256 * 4 <= by128 + by128 / 8) return som::kFour256;
     return by64 <= 512 || by128 * 3 > by64 ? som::kFour64 : som::kFour128;
 }

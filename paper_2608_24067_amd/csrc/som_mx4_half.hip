@@ -22,6 +22,7 @@ template <typename T> hipError_t by_tile(FourTile t, const FourProduct &p, hipSt
 {
     if (t == kFour64) return launch<T, Tile<64, 64, 2, 2, 2>>(p, st);
     if (t == kFour128) return launch<T, Tile<128, 128, 2, 2, 2>>(p, st);
+    if (t == kFour192x256) return launch<T, Tile<192, 256, 2, 4, 1>>(p, st);
     return launch<T, Tile<256, 256, 2, 4, 1>>(p, st);
 }
 

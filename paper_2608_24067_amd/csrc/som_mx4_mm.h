@@ -37,6 +37,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 template <int BM_, int BN_, int WM_, int WN_, int PER_CU_> struct Tile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, PER_CU = PER_CU_, NT = 64 * WM_ * WN_;
     static constexpr int MI = BM_ / WM_ / 16, NI = BN_ / WN_ / 16;
+    static constexpr int WINDOW = MI % 4 || MI < 4 ? MI / 2 : 4;  // fragments of A in registers; they divide MI
 };
 
 // BYTES-byte pieces (16 or 4) of a row's scales, one row a thread, straight to LDS.
@@ -273,8 +274,8 @@ template <typename T, class S> __global__ __launch_bounds__(S::NT, S::PER_CU * S
     lb.init(p.w, bytes, n0, (int)p.M, bytes);
     // A thread's row of scales: BM of x, then BN of w; later waves repeat the earlier ones' loads.
     constexpr int kRows = S::BM + S::BN;
-    static_assert(S::NT % kRows == 0, "whole rows");
-    const int sr = (int)threadIdx.x % kRows;
+    static_assert(kRows % 64 == 0 && S::NT >= kRows, "whole waves");
+    const int sr = wave % (kRows / 64) * 64 + lane;
     const uint8_t *scale_row = sr < S::BM ? p.x_scales + (int64_t)min(m0 + sr, (int)p.N - 1) * p.x_pitch
                                           : p.w_scales + (int64_t)min(n0 + sr - S::BM, (int)p.M - 1) * p.w_pitch;
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
@@ -324,7 +325,7 @@ template <typename T, class S> __global__ __launch_bounds__(S::NT, S::PER_CU * S
 #pragma unroll
         for (int c = 0; c < kLoads; ++c) load(c, t, t);
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads) : "memory");
-    constexpr int kWindow = S::MI < 4 ? S::MI / 2 : 4, kMeet = S::MI - kWindow;
+    constexpr int kWindow = S::WINDOW, kMeet = S::MI - kWindow;
     Fragment even[S::NI], odd[S::NI], a[kWindow];
     Start first = starts(0, 0, 0);
 #pragma unroll
@@ -526,7 +527,7 @@ template <typename T, class S> __global__ __launch_bounds__(S::NT, S::PER_CU * S
             return c;
         };
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kA + kB + 2) : "memory");
-        constexpr int kWindow = S::MI < 4 ? S::MI / 2 : 4, kMeet = S::MI - kWindow;
+        constexpr int kWindow = S::WINDOW, kMeet = S::MI - kWindow;
         Wide even[S::NI], odd[S::NI];
         Frag a[kWindow];
         Raw raw[S::NI];

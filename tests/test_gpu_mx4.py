@@ -229,7 +229,7 @@ def test_residual_in_place_and_no_rows(dev):
 
 # Every tile, and its edges: sizes on both sides of the rules' bounds.
 TILES = [(16, 70, 4096), (16, 70, 4100), (16, 70, 8192), (16, 70, 8200), (33, 200, 3000), (128, 100, 1025), (60, 96, 5000),
-         (31, 64, 16000), (20000, 70, 10), (9000, 200, 130), (40, 100, 33000), (300, 320, 2000), (1000, 33, 2000), (1500, 577, 2000), (2500, 96, 5000), (3300, 513, 3700)]
+         (31, 64, 16000), (20000, 70, 10), (9000, 200, 130), (40, 100, 33000), (300, 320, 2000), (1000, 33, 2000), (1500, 577, 2000), (2500, 96, 5000), (3300, 513, 3700), (2000, 100, 5600), (3800, 1090, 3000)]
 
 
 @pytest.mark.parametrize("packed", [False, True])
