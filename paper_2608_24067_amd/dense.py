@@ -16,6 +16,7 @@ import ctypes
 import functools
 from array import array
 from itertools import chain
+from operator import attrgetter
 from typing import NamedTuple, Optional
 
 import torch
@@ -476,13 +477,18 @@ def _held(t, name, n, dtype, at):
     return t.data_ptr()
 
 
+# What a list of tensors is asked, one question at a time: faster than tensor by tensor.
+_numel, _number, _dtype = torch.Tensor.numel, torch.Tensor.get_device, attrgetter("dtype")
+_dense, _address = torch.Tensor.is_contiguous, torch.Tensor.data_ptr
+
+
 def _held_all(ts, name, dtype, sizes, at):
     """The pointers of such tensors; dtype None: of any type."""
     try:
-        if ([t.numel() for t in ts] == sizes and {t.get_device() for t in ts} == {at}
-                and (dtype is None or {t.dtype for t in ts} == {dtype}) and all([t.is_contiguous() for t in ts])):
-            return [t.data_ptr() for t in ts]
-    except AttributeError:  # something that is no tensor
+        if (list(map(_numel, ts)) == sizes and set(map(_number, ts)) == {at}
+                and (dtype is None or set(map(_dtype, ts)) == {dtype}) and all(map(_dense, ts))):
+            return list(map(_address, ts))
+    except (AttributeError, TypeError):  # something that is no tensor
         pass
     return [_held(t, name, n, t.dtype if dtype is None else dtype, at) for t, n in zip(ts, sizes)]
 
@@ -537,11 +543,13 @@ def adamw(params, grads, states, step, lr=1e-3, betas=(0.9, 0.999), eps: float =
         raise ValueError("the parameters must be on the GPU")
     dev = params[0].device
     at, eight = dev.index, states[0][2] is not None
-    kinds, grad_kinds = ([_TYPES.get(getattr(t, "dtype", None)) for t in ts] for ts in (params, grads))
-    if None in kinds or None in grad_kinds:
+    try:
+        kinds, grad_kinds = ([_TYPES[t] for t in map(_dtype, ts)] for ts in (params, grads))
+    except (AttributeError, KeyError):
         for t in params + grads:
             _type(t, "params and grads", halves=False)
-    sizes = [t.numel() for t in params]
+        raise
+    sizes = list(map(_numel, params))
     pointers = _held_all(params, "params", None, sizes, at)
     table, address = _table(pointers, _held_all(grads, "grads", None, sizes, at), *_state_pointers(states, sizes, eight, at),
                             sizes, [k | g << 32 for k, g in zip(kinds, grad_kinds)])
@@ -574,7 +582,7 @@ def adamw_values(states, out=None):
     if not isinstance(states[0][0], torch.Tensor) or not states[0][0].is_cuda:
         raise ValueError("the states must be on the GPU")
     dev = states[0][0].device
-    sizes, none = [s[0].numel() for s in states], [0] * n
+    sizes, none = list(map(_numel, [s[0] for s in states])), [0] * n
     held = _state_pointers([(*s[:4], None) for s in states], sizes, True, dev.index)
     table, address = _table(none, none, *held, sizes, none)  # read during the call
     tos = [array("q", _held_all(ts, name, torch.float32, sizes, dev.index)) for ts, name in zip(out, ("m", "v"))]
