@@ -198,8 +198,9 @@ template <typename X, typename Y> __global__ __launch_bounds__(1024) void k_norm
 
 // The gradient. With h = (x - mean) / std and t = dy * weight:
 //   dx = add + (t - mean(t) - h mean(t h)) / std,   dweight = sum over rows of dy h,   dbias = of dy.
-// A workgroup takes part_rows rows and holds its sums of dweight and dbias in registers; they are
-// joined over its waves in LDS and written as one part, and k_norm_sums adds the parts in order.
+// A workgroup holds its rows' sums of dweight and dbias in registers; they are joined over its waves in LDS
+// and written as one part, and k_norm_sums adds the parts in order. Its rows are as far apart as there are
+// workgroups, so that those in flight are neighbours (6000 x 4096 fp32: 44.5 us, 50.4 with its rows side by side).
 // Two workgroups a CU, whose loads hide each other's exchanges, where a thread has two vectors at most.
 template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT, S::C <= 2 ? 4 : 2) void k_norm_grad(const NormArgs a)
 {
@@ -217,7 +218,7 @@ template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT, S::C <= 2 ? 4
 #pragma unroll
         for (int i = 0; i < V; ++i) dw[c][i] = db[c][i] = 0.0f;
     }
-    const int64_t first = (int64_t)blockIdx.x * a.part_rows, end = min(a.N, first + a.part_rows);
+    const int64_t first = (int64_t)blockIdx.x * S::ROWS, end = a.N, step = (int64_t)gridDim.x * S::ROWS;
     const X *x = static_cast<const X *>(a.x);
     const Y *dy = static_cast<const Y *>(a.y);
     Row<X, S> xn, xl;
@@ -231,9 +232,9 @@ template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT, S::C <= 2 ? 4
         i = a.stats[2 * row + 1];
     };
     fetch(first + sub, xn, gn, mean_n, inv_n);
-    for (int64_t n = first; n < end; n += S::ROWS) {
+    for (int64_t n = first; n < end; n += step) {
         const int64_t row = n + sub;
-        fetch(row + S::ROWS, xl, gl, mean_l, inv_l);
+        fetch(row + step, xl, gl, mean_l, inv_l);
         const Centre centre(mean_n, inv_n);
         const bool in = row < end;
         float s = 0, q = 0;
