@@ -5,7 +5,7 @@
 //
 // One launch takes the chunks of up to 44 tensors; a thread's four or eight elements are loaded in
 // vectors. Bound by the bytes it moves: 28 an element in fp32 (168 million elements: 865 us, 5.5 TB/s), 10
-// of a 16-bit parameter with 8-bit states (350 us, 4.8 TB/s), whose arithmetic, some 65 instructions an
+// of a 16-bit parameter with 8-bit states (350 us, 4.8 TB/s), whose arithmetic, some 60 instructions an
 // element, takes nearly as long. A block's bytes are loaded before its codes: asked for after them, their wait came on top.
 //
 // 8-bit states. A block of 256 values shares a power of two 2^e, the least at which its largest

@@ -27,7 +27,7 @@ struct NormArgs {
     void *dx;                   // or null
     int64_t lddx;
     float *parts;               // [n_parts][2][D]: dweight, dbias; or null
-    int64_t n_parts, part_rows; // parts of part_rows rows each
+    int64_t n_parts, part_rows; // of rows too long for registers: parts of part_rows rows each
     float *means;               // [N][2], of rows too long for registers
 };
 

@@ -512,11 +512,11 @@ template <typename T, class S> __global__ __launch_bounds__(S::NT, S::PER_CU * S
     // The product of the tile; scaled: the widened codes hold their scale, in fp16 over 2^(top - 13 - 127).
     auto run = [&](auto scaled, f32x4 (&acc)[S::MI][S::NI], int top) {
         constexpr bool kScaled = decltype(scaled)::value;
-        const int over = (140 - top) * (1 << 23);
+        const uint32_t over = (uint32_t)(140 - top) << 23;
         auto widen = [&](const Raw &r) {
             if constexpr (kBf16) return Wide{widen8<T>(r.codes, r.scale), 0.0f};
             // a block of zeros may end below 0 and is taken there
-            else if constexpr (kScaled) return Wide{layer::widen8_by<T>(r.codes, __int_as_float(max((int)(r.scale << 23) + over, 0))), 0.0f};
+            else if constexpr (kScaled) return Wide{layer::widen8_by<T>(r.codes, __int_as_float(max((int)((r.scale << 23) + over), 0))), 0.0f};
             else return Wide{widen8<T>(r.codes, r.scale), scale_value(r.scale)};
         };
         auto multiply = [&](const Wide &b, const Frag &a, f32x4 c) {
