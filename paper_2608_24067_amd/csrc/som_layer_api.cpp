@@ -224,15 +224,18 @@ som_status som_layer_norm_bwd(int32_t type, const void *X, int64_t ldx, const vo
     a.x = X, a.ldx = ldx, a.weight = weight, a.weights_f32 = weight_type == SOM_F32;
     a.y = const_cast<void *>(dY), a.ldy = lddy, a.stats = const_cast<double *>(stats), a.N = N, a.D = (int32_t)D;
     a.add = add, a.lda = ldadd, a.dx = dX, a.lddx = lddx;
-    a.n_parts = som::norm_parts(N, D * size_of(type) > 1024 * 16);  // rows of more than 1,024 vectors
+    const int64_t vectors = (D * size_of(type) + 15) / 16;
+    const bool whole = N > 0 && vectors <= 2048 && N * som::norm_grad_threads(vectors) <= 2 * 512;
+    a.n_parts = whole ? 1 : som::norm_parts(N, vectors > 1024);
     a.part_rows = (N + a.n_parts - 1) / a.n_parts;
-    a.parts = sums ? static_cast<float *>(workspace) : nullptr;
+    if (whole) a.dweight = dweight, a.dbias = dbias;
+    a.parts = sums && !whole ? static_cast<float *>(workspace) : nullptr;
     a.means = reinterpret_cast<float *>(static_cast<char *>(workspace) + align256((size_t)a.n_parts * 2 * (size_t)D * 4));
     if (N > 0 && (dX || sums)) {
         const hipError_t e = som::launch_norm_grad(type, y_type, a, s);
         if (e != hipSuccess) return done(e, who);
     }
-    if (!sums) return ok();
+    if (!sums || whole) return ok();
     return done(som::launch_norm_sums(a.parts, N > 0 ? a.n_parts : 0, a.D, dweight, dbias, weight_type, s), who);
 }
 

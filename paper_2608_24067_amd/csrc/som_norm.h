@@ -277,7 +277,7 @@ template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT, S::C <= 2 ? 4
         mean_n = mean_l;
         inv_n = inv_l;
     }
-    if (!a.parts) return;
+    if (!a.parts && !a.dweight && !a.dbias) return;
     float *out = a.parts + (int64_t)blockIdx.x * 2 * D;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -300,7 +300,13 @@ template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT, S::C <= 2 ? 4
                     }
                 }
             }
-            if (sub == 0 && at < D) store<V>(out + (int64_t)j * D + at, WHOLE ? V : D - at, v);
+            if (sub != 0 || at >= D) continue;
+            if (a.parts) {
+                store<V>(out + (int64_t)j * D + at, WHOLE ? V : D - at, v);
+            } else if (void *to = j ? a.dbias : a.dweight) {  // of the only part
+                if (a.weights_f32) store<V>(static_cast<float *>(to) + at, WHOLE ? V : D - at, v);
+                else store<V>(static_cast<Y *>(to) + at, WHOLE ? V : D - at, v);
+            }
         }
     }
 }
