@@ -201,8 +201,10 @@ template <typename X, typename Y> __global__ __launch_bounds__(1024) void k_norm
 // A workgroup holds its rows' sums of dweight and dbias in registers; they are joined over its waves in LDS
 // and written as one part, and k_norm_sums adds the parts in order. Its rows are as far apart as there are
 // workgroups, so that those in flight are neighbours (6000 x 4096 fp32: 44.5 us, 50.4 with its rows side by side).
-// Two workgroups a CU, whose loads hide each other's exchanges, where a thread has two vectors at most.
-template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT, S::C <= 2 ? 4 : 2) void k_norm_grad(const NormArgs a)
+// Two workgroups a CU, whose loads hide each other's exchanges, where a thread has two vectors at most; but one
+// for rows of 512 threads that end inside a vector, whose code takes more registers (5000 x 8190 bf16 101 us,
+// with two 114; 8192 x 4095, 256 threads a row, 78 and with two 63).
+template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT, S::C <= 2 && (WHOLE || S::TPR < 512) ? 4 : 2) void k_norm_grad(const NormArgs a)
 {
     typedef typename S::X X;
     typedef typename S::Y Y;
