@@ -66,13 +66,14 @@ struct Rates : AdamwRates {
     // by1, by2: b1 and b2, or what stands for them (an 8-bit block's). The products of m and v are
     // rounded one by one, as documented; the parameter's part takes the hardware's root and reciprocal,
     // good to a unit in the last place, for a third of an 8-bit step's instructions. The hardware takes a
-    // subnormal root's argument as zero, so it is kept at the smallest normal value.
+    // subnormal root's argument as zero: such a v is taken times 2^64, and its root's factor over 2^32.
     __device__ void apply(float &p, float g, float &m, float &v, float by1, float by2) const
     {
         g *= grad;
         m = m * by1 + g * c1;
         v = v * by2 + g * g * c2;
-        const float den = fmaf(__builtin_amdgcn_sqrtf(v < 0x1p-126f ? 0x1p-126f : v), root, eps);
+        const bool small = v < 0x1p-126f;
+        const float den = fmaf(__builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v), small ? root * 0x1p-32f : root, eps);
         p = fmaf(-rate, m * __builtin_amdgcn_rcpf(den), p * keep);
     }
 };

@@ -69,6 +69,22 @@ def adamw(p, g, m, v, step, lr, betas, eps, weight_decay, grad_scale=1.0):
     return (p2, 4 * E * p.abs() + off), (m2, off_m), (v2, off_v)
 
 
+def adamw_between(p, g, m, v, step, lr, betas, eps, weight_decay):
+    """(low, high) of p after a step where v may underflow: any v that fp32 may hold instead is allowed, and nothing more.
+
+    v is off by off_v at most, so the root lies between those of v - off_v (not below 0) and v + off_v. The root, its
+    factor, eps, their fma, the reciprocal, its product with m and the rate round by 10 E together, p's decay by 3 E;
+    what is subnormal on the way is off by 2^-149."""
+    b1, b2 = betas
+    _, (m2, off_m), (v2, off_v) = adamw(p, g, m, v, step, lr, betas, eps, weight_decay)
+    rate = lr / (1 - b1 ** step)
+    dens = [torch.sqrt(t / (1 - b2 ** step)) + eps for t in ((v2 - off_v).clamp_min(0), v2 + off_v)]
+    updates = torch.stack([rate * t / d for t in (m2 - off_m, m2 + off_m) for d in dens])
+    keep = wide(p) * (1 - lr * weight_decay)
+    off = 3 * E * wide(p).abs() + (1 + rate) * 2.0 ** -148
+    return (keep - (updates + 10 * E * updates.abs()).amax(0) - off,
+            keep - (updates - 10 * E * updates.abs()).amin(0) + off)
+
 BLOCK = 256
 U32 = np.uint32
 

@@ -266,3 +266,35 @@ def test_nothing_to_do(dev):
     assert dense.adamw_values([]) == ([], [])
     p = torch.empty(0, device=dev)
     dense.adamw([p], [p], [dense.adamw_state(p, 8)], 1)
+
+
+def between(p, low, high, what):
+    """p within [low, high], and a rounding of it."""
+    p = wide(p)
+    off = ref.E * torch.maximum(low.abs(), high.abs()) + 2.0 ** -149
+    bad = ~((p >= low - off) & (p <= high + off))
+    assert not bool(bad.any()), (f"{what}: {int(bad.sum())} of {bad.numel()} outside, first at {bad.nonzero()[0].tolist()}: "
+                                 f"{float(p[bad][0])} not in {float(low[bad][0])} ... {float(high[bad][0])}")
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-12, 1e-15, 1e-18, 1e-20, 1e-30, 2.0 ** -126])
+@pytest.mark.parametrize("size", [1e-14, 1e-17, 1e-18, 1e-19, 1e-20, 1e-22, 1e-24, 0.0])
+def test_small_eps_beside_small_squares(dev, bits, eps, size):
+    # squares that fp32 holds as subnormals, or not at all, against an eps as small as their roots
+    how = {**HOW, "eps": eps}
+    g = torch.Generator().manual_seed(11)
+    grads = [torch.randn(n, generator=g).to(dev) * size for n in (1000, 77)]
+    params = [torch.zeros_like(t) for t in grads]
+    states = [dense.adamw_state(p, bits) for p in params]
+    if bits == 32:
+        states[1].m.fill_(1e-3 * eps)  # with v == 0: eps alone stands below it
+    for step in (1, 2, 3):
+        before, old = [p.clone() for p in params], copies(states)
+        dense.adamw(params, grads, states, step, seed=step, **how)
+        for p, t, s, b, o in zip(params, grads, states, before, old):
+            m, v = o.m, o.v
+            if bits == 8:
+                m = torch.from_numpy(ref.values8(o.m.cpu().numpy(), o.m_scales.cpu().numpy(), True))
+                v = torch.from_numpy(ref.values8(o.v.cpu().numpy(), o.v_scales.cpu().numpy(), False))
+            between(p, *ref.adamw_between(b, t, m, v, step, **how), f"p, step {step}")
