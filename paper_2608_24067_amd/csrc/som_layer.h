@@ -92,6 +92,7 @@ struct AdamwTable {
 // What a step multiplies by, in fp32 from fp64: the same bits on the host and on the device.
 struct AdamwRates {
     float b1, c1, b2, c2, keep, rate, root, eps, grad;
+    float down;  // 1; or, where eps is so large that a denominator's reciprocal is subnormal, 2^-8, which rate, root and eps hold
     uint32_t step;
 
     __host__ __device__ static double power(double b, uint32_t t)  // by squaring
@@ -107,8 +108,8 @@ struct AdamwRates {
         b1 = (float)beta1, c1 = (float)(1.0 - beta1);
         b2 = (float)beta2, c2 = (float)(1.0 - beta2);
         keep = (float)(1.0 - lr * weight_decay);
-        rate = (float)(lr / (1.0 - power(beta1, t)));
-        root = (float)(1.0 / sqrt(1.0 - power(beta2, t)));
+        rate = (float)(lr / (1.0 - power(beta1, t)) * down);
+        root = (float)(1.0 / sqrt(1.0 - power(beta2, t)) * down);
     }
 };
 

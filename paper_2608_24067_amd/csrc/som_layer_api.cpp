@@ -258,8 +258,9 @@ som_status som_adamw(const som_adamw_tensor *tensors, int64_t count, const som_a
     if (st != SOM_OK) return st;
     som::AdamwArgs a{};
     a.lr = c.lr, a.beta1 = c.beta1, a.beta2 = c.beta2, a.weight_decay = c.weight_decay;
+    a.rates.down = c.eps > 0x1p100 ? 0x1p-8f : 1.0f;
     a.rates.set(c.lr, c.beta1, c.beta2, c.weight_decay, (uint32_t)c.step);
-    a.rates.eps = (float)c.eps, a.rates.grad = (float)c.grad_scale;
+    a.rates.eps = (float)c.eps * a.rates.down, a.rates.grad = (float)c.grad_scale;
     a.seed = c.seed, a.lr_at = c.lr_at, a.step_at = c.step_at, a.norm = c.norm;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return done(over_tables(tensors, count, bits8, [&](som::AdamwTable &t, int64_t) { return som::launch_adamw(t, bits8, a, s); }), who);

@@ -298,3 +298,24 @@ def test_small_eps_beside_small_squares(dev, bits, eps, size):
                 m = torch.from_numpy(ref.values8(o.m.cpu().numpy(), o.m_scales.cpu().numpy(), True))
                 v = torch.from_numpy(ref.values8(o.v.cpu().numpy(), o.v_scales.cpu().numpy(), False))
             between(p, *ref.adamw_between(b, t, m, v, step, **how), f"p, step {step}")
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [2.0 ** 100, 2.0 ** 126, 1.0e38, 3.4e38])
+@pytest.mark.parametrize("where", ["host", "device"])
+def test_large_eps(dev, bits, eps, where):
+    # a denominator whose reciprocal is subnormal in fp32; step and rate from the call, or read on the device
+    how = {**HOW, "eps": eps}
+    g = torch.Generator().manual_seed(12)
+    grad = (1 + torch.rand(1000, generator=g)).to(dev) * 1e18
+    grad[::2] *= -1
+    param = torch.zeros(1000, device=dev)
+    state = dense.adamw_state(param, bits)
+    zero = torch.zeros(1000, dtype=torch.float64)
+    if where == "device":
+        at = dict(lr=torch.full((1,), HOW["lr"], device=dev))
+        dense.adamw([param], [grad], [state], torch.ones(1, dtype=torch.int32, device=dev), **{**how, **at})
+        how["lr"] = float(at["lr"])
+    else:
+        dense.adamw([param], [grad], [state], 1, **how)
+    between(param, *ref.adamw_between(zero, grad, zero, zero, 1, **how), "p")
