@@ -47,12 +47,12 @@ __device__ inline void moments(double s, double q, double from, int D, double ep
 
 // (x - mean) / std in fp32: the mean in two parts, so that a mean much larger than the spread costs
 // nothing. Rows that come near the end of fp32's range are scaled down first, which is exact and, in the
-// fused product, free.
+// fused product, free. The others are at most sqrt(D) < 2^10 times the spread, and so 2^126, from their mean.
 struct Centre {
     float scale, hi, lo, inv, inv_std;
     __device__ Centre(double mean, double i) : inv_std((float)i)
     {
-        const bool far = !(fabs(mean) < 0x1p125 && i > 0x1p-120);
+        const bool far = !(fabs(mean) < 0x1p125 && i > 0x1p-116);
         const double s = far ? 0x1p-32 : 1.0;
         scale = (float)s;
         hi = (float)(mean * s);

@@ -225,3 +225,24 @@ def test_captured_forward_and_backward_replayed(dev):
         torch.cuda.synchronize()
         for a, c in zip((y, stats, *out), (want[0], want[1], *want[2])):
             assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("x,y", [(F32, F32), (F32, BF16), (BF16, BF16)])
+@pytest.mark.parametrize("D", [66000, 70001, 1000003])
+def test_the_largest_value_far_from_a_long_rows_mean(dev, x, y, D):
+    # its distance from the mean passes fp32's range, while the spread of so many features does not come near it
+    top = torch.finfo(x).max
+    rows = torch.full((3, D), -top / 100)
+    rows[:, ::3] *= 1.01
+    rows[0, 17] = rows[1, D - 1] = rows[2, 0] = top
+    rows[2] *= -1
+    g = torch.Generator().manual_seed(D)
+    rows, dy = rows.to(x).to(dev), torch.randn(3, D, generator=g).to(y).to(dev)
+    w, b = (1 + 0.3 * torch.randn(D, generator=g)).to(dev), (0.3 * torch.randn(D, generator=g)).to(dev)
+    y_, stats, (dx, dw, db) = run(rows, w, b, dy, None, y)
+    want, bound, *_ = ref.norm(rows, w, b, EPS)
+    check(y_, want, bound, "y")
+    (vx, off), (vw, off_w), (vb, off_b) = ref.norm_grad(rows, w, dy, EPS)
+    check(dx, vx, off + 2.0 ** -146, "dx")  # near fp32's smallest values: a few roundings of 2^-149
+    check(dw, vw, off_w, "dweight")
+    check(db, vb, off_b, "dbias")
