@@ -651,7 +651,7 @@ def mx4_linear(x, W: Mx4, bias=None, residual=None, act: str = "none", out=None,
     """residual + act(x W + bias), as linear, with W in 4 bits (mx4_quantise(W, columns=True)).
 
     x is rows [N, K] in float16 or bfloat16, or in 4 bits (an Mx4; the result's type is then ``dtype``, that of out,
-    residual or a 16-bit bias, or bfloat16). bias, residual and the result are as in linear.
+    residual or a 16-bit bias, a 16-bit ``out_dtype``, or bfloat16). bias, residual and the result are as in linear.
     """
     packed = isinstance(x, tuple)
     if packed:
@@ -660,7 +660,7 @@ def mx4_linear(x, W: Mx4, bias=None, residual=None, act: str = "none", out=None,
         ldx, at = 0, x[0]
         if dtype is None:
             dtype = next((t.dtype for t in (out, residual, bias) if isinstance(t, torch.Tensor) and t.dtype != torch.float32),
-                         torch.bfloat16)
+                         out_dtype if out_dtype not in (None, torch.float32) else torch.bfloat16)
     else:
         _type(x, "x")
         dev, at, dtype, xs = x.device, x, x.dtype, None

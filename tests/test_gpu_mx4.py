@@ -351,3 +351,17 @@ def test_residual_is_the_result(dev, dtype, packed, N, K, M):
     sides = r[:, 0].clone(), r[:, M + 1].clone()
     dense.mx4_linear(rows, W, residual=r[:, 1:M + 1], act="silu", out=r[:, 1:M + 1])
     assert torch.equal(r[:, 1:M + 1], want) and torch.equal(r[:, 0], sides[0]) and torch.equal(r[:, M + 1], sides[1])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("N", [3, 300])
+def test_type_of_a_new_result_of_packed_rows(dev, dtype, N):
+    W = matrix(9, 96, 130, dev)
+    rows = dense.mx4_quantise(torch.randn(N, 96, generator=torch.Generator().manual_seed(9)).to(dev))
+    want = dense.mx4_linear(rows, W, dtype=dtype)
+    got = dense.mx4_linear(rows, W, out_dtype=dtype)
+    assert got.dtype == dtype and torch.equal(got, want)
+    b = torch.randn(130, generator=torch.Generator().manual_seed(10)).to(dtype).to(dev)
+    assert torch.equal(dense.mx4_linear(rows, W, b, out_dtype=dtype), dense.mx4_linear(rows, W, b))
+    with pytest.raises(TypeError):
+        dense.mx4_linear(rows, W, b, out_dtype=F16 if dtype == BF16 else BF16)
