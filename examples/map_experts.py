@@ -87,10 +87,11 @@ class MapExperts:
         self.rebalance(x.shape[0])
         return miss.square().sum(1).mean(), norm
 
-    def rebalance(self, n):
-        """Units that take more than their share become less attractive, without a gradient."""
+    def rebalance(self, n, counts=True):
+        """Units that take more than their share become less attractive, without a gradient; nothing changes where
+        ``counts``, a truth value on the host or the GPU, is false."""
         share = self.counts.float() / max(1.0, float(n * self.taken)) * self.units
-        self.balance += 0.05 * (1.0 - share)
+        self.balance += 0.05 * (1.0 - share) * counts
 
 
 class NormedExperts:
@@ -103,7 +104,7 @@ class NormedExperts:
         self.weight, self.bias = torch.ones(width, device=dev), torch.zeros(width, device=dev)
         self.params = [self.weight, self.bias] + self.experts.params
         self.states = [dense.adamw_state(p, bits, master=p.dtype != torch.float32) for p in self.params]
-        self.taken = 0  # steps
+        self.taken = torch.zeros(1, dtype=torch.int32, device=dev)  # steps that were not left out
         self.four = None  # the prototypes in 4 bits, since the last step
 
     def forward(self, x):
@@ -123,15 +124,16 @@ class NormedExperts:
 
     def step(self, x, target, rate=3e-3, max_norm=1.0):
         """One step on the mean squared distance to target; returns (loss, gradients' norm). Gradients that hold no
-        number leave it out."""
+        number leave it out: nothing changes, and it does not count."""
         out, kept = self.forward(x)
         miss = out.float() - target.float()
         grads, _ = self.gradients(x, kept, (miss * (2.0 / miss.shape[0])).to(x.dtype))
         grads, norm = dense.clip(grads, max_norm)
-        self.taken += 1
+        counts = norm.isfinite()  # asked and answered on the GPU
+        self.taken += counts
         dense.adamw(self.params, grads, self.states, self.taken, lr=rate, norm=norm)
         self.four = None
-        self.experts.rebalance(x.shape[0])
+        self.experts.rebalance(x.shape[0], counts)
         return miss.square().sum(1).mean(), norm
 
     def answer(self, x, both=True):

@@ -186,3 +186,28 @@ def test_normalised_rows_in_4_bits(dev):
     hv, wv = ref.values4(rows.codes, rows.scales, D), ref.values4(W.codes, W.scales, D)
     check(y, hv @ wv.t(), sums(D, hv.abs() @ wv.abs().t()), "y")
     check(dense.mx4_linear(h, W, out_dtype=F32), wide(h) @ wv.t(), sums(D, wide(h).abs() @ wv.abs().t()), "y, rows in 16 bits")
+
+
+def test_a_step_that_is_left_out_leaves_no_trace(dev, example):
+    # parameters, running means, the gate's balance, the step's number, and the steps after it: as if it had not been
+    prototypes = torch.randn(48, 16, generator=torch.Generator().manual_seed(2))
+
+    def held(model):
+        return [t.clone() for t in (*model.params, *(t for s in model.states for t in s if t is not None),
+                                    model.experts.balance, model.taken)]
+
+    for first in (False, True):
+        one, two = (example.NormedExperts(prototypes, 72, bits=8, seed=3) for _ in range(2))
+        if not first:
+            assert all(bool(m.step(*example.rows(100, prototypes, seed=4))[1].isfinite()) for m in (one, two))
+        before = held(one)
+        x, target = example.rows(100, prototypes, seed=5)
+        target[3, 5] = float("inf")
+        _, norm = one.step(x, target)
+        assert not bool(norm.isfinite())
+        assert all(torch.equal(a, b) for a, b in zip(before, held(one)))
+        for s in (6, 7):
+            for m in (one, two):
+                m.step(*example.rows(100, prototypes, seed=s))
+            assert all(torch.equal(a, b) for a, b in zip(held(one), held(two)))
+        assert int(one.taken) == (2 if first else 3)
