@@ -45,8 +45,8 @@ class MapExperts:
         self.counts = torch.empty(units, dtype=torch.int32, device=device)
         self.workspace = None
 
-    def forward(self, x, keep=True):
-        """(out, what the backward pass needs) of rows x [N, width]."""
+    def forward(self, x, keep=True, residual=None):
+        """(out, what the backward pass needs) of rows x [N, width]; out is the experts' part and ``residual`` (x)."""
         W, W1, b1, W2, b2 = self.params
         # the norms of the prototypes as they are held now: the search's own pass over the widened codebook
         self.gate_bias = (-0.5 * som.codebook_norms(W.float(), W.shape[0], W.shape[1])).float()
@@ -55,7 +55,8 @@ class MapExperts:
         need = dense.experts_workspace_bytes(x.shape[0], self.taken, self.units, W1.shape[1], W1.shape[2], keep)
         if self.workspace is None or self.workspace.numel() < need:
             self.workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-        out = dense.experts(x, idx, w, W1, b1, W2, b2, residual=x, keep=keep, workspace=self.workspace)
+        out = dense.experts(x, idx, w, W1, b1, W2, b2, residual=x if residual is None else residual, keep=keep,
+                            workspace=self.workspace)
         return out, (scores, idx, w)
 
     def backward(self, x, kept, dout, dx=None):
@@ -110,8 +111,8 @@ class NormedExperts:
     def forward(self, x):
         stats = torch.empty(x.shape[0], 2, dtype=torch.float64, device=x.device)
         h = dense.layer_norm(x, self.weight, self.bias, stats=stats)
-        out, kept = self.experts.forward(h)  # h + the experts' part
-        return out.add_(x).sub_(h), (h, stats, kept)
+        out, kept = self.experts.forward(h, residual=x)
+        return out, (h, stats, kept)
 
     def gradients(self, x, kept, dout):
         """The parameters' gradients, in their order, and the rows', which go round the layer too."""

@@ -211,3 +211,18 @@ def test_a_step_that_is_left_out_leaves_no_trace(dev, example):
                 m.step(*example.rows(100, prototypes, seed=s))
             assert all(torch.equal(a, b) for a, b in zip(held(one), held(two)))
         assert int(one.taken) == (2 if first else 3)
+
+
+def test_rows_much_larger_than_the_experts_part(dev, example):
+    # the sum with the rows is rounded once: a bf16 result is off by half its step, and by the experts' own part's error,
+    # which the same call without the residual shows the size of
+    prototypes = torch.randn(48, 16, generator=torch.Generator().manual_seed(2))
+    model = example.NormedExperts(prototypes, 72, seed=3)
+    x, _ = example.rows(200, prototypes, seed=4)
+    x = x + 37.0
+    out, (h, _, (_, idx, w)) = model.forward(x)
+    _, W1, b1, W2, b2 = model.experts.params
+    assert torch.equal(out, dense.experts(h, idx, w, W1, b1, W2, b2, residual=x))
+    part = dense.experts(h, idx, w, W1, b1, W2, b2)
+    want = wide(x) + wide(part)
+    check(out, want, 2.0 ** -8 * wide(part).abs(), "out")
