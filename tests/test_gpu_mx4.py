@@ -365,3 +365,23 @@ def test_type_of_a_new_result_of_packed_rows(dev, dtype, N):
     assert torch.equal(dense.mx4_linear(rows, W, b, out_dtype=dtype), dense.mx4_linear(rows, W, b))
     with pytest.raises(TypeError):
         dense.mx4_linear(rows, W, b, out_dtype=F16 if dtype == BF16 else BF16)
+
+
+@pytest.mark.parametrize("N,K,M", [(2, 544, 40), (16, 544, 4100), (40, 544, 3000), (33, 544, 9000), (300, 544, 1500), (1000, 544, 2000),
+                                   (2011, 544, 5625), (4000, 544, 3400)])
+def test_bf16_rows_and_the_smallest_scales(dev, N, K, M):
+    # the scale 0 stands for 2^-127, under which the codes for 0.5 to 1.5 are subnormal in bf16
+    codes, scales = codes_and_scales(6, K, M, 0, 2, dev)
+    g = torch.Generator().manual_seed(N)
+    x = (torch.randn(N, K, generator=g) * 2.0 ** 100).to(BF16)
+    if N > 2:
+        x[1] = 2.0 ** -100 * x[1]  # products that are subnormal in fp32
+    W = dense.Mx4(codes.to(dev), scales.to(dev), K)
+    wv = ref.values4(codes, scales, K)
+    y = dense.mx4_linear(x.to(dev), W, out_dtype=F32)
+    check(y, wide(x) @ wv.t(), sums(K, wide(x).abs() @ wv.abs().t()) + 2.0 ** -147, "y")
+    # the four smallest sizes alone
+    codes &= 0x33
+    wv = ref.values4(codes, scales * 0, K)
+    y = dense.mx4_linear(x.to(dev), dense.Mx4(codes.to(dev), (scales * 0).to(dev), K), out_dtype=F32)
+    check(y, wide(x) @ wv.t(), sums(K, wide(x).abs() @ wv.abs().t()) + 2.0 ** -147, "y, the smallest")
