@@ -319,3 +319,39 @@ def test_large_eps(dev, bits, eps, where):
     else:
         dense.adamw([param], [grad], [state], 1, **how)
     between(param, *ref.adamw_between(zero, grad, zero, zero, 1, **how), "p")
+
+
+def test_values_of_every_code_and_scale_of_states(dev):
+    codes = torch.arange(256, dtype=torch.uint8).repeat(256)
+    scales = torch.arange(256, dtype=torch.uint8)
+    state = dense.AdamwState(codes.to(dev), codes.to(dev), scales.to(dev), scales.to(dev))
+    (m,), (v,) = dense.adamw_values([state])
+    for x, signed in ((m, True), (v, False)):
+        want = ref.values8(codes.numpy(), scales.numpy(), signed)
+        with np.errstate(over="ignore"):  # a byte of 254 stands for values beyond fp32's range, too
+            assert np.array_equal(x.cpu().numpy(), want.astype(np.float32), equal_nan=True)
+
+
+@pytest.mark.parametrize("bits", [[0], [0, 1, 2, 255]])
+def test_states_at_every_exponent(dev, bits):
+    # a block for each exponent of its largest gradient, subnormals and the largest too, the others of any size below it;
+    # betas of 0 make the states the gradient and its square
+    rng = np.random.default_rng(17)
+    e = np.arange(255, dtype=np.int64)[:, None]
+    top = (e << 23) + rng.integers(0, 1 << 23, (255, 1))
+    g = np.minimum((np.maximum(e - rng.integers(0, 40, (255, 256)), 0) << 23) + rng.integers(0, 1 << 23, (255, 256)), top)
+    g[np.arange(255), rng.integers(0, 256, 255)] = top[:, 0]
+    g = (g + (rng.integers(0, 2, g.shape) << 31)).astype(np.uint32).view(np.float32).reshape(-1)
+    p = torch.zeros(g.size, device=dev)
+    state = dense.adamw_state(p, bits=8)
+    # what stood there before counts for nothing, but for a block of NaN
+    for s in (state.m_scales, state.v_scales):
+        s.copy_(torch.tensor(bits, dtype=torch.uint8).repeat(255)[:255])
+    old = copies([state])[0]
+    grad = torch.from_numpy(g).to(dev)
+    dense.adamw([p], [grad], [state], 3, seed=9, lr=0.0, betas=(0.0, 0.0))
+    (mc, ms), (vc, vs), *_ = next_states(old, grad, 0, 9, 3, (0.0, 0.0))
+    for codes, scales, c, s in ((state.m, state.m_scales, mc, ms), (state.v, state.v_scales, vc, vs)):
+        assert np.array_equal(scales.cpu().numpy(), s)
+        some = np.repeat(s != 255, 256)  # codes of a block of NaN have no meaning
+        assert np.array_equal(codes.cpu().numpy()[some], c[some])

@@ -385,3 +385,110 @@ def test_bf16_rows_and_the_smallest_scales(dev, N, K, M):
     wv = ref.values4(codes, scales * 0, K)
     y = dense.mx4_linear(x.to(dev), dense.Mx4(codes.to(dev), (scales * 0).to(dev), K), out_dtype=F32)
     check(y, wide(x) @ wv.t(), sums(K, wide(x).abs() @ wv.abs().t()) + 2.0 ** -147, "y, the smallest")
+
+
+@pytest.mark.parametrize("columns", [False, True])
+def test_values_of_every_code_and_scale(dev, columns):
+    # a row for each scale byte: its blocks hold every code at every place
+    K = 64
+    four = (torch.arange(256)[:, None] + torch.arange(K)[None, :] * 5) % 16
+    codes = (four[:, 0::2] | four[:, 1::2] << 4).to(torch.uint8)
+    scales = torch.arange(256)[:, None].expand(256, 2).to(torch.uint8).contiguous()
+    want = ref.values4(codes, scales, K)
+    q = dense.Mx4(codes.to(dev), scales.to(dev), K)
+    for t in (F32, BF16, F16):
+        v = dense.mx4_values(q, columns=columns, dtype=t).cpu()
+        v = v.t() if columns else v
+        assert torch.equal(v.isnan(), want.isnan())
+        assert torch.equal(v[:255], want.to(t)[:255])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_codes_at_every_exponent(dev, dtype):
+    # a block for each exponent of its largest value, subnormals too, and smaller values down to 2^-6 of it: ties, their
+    # neighbours on either side, and any bits
+    g = torch.Generator().manual_seed(31)
+    kind, sign, last = {F32: (torch.int32, 1 << 31, 23), BF16: (torch.int16, 1 << 15, 7), F16: (torch.int16, 1 << 15, 10)}[dtype]
+    most = (torch.tensor(torch.finfo(dtype).max, dtype=dtype).view(kind).item() >> last) + 1
+    rows = []
+    for e in range(most):
+        for r in range(8):
+            top = (e << last) + int(torch.randint(0, 1 << last, (1,), generator=g))
+            low = max(0, top - (6 << last))
+            bits = torch.randint(low, top + 1, (32,), generator=g)
+            if r % 2:  # one bit behind the point, or two, and a step beside it
+                bits = (bits >> (last - 2) << (last - 2)) + torch.randint(-1, 2, (32,), generator=g)
+            bits = bits.clamp(0, top)
+            bits[int(torch.randint(0, 32, (1,), generator=g))] = top
+            bits = bits + sign * torch.randint(0, 2, (32,), generator=g)
+            rows.append(bits)
+    bits = torch.stack(rows)
+    bits = torch.where(bits >= sign, bits - 2 * sign, bits).to(kind)
+    x = bits.view(dtype)
+    assert x.isfinite().all()
+    codes_equal(dense.mx4_quantise(x.to(dev)), x)
+    codes_equal(dense.mx4_quantise(x.t().contiguous().to(dev), columns=True), x)
+
+
+# N, M: every tile for K = 96, by both kinds of rows
+EVERY_TILE = [(3, 50), (16, 4200), (40, 3000), (33, 9000), (128, 2100), (300, 1500), (1000, 2000), (2011, 5625), (4000, 3400)]
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("N,M", EVERY_TILE)
+def test_blocks_for_nan_whose_codes_are_zeros(dev, dtype, packed, N, M):
+    K = 96
+    codes, scales = codes_and_scales(7, K, M, 126, 128, dev)
+    codes[5, 16:32], scales[5, 1] = 0, 255
+    codes[M - 1], scales[M - 1] = 0, 255
+    W = dense.Mx4(codes.to(dev), scales.to(dev), K)
+    spoiled = torch.zeros(N, M, dtype=torch.bool, device=dev)
+    spoiled[:, 5] = spoiled[:, M - 1] = True
+    if packed:
+        x, xs = codes_and_scales(8, K, N, 126, 128, dev)
+        x[N - 1, 32:48], xs[N - 1, 2] = 0, 255
+        spoiled[N - 1] = True
+        rows = dense.Mx4(x.to(dev), xs.to(dev), K)
+    else:
+        rows = torch.randn(N, K, generator=torch.Generator().manual_seed(N)).to(dtype).to(dev)
+    for act_ in ("none", "relu", "silu", "gelu"):
+        y = dense.mx4_linear(rows, W, act=act_, dtype=dtype if packed else None)
+        assert torch.equal(y.isnan(), spoiled), act_
+
+
+@pytest.mark.parametrize("N,M", EVERY_TILE)
+def test_packed_rows_and_scales_from_end_to_end(dev, N, M):
+    # a scale for each row and one for each column: their powers cancel, multiply beyond fp32's range, or below it
+    K = 96
+    g = torch.Generator().manual_seed(41)
+    codes, scales = codes_and_scales(9, K, M, 127, 127, dev)
+    x, xs = codes_and_scales(10, K, N, 127, 127, dev)
+    ends = torch.tensor([0, 1, 2, 20, 60, 63, 64, 65, 100, 126, 127, 128, 150, 189, 190, 191, 220, 240, 250, 252], dtype=torch.uint8)
+    scales[:] = ends[torch.randint(0, len(ends), (M, 1), generator=g)]
+    xs[:] = ends[torch.randint(0, len(ends), (N, 1), generator=g)]
+    y = wide(dense.mx4_linear(dense.Mx4(x.to(dev), xs.to(dev), K), dense.Mx4(codes.to(dev), scales.to(dev), K), out_dtype=F32))
+    xv, wv = ref.values4(x, xs, K), ref.values4(codes, scales, K)
+    want, size = xv @ wv.t(), xv.abs() @ wv.abs().t()
+    inside = size < 2.0 ** 127
+    off = sums(K, size) + K * 2.0 ** -149  # additions of subnormal sums round, too
+    assert ((y - want).abs() <= off)[inside].all()
+    beyond = want.abs() - sums(K, size) > 2.0 ** 128
+    assert (~y.isfinite())[beyond].all()
+
+
+@pytest.mark.parametrize("N,M", EVERY_TILE)
+def test_bf16_rows_and_scales_from_end_to_end(dev, N, M):
+    K = 96
+    g = torch.Generator().manual_seed(43)
+    codes, scales = codes_and_scales(11, K, M, 127, 127, dev)
+    ends = torch.tensor([0, 1, 2, 20, 60, 64, 100, 126, 127, 128, 150, 190, 220, 240, 250, 252], dtype=torch.uint8)
+    scales[:] = ends[torch.randint(0, len(ends), (M, 1), generator=g)]
+    x = (torch.randn(N, K, generator=g) * torch.exp2(torch.randint(-130, 120, (N, 1), generator=g).float())).to(BF16)
+    y = wide(dense.mx4_linear(x.to(dev), dense.Mx4(codes.to(dev), scales.to(dev), K), out_dtype=F32))
+    wv = ref.values4(codes, scales, K)
+    want, size = wide(x) @ wv.t(), wide(x).abs() @ wv.abs().t()
+    inside = size < 2.0 ** 127
+    assert ((y - want).abs() <= sums(K, size) + K * 2.0 ** -149)[inside].all()
+    beyond = want.abs() - sums(K, size) > 2.0 ** 128
+    assert (~y.isfinite())[beyond].all()
