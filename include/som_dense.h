@@ -260,9 +260,10 @@ typedef struct {
  * A step of AdamW (decoupled weight decay) over `count` tensors, with g = grad_scale * grad:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
- * in fp32. Of 8-bit states the step uses the new values before they are rounded. They are rounded to either of
- * the codes beside them, by the seed, so that their mean is kept; a v above zero is never rounded to zero. The same
- * arguments give the same bits.
+ * in fp32 (v below 2^-126 with its absolute error, 2^-149; root and reciprocal to a unit in the last place). Of 8-bit
+ * states the step uses the new values before they are rounded. They are rounded to either of the codes beside them, by
+ * the seed, so that their mean is kept; a v above zero is never rounded to zero but in a block that is all below 2^-100:
+ * eps should be well above the root of that, 2^-50. The same arguments give the same bits.
  * tensors is a host array, read during the call.
  */
 som_status som_adamw(const som_adamw_tensor *tensors, int64_t count, const som_adamw_config *config, void *stream);

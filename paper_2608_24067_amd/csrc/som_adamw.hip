@@ -5,7 +5,7 @@
 //
 // One launch takes the chunks of up to 44 tensors; a thread's four or eight elements are loaded in
 // vectors. Bound by the bytes it moves: 28 an element in fp32 (168 million elements: 865 us, 5.5 TB/s), 10
-// of a 16-bit parameter with 8-bit states (350 us, 4.8 TB/s), whose arithmetic, some 60 instructions an
+// of a 16-bit parameter with 8-bit states (336 us, 5.0 TB/s), whose arithmetic, some 60 instructions an
 // element, takes nearly as long. A block's bytes are loaded before its codes: asked for after them, their wait came on top.
 //
 // 8-bit states. A block of 256 values shares a power of two 2^e, the least at which its largest
@@ -17,7 +17,7 @@
 // by a thousandth of itself a step, and rounding to nearest, in steps of a sixteenth, would leave it
 // where it is. The 16 bits that decide come from a hash of the seed, the step, the tensor's number in
 // the call and the element's in the tensor: the same inputs give the same bits. A v above zero is
-// never rounded to zero, or a later step would divide what is left of m by eps alone.
+// never rounded to zero (but with its whole block), or a later step would divide what is left of m by eps alone.
 
 #include "som_layer_device.h"
 

@@ -117,6 +117,8 @@ struct FourLayout {
 
 // Bytes of the copied rows at most: strips of them stay in the cache.
 constexpr int64_t kFourStrip = (int64_t)32 << 20;
+// Rows of more than 65,536 features, 256 of which do not fit, are not copied: those off 16 bytes take the kernel for few
+// rows, whatever their number (300 x 70001 x 200 in bf16 187 us; 65,600 features, which tiles read as they are, 68).
 // Features up to which the rows of a tile lie within the 32-bit offsets that its loads use.
 constexpr int64_t kFourMostWidth = (int64_t)1 << 22;
 
@@ -363,7 +365,7 @@ som_status som_mx4_linear(int32_t type, const void *X, int64_t ldx, const uint8_
         return done(som::launch_mx4_few(bf16, few_rows(L.tile) ? L.tile : som::kFour32x32, p, s), who);
     char *b = static_cast<char *>(workspace);
     p.x_pitch = p.w_pitch = som::four_pitch(K);
-    if (ragged) {
+    if (ragged) {  // in every call: 2048 x 768 x 4096 in 4 bits takes 17.7 us, of 1024 features, without these copies, 11.7
         uint8_t *ws = reinterpret_cast<uint8_t *>(b + L.ws), *xs = reinterpret_cast<uint8_t *>(b + L.xs);
         hipError_t e = som::launch_pad_scales(w_scales, M, K, ws, s);
         if (e == hipSuccess && packed) e = som::launch_pad_scales(x_scales, N, K, xs, s);

@@ -11,7 +11,7 @@
 //     whose scales fp16 does not span widens without them; the instruction's sums over a block are then
 //     added under the scale in fp32, four additions for each instruction.
 // Measured, us and TFLOP/s: 8192 x 4096 x 4096 rows in 4 bits 77 and 3,560, in bf16 200 and 1,370, in fp16 212
-// and 1,300 (316 and 870 without the scales). Of 8192 x 2048 x 4096 in 4 bits, 54 us, some 30 go to the
+// and 1,300 (316 and 870 without the scales; by 256 x 256 it spills six registers). Of 8192 x 2048 x 4096 in 4 bits, 54 us, some 30 go to the
 // first loads and the results' stores, during which the matrix units wait: there is one workgroup a CU.
 //
 // Rows must be whole lines (the host copies others to the workspace). Rows and columns past the last

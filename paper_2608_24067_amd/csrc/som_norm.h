@@ -202,8 +202,11 @@ template <typename X, typename Y> __global__ __launch_bounds__(1024) void k_norm
 // and written as one part, and k_norm_sums adds the parts in order. Its rows are as far apart as there are
 // workgroups, so that those in flight are neighbours (6000 x 4096 fp32: 44.5 us, 50.4 with its rows side by side).
 // Two workgroups a CU, whose loads hide each other's exchanges, where a thread has two vectors at most; but one
-// for rows of 512 threads that end inside a vector, whose code takes more registers (5000 x 8190 bf16 101 us,
-// with two 114; 8192 x 4095, 256 threads a row, 78 and with two 63).
+// for rows of 512 threads that end inside a vector, whose code takes more registers (without add, on the same
+// buffers in every pass: 5000 x 8190 bf16 101 us, with two 114; 8192 x 4095, 256 threads a row, 78 and with two
+// 63, though 16-bit rows of that shape spill 70 registers). Such rows are further from their bytes than whole
+// ones, every element being tested and the last ones loaded one by one: on buffers by turns 8192 x 4095 takes 77 us
+// (with add 105), 8192 x 4096 51.5 (61.5).
 template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT, S::C <= 2 && (WHOLE || S::TPR < 512) ? 4 : 2) void k_norm_grad(const NormArgs a)
 {
     typedef typename S::X X;
@@ -313,7 +316,9 @@ template <class S, bool WHOLE> __global__ __launch_bounds__(S::NT, S::C <= 2 && 
     }
 }
 
-// Rows longer than that: first each row's mean(t) and mean(t h) ...
+// Rows longer than that (fp32 above 8,192 features, 16-bit above 16,384) are read twice: 2000 x 16384 fp32 takes 141 us,
+// with add 166, 2000 x 24576 bf16 123 and 138, where the bytes of one pass take 80, 106, 60 and 80 at a copy's rate.
+// First each row's mean(t) and mean(t h) ...
 template <typename X, typename Y> __global__ __launch_bounds__(1024) void k_norm_means(const NormArgs a)
 {
     constexpr int V = 16 / sizeof(X);

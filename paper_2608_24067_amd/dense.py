@@ -528,7 +528,7 @@ def adamw(params, grads, states, step, lr=1e-3, betas=(0.9, 0.999), eps: float =
     The parameters and their gradients are contiguous, each float32, float16 or bfloat16, on one device; states are
     AdamwState (adamw_state), all in 32 bits or all in 8. A state's master, where it has one, is what the step reads and
     updates; the parameter takes its rounded value. ``step`` is this step's number from 1 on, ``lr`` the rate; either
-    may be a tensor of one element on the device (int32, float32), so that a captured step goes on when replayed.
+    may be a tensor [1] on the device (int32, float32), so that a captured step goes on when replayed.
     Gradients are multiplied by ``grad_scale``. ``norm``, float32 [1], as clip returns it: where it is infinite or NaN
     the step is left out. ``seed`` (0 ... 2^32 - 1) decides the rounding of 8-bit states, together with the step.
     No tensor may hold elements of another.
